@@ -318,6 +318,108 @@ stepq_status stepq_pool_export_pivots(const stepq_pool *pool, const int32_t *slo
 stepq_status stepq_pool_import_pivots(stepq_pool *pool, const int32_t *slot_ids, int32_t n,
                                       const uint16_t *pivots, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Around the decode step: prompts, single tokens on full-precision states, and
+ * attention over a shared prefix.  The same conventions as above; these calls
+ * need no pool.  Workspaces are caller-owned device memory, 256-byte aligned,
+ * of at least the size the *_workspace call gives (host only, no device work);
+ * a workspace may be used again as soon as the stream has passed the call.
+ */
+
+/* The recurrence of one (sequence, value head), state S in R^{d_k x d_v}. */
+typedef enum {
+    STEPQ_RULE_DECAY = 0,     /* linear attention:  u = beta v */
+    STEPQ_RULE_DELTA = 1      /* gated Delta rule:  u = beta (v - alpha S^T k) */
+} stepq_rule;                 /* S <- alpha S + k u^T,  o = S^T q (after the update) */
+
+typedef struct {
+    int64_t n_tokens;         /* tokens of all sequences together, < 2^31 */
+    int32_t n_seq;            /* sequences */
+    int32_t n_v_heads;        /* Hv >= 1 */
+    int32_t n_qk_heads;       /* Hqk >= 1, Hv % Hqk == 0; value head h reads q/k head h / (Hv/Hqk) */
+    int32_t d_k;              /* 1 .. 128 */
+    int32_t d_v;              /* 64 or 128 */
+    int32_t act_dtype;        /* stepq_dtype of q, k, v and o */
+    int32_t gate_dtype;       /* stepq_dtype of alpha and beta */
+    int32_t rule;             /* stepq_rule */
+    int32_t n_states_in;      /* states in state_in (0 without it) */
+    /* elements from one token to the next (q, k, v may be slices of one
+     * projection's output); 0: tokens back to back */
+    int64_t q_stride, k_stride, v_stride, o_stride;
+} stepq_prompt_desc;
+
+/* Prompts: every token of n_seq packed sequences through the recurrence, from
+ * an initial state to the final one, in chunks on the matrix cores.  Sequence
+ * i is tokens cu_seqlens[i] .. cu_seqlens[i+1] (device, int32 [n_seq+1], from
+ * 0 up and never down; empty sequences keep their initial state).
+ *   q, k [n_tokens][Hqk][d_k], v, o [n_tokens][Hv][d_v] in act_dtype (token
+ *   strides above), alpha, beta [n_tokens][Hv] in gate_dtype, beta NULL: 1;
+ *   state_in [n_states_in][Hv][d_k][d_v] fp32, NULL: zeros; in_ids [n_seq]
+ *   int32: sequence i starts from state_in[in_ids[i]] (several may start from
+ *   one; an id outside [0, n_states_in): zeros), NULL: from state_in[i];
+ *   state_out [n_seq][Hv][d_k][d_v] fp32: what stepq_pool_load packs.
+ * alpha lies in [0, 1]: 0 forgets everything before the token, an alpha < 0
+ * gives NaN.  state_out may be state_in itself (in place) when in_ids is NULL,
+ * and must not overlap it otherwise.
+ * Sums, decays and states are fp32 or wider; o is rounded once, to act_dtype. */
+stepq_status stepq_prompt_workspace(const stepq_prompt_desc *desc, size_t *bytes);
+stepq_status stepq_prompt(const stepq_prompt_desc *desc, const int32_t *cu_seqlens, const void *q, const void *k,
+                          const void *v, const void *alpha, const void *beta, void *o, const float *state_in,
+                          const int32_t *in_ids, float *state_out, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+typedef struct {
+    int32_t n_states;         /* states in the array */
+    int32_t n_v_heads, n_qk_heads, d_k, d_v;   /* as in stepq_prompt_desc */
+    int32_t act_dtype;        /* stepq_dtype of q, k and v */
+    int32_t gate_dtype;       /* stepq_dtype of alpha and beta */
+    int32_t rule;             /* stepq_rule */
+} stepq_state_desc;
+
+/* One token of `batch` requests on full-precision states, in place: the single-
+ * token form of stepq_prompt, and stepq_decode_step without the quantization.
+ *   state [n_states][Hv][d_k][d_v] fp32; ids [batch] int32, distinct; a request
+ *   whose id is outside [0, n_states) is an empty row of the batch: its o is
+ *   zero and no state changes.  q, k [batch][Hqk][d_k], v [batch][Hv][d_v],
+ *   alpha, beta [batch][Hv] (beta NULL: 1), o [batch][Hv][d_v] fp32.
+ * fp32 arithmetic. */
+stepq_status stepq_state_step(const stepq_state_desc *desc, float *state, const int32_t *ids, int32_t batch,
+                              const void *q, const void *k, const void *v, const void *alpha, const void *beta, float *o,
+                              void *stream);
+
+typedef struct {
+    int32_t batch;
+    int32_t n_q_heads;        /* Hq */
+    int32_t n_kv_heads;       /* Hkv, Hq % Hkv == 0; query head h reads key/value head h / (Hq/Hkv) */
+    int32_t head_dim;         /* D: 64, 128 or 256 */
+    int32_t n_pages;          /* pages in each cache */
+    int32_t page_size;        /* tokens per page, >= 1 */
+    int64_t prefix_len;       /* tokens of the common prefix, >= 0 */
+    int32_t max_pages;        /* columns of page_table */
+    int32_t act_dtype;        /* stepq_dtype of q, the caches and o */
+    float scale;              /* scores are scale q.k */
+} stepq_attn_desc;
+
+/* Softmax attention of one query token of each of `batch` requests over the
+ * tokens of a prefix they all share, then their own:
+ *   o = sum_t p_t v_t,  p = softmax over t of scale q.k_t,  lse = log sum_t exp(scale q.k_t).
+ * The prefix is read once for the whole batch, its products being matrix
+ * products over all requests' queries; each request's own tokens are read once.
+ *   k_cache, v_cache [n_pages][Hkv][page_size][D];
+ *   prefix_pages [ceil(prefix_len / page_size)] int32: the prefix's pages;
+ *   page_table [batch][max_pages] int32, lengths [batch] int32: request b's own
+ *   tokens are the first lengths[b] of its pages (0 .. max_pages * page_size);
+ *   q, o [batch][Hq][D]; lse [batch][Hq] fp32 (natural logarithm) or NULL.
+ * Entries past a request's length, and cache rows past it, are not read or do
+ * not matter, whatever they hold.  Tokens of a page id outside [0, n_pages) are
+ * left out.  A row without any key, or with all scores -inf, gets o = 0 and
+ * lse = -inf. */
+stepq_status stepq_prefix_attention_workspace(const stepq_attn_desc *desc, size_t *bytes);
+stepq_status stepq_prefix_attention(const stepq_attn_desc *desc, const void *q, const void *k_cache,
+                                    const void *v_cache, const int32_t *prefix_pages, const int32_t *page_table,
+                                    const int32_t *lengths, void *o, float *lse, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
 /* Last failure message of the calling thread ("" if none). */
 const char *stepq_last_error(void);
 

@@ -12,6 +12,8 @@
 #include "stepq_internal.h"
 #include "stepq_plan.h"
 
+#include "stepq_seq.h"
+
 using stepq::HeadInfo;
 
 struct stepq_pool {
@@ -164,6 +166,12 @@ stepq_status common_checks(const stepq_pool *p, const int32_t *ids, int32_t n)
 }
 
 }  // namespace
+
+namespace stepq {
+
+stepq_status set_error(stepq_status s, const std::string &msg) { return fail(s, msg); }
+
+}  // namespace stepq
 
 extern "C" {
 

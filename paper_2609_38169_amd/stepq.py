@@ -23,6 +23,7 @@ LIB_PATH = os.environ.get("STEPQ_LIB") or os.path.join(_HERE, "libstepq.so")
 STEPQ_F32, STEPQ_BF16 = 0, 1
 STEPQ_LEVELS_ABSMAX, STEPQ_LEVELS_POW2 = 0, 1     # N1: z = q / q_b;  N2: z = 2^(8-b) q
 STEPQ_STEP_KDA_GATE, STEPQ_STEP_REFIT, STEPQ_STEP_ROW_ABSMAX, STEPQ_STEP_ADJACENT_SLOTS = 1, 2, 4, 8
+STEPQ_RULE_DECAY, STEPQ_RULE_DELTA = 0, 1         # u = beta v;  u = beta (v - alpha S^T k)
 _STATUS = {0: "STEPQ_OK", 1: "STEPQ_E_INVALID", 2: "STEPQ_E_UNSUPPORTED", 3: "STEPQ_E_NOMEM", 4: "STEPQ_E_HIP"}
 
 EXPORTED = (
@@ -34,6 +35,8 @@ EXPORTED = (
     "stepq_setup_fit_ex", "stepq_setup_fit_levels", "stepq_setup_lifetime_bits", "stepq_setup_row_impact", "stepq_setup_distortion",
     "stepq_setup_lifetime_weights", "stepq_setup_allocate", "stepq_setup_select_pivots",
     "stepq_setup_mean_log_retention", "stepq_setup_lifetime_costs", "stepq_setup_pivot_risk",
+    "stepq_prompt_workspace", "stepq_prompt", "stepq_state_step", "stepq_prefix_attention_workspace",
+    "stepq_prefix_attention",
 )
 
 
@@ -51,6 +54,23 @@ class stepq_pool_desc(ctypes.Structure):
     _fields_ = [("n_slots", ctypes.c_int32), ("n_v_heads", ctypes.c_int32), ("n_qk_heads", ctypes.c_int32),
                 ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32), ("row_bits", ctypes.c_void_p),
                 ("levels", ctypes.c_int32)]
+
+
+class stepq_prompt_desc(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in (
+        "n_seq", "n_v_heads", "n_qk_heads", "d_k", "d_v", "act_dtype", "gate_dtype", "rule", "n_states_in")] + [
+        (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "o_stride")]
+
+
+class stepq_state_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_states", "n_v_heads", "n_qk_heads", "d_k", "d_v", "act_dtype",
+                                              "gate_dtype", "rule")]
+
+
+class stepq_attn_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "n_pages", "page_size")] + [
+        ("prefix_len", ctypes.c_int64), ("max_pages", ctypes.c_int32), ("act_dtype", ctypes.c_int32),
+        ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -96,6 +116,11 @@ def lib():
             "stepq_last_error": ([], ctypes.c_char_p),
             "stepq_setup_fit": ([i64, i32, i32, P, P, P, P, i32], st),
             "stepq_setup_lifetime_bits": ([P, i32, i32, i32, i32, ctypes.c_double, i32, i32, P], st),
+            "stepq_prompt_workspace": ([P, P], st),
+            "stepq_prompt": ([P] * 12 + [ctypes.c_size_t, P], st),
+            "stepq_state_step": ([P, P, P, i32] + [P] * 7, st),
+            "stepq_prefix_attention_workspace": ([P, P], st),
+            "stepq_prefix_attention": ([P] * 10 + [ctypes.c_size_t, P], st),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -464,6 +489,194 @@ def _dev16(t, name, shape, device):
     if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int16, torch.uint16):
         raise TypeError(f"{name} must be a torch.int16 or torch.uint16 tensor of binary16 bit patterns")
     return _dev(t, name, t.dtype, shape, device)
+
+
+# ---------------------------------------------------------------------------
+# around the decode step: prompts, single tokens on full-precision states,
+# attention over a shared prefix
+def _act_dtype(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("activations must be float32 or bfloat16")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.dtype, STEPQ_F32 if t.dtype == torch.float32 else STEPQ_BF16
+
+
+def _tokens(t, name, dtype, shape, device):
+    """A tensor of tokens whose heads are contiguous: its pointer and the elements from one token to the next."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, q is on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    st, (n, h, d) = t.stride(), shape
+    if n and ((d > 1 and st[2] != 1) or (h > 1 and st[1] != d) or (n > 1 and st[0] < h * d)):
+        raise ValueError(f"{name}: each token's heads must be contiguous, and tokens must not overlap")
+    return ctypes.c_void_p(t.data_ptr()), st[0] if n > 1 else 0
+
+
+def _gates(alpha, beta, shape, device):
+    """(alpha, beta pointers, their dtype code); beta None: 1 everywhere."""
+    if not isinstance(alpha, torch.Tensor):
+        raise TypeError("alpha must be a torch.Tensor")
+    if alpha.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("alpha and beta must be float32 or bfloat16")
+    return (_dev(alpha, "alpha", alpha.dtype, shape, device),
+            None if beta is None else _dev(beta, "beta", alpha.dtype, shape, device),
+            STEPQ_F32 if alpha.dtype == torch.float32 else STEPQ_BF16)
+
+
+def _workspace(n, workspace, device, stream):
+    """Device memory of at least n bytes for one call on `stream`: the caller's, or torch's, taken on that
+    stream so that its next owner there comes after the call."""
+    if workspace is not None:
+        if not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+            raise TypeError("workspace must be a contiguous torch.uint8 tensor")
+        if workspace.device != device or workspace.numel() < n:
+            raise ValueError(f"workspace needs {n} bytes on {device}")
+        return workspace
+    if n == 0:
+        return None
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(s):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _ptr(t):
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def _prompt_desc(T, n_seq, Hv, Hqk, dk, dv, act, gate, rule, n_in, strides):
+    return stepq_prompt_desc(T, n_seq, Hv, Hqk, dk, dv, act, gate, int(rule), n_in, *strides)
+
+
+def stepq_prompt_workspace(n_tokens, n_seq, n_v_heads, n_qk_heads, d_k, d_v, rule, act_dtype=torch.bfloat16) -> int:
+    """Bytes of workspace a stepq_prompt call of these sizes takes."""
+    d = _prompt_desc(n_tokens, n_seq, n_v_heads, n_qk_heads, d_k, d_v,
+                     STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16, STEPQ_F32, rule, 0, (0, 0, 0, 0))
+    n = ctypes.c_size_t()
+    _check(lib().stepq_prompt_workspace(ctypes.byref(d), ctypes.byref(n)))
+    return n.value
+
+
+def stepq_prompt(q, k, v, alpha, beta, o, state_out, rule=STEPQ_RULE_DELTA, cu_seqlens=None, state_in=None, in_ids=None,
+                 workspace=None, stream=None):
+    """Packed prompts through the recurrence of `rule`: q, k [T][Hqk][d_k],
+    v, o [T][Hv][d_v] (float32 or bfloat16; slices of a wider token are
+    taken as they are), alpha, beta [T][Hv] (float32 or bfloat16; beta None:
+    1).  cu_seqlens [n+1] int32 (None: one sequence), state_in
+    [m][Hv][d_k][d_v] float32 (None: zeros), in_ids [n] int32 the state each
+    sequence starts from (None: its own), state_out [n][Hv][d_k][d_v]."""
+    dt, code = _act_dtype(q, "q")
+    dev = q.device
+    if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3:
+        raise ValueError("q and v must be [T][heads][d]")
+    (T, Hqk, dk), (Hv, dv) = q.shape, v.shape[1:]
+    qp, qs = _tokens(q, "q", dt, (T, Hqk, dk), dev)
+    kp, ks = _tokens(k, "k", dt, (T, Hqk, dk), dev)
+    vp, vs = _tokens(v, "v", dt, (T, Hv, dv), dev)
+    op, os_ = _tokens(o, "o", dt, (T, Hv, dv), dev)
+    ap, bp, gate = _gates(alpha, beta, (T, Hv), dev)
+    if cu_seqlens is None:
+        cu_seqlens = torch.tensor([0, T], dtype=torch.int32, device=dev)
+    if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+        raise ValueError("cu_seqlens must be a 1-D tensor of n + 1 entries")
+    n = cu_seqlens.shape[0] - 1
+    cu = _dev(cu_seqlens, "cu_seqlens", torch.int32, (n + 1,), dev)
+    out = _dev(state_out, "state_out", torch.float32, (n, Hv, dk, dv), dev)
+    sp, ip, m = None, None, 0
+    if state_in is not None:
+        m = state_in.shape[0] if in_ids is not None and isinstance(state_in, torch.Tensor) and state_in.dim() else n
+        sp = _dev(state_in, "state_in", torch.float32, (m, Hv, dk, dv), dev)
+        if in_ids is not None:
+            ip = _dev(in_ids, "in_ids", torch.int32, (n,), dev)
+        lo, hi = (state_in.data_ptr(), state_out.data_ptr()) if in_ids is not None or \
+            state_in.data_ptr() != state_out.data_ptr() else (0, 0)
+        if lo < hi + state_out.nbytes and hi < lo + state_in.nbytes and hi:
+            raise ValueError("state_out overlaps state_in")
+    elif in_ids is not None:
+        raise ValueError("in_ids without state_in")
+    d = _prompt_desc(T, n, Hv, Hqk, dk, dv, code, gate, rule, m, (qs, ks, vs, os_))
+    size = ctypes.c_size_t()
+    _check(lib().stepq_prompt_workspace(ctypes.byref(d), ctypes.byref(size)))
+    ws = _workspace(size.value, workspace, dev, stream)
+    _check(lib().stepq_prompt(ctypes.byref(d), cu, qp, kp, vp, ap, bp, op, sp, ip, out, _ptr(ws),
+                              0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def stepq_state_step(state, ids, q, k, v, alpha, beta, o, rule=STEPQ_RULE_DELTA, stream=None):
+    """One token of each request on full-precision states, in place: state
+    [n][Hv][d_k][d_v] float32, ids [B] int32 (distinct; outside [0, n): an
+    empty row), q, k [B][Hqk][d_k], v [B][Hv][d_v], alpha, beta [B][Hv]
+    (beta None: 1), o [B][Hv][d_v] float32."""
+    dt, code = _act_dtype(q, "q")
+    dev = q.device
+    if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3 or not isinstance(state, torch.Tensor) or state.dim() != 4:
+        raise ValueError("q and v must be [B][heads][d], state [n][Hv][d_k][d_v]")
+    (B, Hqk, dk), (Hv, dv) = q.shape, v.shape[1:]
+    d = stepq_state_desc(state.shape[0], Hv, Hqk, dk, dv, code, 0, int(rule))
+    ap, bp, d.gate_dtype = _gates(alpha, beta, (B, Hv), dev)
+    _check(lib().stepq_state_step(
+        ctypes.byref(d), _dev(state, "state", torch.float32, (state.shape[0], Hv, dk, dv), dev),
+        _dev(ids, "ids", torch.int32, (B,), dev), B, _dev(q, "q", dt, (B, Hqk, dk), dev),
+        _dev(k, "k", dt, (B, Hqk, dk), dev), _dev(v, "v", dt, (B, Hv, dv), dev), ap, bp,
+        _dev(o, "o", torch.float32, (B, Hv, dv), dev), _stream(stream)))
+
+
+def stepq_prefix_attention_workspace(batch, n_q_heads, n_kv_heads, head_dim, prefix_len, max_pages, page_size,
+                                     act_dtype=torch.bfloat16) -> int:
+    """Bytes of workspace a stepq_prefix_attention call of these sizes takes."""
+    d = stepq_attn_desc(batch, n_q_heads, n_kv_heads, head_dim, 0, page_size, prefix_len, max_pages,
+                        STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16, 1.0)
+    n = ctypes.c_size_t()
+    _check(lib().stepq_prefix_attention_workspace(ctypes.byref(d), ctypes.byref(n)))
+    return n.value
+
+
+def stepq_prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, lengths, o, lse=None, scale=None,
+                           workspace=None, stream=None):
+    """Softmax attention of one token of each request over prefix_len shared
+    tokens, then its own: q, o [B][Hq][D], k_cache, v_cache
+    [n_pages][Hkv][page][D] of q's dtype, prefix_pages [P] int32 (None
+    without a prefix), page_table [B][M] int32, lengths [B] int32, lse
+    [B][Hq] float32 (None: not wanted); scale defaults to D ** -0.5."""
+    dt, code = _act_dtype(q, "q")
+    dev = q.device
+    if q.dim() != 3 or not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("q must be [B][Hq][D], the caches [n_pages][Hkv][page][D]")
+    B, Hq, D = q.shape
+    n_pages, Hkv, page = k_cache.shape[:3]
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be [B][pages]")
+    prefix_len = int(prefix_len)
+    if prefix_len < 0 or page < 1:
+        raise ValueError("prefix_len must be >= 0 and pages hold at least one token")
+    P = -(-prefix_len // page)
+    if P:
+        if not isinstance(prefix_pages, torch.Tensor) or prefix_pages.dim() != 1 or prefix_pages.shape[0] < P:
+            raise ValueError(f"prefix_pages must list the prefix's {P} pages")
+        pp = _dev(prefix_pages, "prefix_pages", torch.int32, prefix_pages.shape, dev)
+    else:
+        pp = None
+    M = page_table.shape[1]
+    d = stepq_attn_desc(B, Hq, Hkv, D, n_pages, page, prefix_len, M, code, float(D ** -0.5 if scale is None else scale))
+    args = (_dev(q, "q", dt, (B, Hq, D), dev), _dev(k_cache, "k_cache", dt, (n_pages, Hkv, page, D), dev),
+            _dev(v_cache, "v_cache", dt, (n_pages, Hkv, page, D), dev), pp,
+            _dev(page_table, "page_table", torch.int32, (B, M), dev), _dev(lengths, "lengths", torch.int32, (B,), dev),
+            _dev(o, "o", dt, (B, Hq, D), dev),
+            None if lse is None else _dev(lse, "lse", torch.float32, (B, Hq), dev))
+    size = ctypes.c_size_t()
+    _check(lib().stepq_prefix_attention_workspace(ctypes.byref(d), ctypes.byref(size)))
+    ws = _workspace(size.value, workspace, dev, stream)
+    _check(lib().stepq_prefix_attention(ctypes.byref(d), *args, _ptr(ws), 0 if ws is None else ws.numel(),
+                                        _stream(stream)))
 
 
 def stepq_last_error() -> str:

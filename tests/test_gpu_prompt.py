@@ -1,0 +1,357 @@
+"""Prompts and single tokens on full-precision states against the recurrence
+in 64 bits.
+
+Tolerances.  State and output entries are sums of at most d_k + 64 products
+accumulated in fp32 (24 bits), each operand exact to 22 bits or more, and the
+gates keep earlier errors from growing: (128 + 64) 2^-24 = 1.1e-5 of the sum of
+the terms' magnitudes, taken as 3e-5 of the head's largest entry.  A bfloat16
+output is rounded once (8 significant bits: half a unit in the last place is up
+to 2^-8 of the value) from a value good to 2^-13 of the head's largest."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_38169_amd import stepq
+from _sequence import DECAY, DELTA, recurrence, tokens
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def close_f32(got, ref, what):
+    top = ref.abs().amax(dim=(-1, -2), keepdim=True) if ref.dim() > 1 else ref.abs().max()
+    off = (got.detach().cpu().double() - ref).abs()
+    assert (off <= 3e-5 * top + 1e-30).all(), (what, (off / (top + 1e-30)).max())
+
+
+def close_o(got, ref, what):
+    """ref [T][Hv][dv]; per head over all tokens."""
+    top = ref.abs().amax(dim=(0, 2), keepdim=True)
+    off = (got.detach().cpu().double() - ref).abs()
+    bound = 3e-5 * top if got.dtype == F32 else 2.0 ** -8 * ref.abs() + 2.0 ** -13 * top
+    assert (off <= bound + 1e-30).all(), (what, ((off - bound) / (top + 1e-30)).max())
+
+
+def run(lens, hv, hqk, dk, dv, act, gate, rule, start=None, seed=1, low=0.95, beta=True, edit=None, fused=False,
+        in_place=False, stream=None):
+    """The call on packed prompts, and the references: lists over the sequences."""
+    T = sum(lens)
+    q, k, v, alpha, b = tokens(T, hv, hqk, dk, dv, act, gate, seed, low)
+    if not beta:
+        b = None
+    if edit:
+        edit(q, k, v, alpha, b)
+    n = len(lens)
+    g = torch.Generator().manual_seed(seed + 7)
+    states = ids = None
+    if start == "own":
+        states = 0.3 * torch.randn((n, hv, dk, dv), generator=g)
+    elif start == "shared":
+        states = 0.3 * torch.randn((2, hv, dk, dv), generator=g)
+        ids = torch.tensor([(1, 0, -1, 5)[i % 4] for i in range(n)], dtype=torch.int32)
+    cu = torch.tensor([sum(lens[:i]) for i in range(n + 1)], dtype=torch.int32)
+    dev = lambda x: None if x is None else x.to(DEV)
+    if fused:
+        wide = torch.cat([q.reshape(T, -1), k.reshape(T, -1), v.reshape(T, -1)], 1).to(DEV)
+        nq = hqk * dk
+        Q, K, V = (wide[:, :nq].view(T, hqk, dk), wide[:, nq:2 * nq].view(T, hqk, dk), wide[:, 2 * nq:].view(T, hv, dv))
+    else:
+        Q, K, V = dev(q), dev(k), dev(v)
+    o = torch.full((T, hv, dv), 7.0, dtype=act, device=DEV)
+    S_in = dev(states)
+    out = S_in if in_place else torch.full((n, hv, dk, dv), 7.0, device=DEV)
+    args = (Q, K, V, dev(alpha), dev(b), o, out)
+    kw = dict(rule=rule, cu_seqlens=cu.to(DEV), state_in=S_in, in_ids=dev(ids))
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    stepq.stepq_prompt(*args, **kw, stream=stream)
+    torch.cuda.synchronize()
+    refs = []
+    for i in range(n):
+        j = i if ids is None else int(ids[i])
+        S0 = states[j] if states is not None and 0 <= j < states.shape[0] else torch.zeros(hv, dk, dv)
+        t = slice(int(cu[i]), int(cu[i + 1]))
+        refs.append(recurrence(q[t], k[t], v[t], alpha[t], None if b is None else b[t], S0, rule))
+    return o, out, refs, cu
+
+
+def check(*a, **kw):
+    o, out, refs, cu = run(*a, **kw)
+    for i, (ro, rs) in enumerate(refs):
+        if ro.shape[0]:
+            close_o(o[int(cu[i]):int(cu[i + 1])], ro, f"o of sequence {i}")
+        close_f32(out[i], rs, f"state of sequence {i}")
+
+
+LENS = [[1], [16], [63], [64], [65], [0, 1, 63, 0, 130, 2], [300, 5], [1000]]
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("lens", LENS, ids=lambda x: "-".join(map(str, x)))
+def test_lengths(lens, act, rule):
+    check(lens, 2, 1, 128, 128, act, F32, rule, start="own")
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("hv,hqk,dk,dv", [(4, 4, 64, 64), (6, 3, 77, 64), (3, 1, 96, 128), (2, 2, 128, 64), (5, 5, 37, 128),
+                                          (1, 1, 1, 64), (2, 1, 33, 128)])
+def test_heads(hv, hqk, dk, dv, act, rule):
+    check([70, 3, 129], hv, hqk, dk, dv, act, F32, rule, start="shared", seed=dk)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("dk", [128, 77])
+@pytest.mark.parametrize("act,gate", [(BF16, BF16), (BF16, F32), (F32, BF16)])
+def test_slices_of_one_projection(act, gate, dk, rule):
+    check([65, 200], 4, 2, dk, 64, act, gate, rule, fused=True)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_many_sequences(rule):
+    check([(7 * i) % 90 for i in range(150)], 1, 1, 64, 64, BF16, F32, rule, start="shared")
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_long(rule):
+    check([5000, 2500], 1, 1, 64, 64, BF16, F32, rule, low=0.99)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_without_beta(act, rule):
+    check([100], 2, 2, 64, 64, act, F32, rule, beta=False)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_gates_at_their_ends(act, rule):
+    """Zeros (documents that end inside a prompt), ones, subnormal and tiny gates, and all of them in a row."""
+    def edit(q, k, v, alpha, beta):
+        alpha[5], alpha[64], alpha[70:75], alpha[100:120], alpha[130] = 0.0, 0.0, 1.0, 1e-30, 1e-42
+        alpha[140:145], beta[20:25], beta[30] = 0.0, 0.0, 1.0
+        alpha[150:, 0] = 1.0
+    check([200], 2, 2, 64, 64, act, F32, rule, start="own", edit=edit)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_strong_decay(rule):
+    check([300], 2, 1, 128, 128, F32, F32, rule, start="own", low=0.01)
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_repeated_keys(act):
+    """The Delta rule on keys that repeat: its triangular system has entries as large as beta throughout."""
+    def edit(q, k, v, alpha, beta):
+        k[1:] = k[:1]
+        alpha[:], beta[:] = 1.0, 0.9
+    check([192], 2, 2, 64, 64, act, F32, DELTA, edit=edit)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_in_place(rule):
+    check([70, 0, 130], 2, 2, 64, 128, BF16, F32, rule, start="own", in_place=True)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_value_that_is_not_finite_stays_in_its_column(bad, act, rule):
+    """A non-finite v[j][h][c] reaches o[i][h][c] for i >= j and column c of the final state, and nothing else:
+    not the tokens before it, the other columns, heads or sequences."""
+    j, h, c = 90, 1, 37
+    clean = run([130, 70], 2, 1, 64, 64, act, F32, rule)
+
+    def edit(q, k, v, alpha, beta):
+        v[j, h, c] = bad
+    o, out, _, cu = run([130, 70], 2, 1, 64, 64, act, F32, rule, edit=edit)
+    hit = torch.zeros(200, 2, 64, dtype=torch.bool)
+    hit[j:130, h, c] = True
+    assert not torch.isfinite(o.cpu()[hit]).any()
+    assert torch.equal(o.cpu()[~hit], clean[0].cpu()[~hit])
+    hit = torch.zeros(2, 2, 64, 64, dtype=torch.bool)
+    hit[0, h, :, c] = True
+    assert not torch.isfinite(out.cpu()[hit]).any()
+    assert torch.equal(out.cpu()[~hit], clean[1].cpu()[~hit])
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("what", ["k", "alpha", "beta", "q"])
+def test_what_is_not_finite_does_not_reach_back(what, act, rule):
+    """A NaN key or gate at token j leaves the tokens before it, the other heads and sequences as they are,
+    and makes the head's o from j on NaN; a NaN query its own token's alone."""
+    j = 77
+    clean = run([130, 70], 2, 2, 64, 64, act, F32, rule)
+
+    def edit(q, k, v, alpha, beta):
+        if what == "k":
+            k[j, 1, 5] = math.nan
+        elif what == "q":
+            q[j, 1, 5] = math.nan
+        else:
+            dict(alpha=alpha, beta=beta)[what][j, 1] = math.nan
+    o, out, _, cu = run([130, 70], 2, 2, 64, 64, act, F32, rule, edit=edit)
+    hit = torch.zeros(200, 2, 64, dtype=torch.bool)
+    hit[j:j + 1 if what == "q" else 130, 1] = True
+    assert torch.isnan(o.cpu()[hit]).all()
+    assert torch.equal(o.cpu()[~hit], clean[0].cpu()[~hit])
+    assert torch.equal(out[1].cpu(), clean[1][1].cpu()) and torch.equal(out[0, 0].cpu(), clean[1][0, 0].cpu())
+    if what == "q":
+        assert torch.equal(out.cpu(), clean[1].cpu())
+    else:
+        assert torch.isnan(out[0, 1]).any()
+
+
+def test_another_stream():
+    s = torch.cuda.Stream()
+    check([200, 70], 2, 2, 64, 64, BF16, F32, DELTA, stream=s)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_graph(rule):
+    """Captured and replayed with other inputs in the same buffers."""
+    T, hv = 150, 2
+    x = [t.to(DEV) for t in tokens(T, hv, 2, 64, 64, BF16, F32, 3)]
+    o, out = torch.zeros((T, hv, 64), dtype=BF16, device=DEV), torch.zeros((2, hv, 64, 64), device=DEV)
+    cu = torch.tensor([0, 60, T], dtype=torch.int32, device=DEV)
+    call = lambda: stepq.stepq_prompt(*x, o, out, rule, cu_seqlens=cu)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in (4, 5, 6):
+        for a, b in zip(x, tokens(T, hv, 2, 64, 64, BF16, F32, seed)):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = o.clone(), out.clone()
+        o.zero_(), out.zero_()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], o) and torch.equal(got[1], out)
+
+
+def test_same_bits_every_time():
+    a = run([500, 33], 4, 2, 128, 128, BF16, F32, DELTA, start="own")
+    b = run([500, 33], 4, 2, 128, 128, BF16, F32, DELTA, start="own")
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_offsets_over_32_bits(rule):
+    """Tokens 2^26 elements apart: the last starts beyond 2^32 elements."""
+    T, step = 66, 1 << 26
+    q, k, v, alpha, beta = tokens(T, 1, 1, 64, 64, BF16, F32, 9)
+    wide = torch.empty((T, step), dtype=BF16, device=DEV)
+    V, O = wide[:, :64].view(T, 1, 64), wide[:, 64:128].view(T, 1, 64)
+    Q, K = wide[:, 128:192].view(T, 1, 64), wide[:, 192:256].view(T, 1, 64)
+    V.copy_(v), Q.copy_(q), K.copy_(k)
+    out = torch.empty((1, 1, 64, 64), device=DEV)
+    stepq.stepq_prompt(Q, K, V, alpha.to(DEV), beta.to(DEV), O, out, rule)
+    torch.cuda.synchronize()
+    ro, rs = recurrence(q, k, v, alpha, beta, torch.zeros(1, 64, 64), rule)
+    close_o(O, ro, "o")
+    close_f32(out[0], rs, "state")
+
+
+def test_malformed_cu_seqlens_stays_inside():
+    """Bounds past the tokens are cut, ones that go down give empty sequences."""
+    q, k, v, alpha, beta = (x.to(DEV) for x in tokens(100, 1, 1, 64, 64, BF16, F32, 2))
+    o, out = torch.zeros((100, 1, 64), dtype=BF16, device=DEV), torch.full((3, 1, 64, 64), 7.0, device=DEV)
+    cu = torch.tensor([0, 40, 30, 5000], dtype=torch.int32, device=DEV)
+    stepq.stepq_prompt(q, k, v, alpha, beta, o, out, DELTA, cu_seqlens=cu)
+    torch.cuda.synchronize()
+    assert torch.equal(out[1], torch.zeros_like(out[1]))
+
+
+# ---------------------------------------------------------------------------
+# one token at a time
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act,gate", [(F32, F32), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("hv,hqk,dk,dv", [(4, 4, 64, 64), (6, 3, 77, 64), (3, 1, 96, 128), (2, 2, 128, 128), (1, 1, 1, 64)])
+def test_single_tokens(hv, hqk, dk, dv, act, gate, rule):
+    B, n = 5, 9
+    g = torch.Generator().manual_seed(dk)
+    state = 0.3 * torch.randn((n, hv, dk, dv), generator=g)
+    ids = torch.tensor([3, 8, -1, 0, n], dtype=torch.int32)
+    S = state.to(DEV)
+    o = torch.full((B, hv, dv), 7.0, device=DEV)
+    ref = state.double().clone()
+    for t in range(3):
+        q, k, v, alpha, beta = tokens(B, hv, hqk, dk, dv, act, gate, t + 50)
+        beta = None if t == 1 else beta
+        stepq.stepq_state_step(S, ids.to(DEV), *(None if x is None else x.to(DEV) for x in (q, k, v, alpha, beta)), o, rule)
+        for b in range(B):
+            if not 0 <= int(ids[b]) < n:
+                assert not o[b].any()
+                continue
+            ro, ref[ids[b]] = recurrence(q[b:b + 1], k[b:b + 1], v[b:b + 1], alpha[b:b + 1],
+                                         None if beta is None else beta[b:b + 1], ref[ids[b]], rule)
+            close_o(o[b:b + 1], ro, f"o of request {b} at token {t}")
+    for i in range(n):
+        if i in (3, 8, 0):
+            close_f32(S[i], ref[i], f"state {i}")
+        else:
+            assert torch.equal(S[i].cpu(), state[i])
+
+
+def test_single_token_of_a_prompt():
+    """The two forms of the operator: tokens one by one from the state a prompt left."""
+    hv, T = 2, 20
+    x = [t.to(DEV) for t in tokens(T, hv, 1, 128, 128, F32, F32, 4)]
+    S = torch.empty((1, hv, 128, 128), device=DEV)
+    o = torch.empty((T, hv, 128), device=DEV)
+    stepq.stepq_prompt(*x, o, S, DELTA)
+    S2, o2, part = torch.empty_like(S), torch.empty((1, hv, 128), device=DEV), torch.empty((15, hv, 128), device=DEV)
+    stepq.stepq_prompt(*(t[:15].contiguous() for t in x), part, S2, DELTA)
+    ids = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for t in range(15, T):
+        stepq.stepq_state_step(S2, ids, *(y[t:t + 1].contiguous() for y in x), o2, DELTA)
+        assert torch.allclose(o2[0], o[t], rtol=0, atol=3e-5 * float(o.abs().max()))
+    assert torch.allclose(S2, S, rtol=0, atol=3e-5 * float(S.abs().max()))
+
+
+# ---------------------------------------------------------------------------
+# what is refused
+
+def test_refusals():
+    T, hv, hqk, dk, dv = 8, 4, 2, 64, 64
+    q, k, v, alpha, beta = (x.to(DEV) for x in tokens(T, hv, hqk, dk, dv, BF16, F32, 1))
+    o, S = torch.empty((T, hv, dv), dtype=BF16, device=DEV), torch.empty((1, hv, dk, dv), device=DEV)
+    call = stepq.stepq_prompt
+    with pytest.raises(TypeError):
+        call(q.half(), k, v, alpha, beta, o, S)
+    with pytest.raises(TypeError):
+        call(q, k.float(), v, alpha, beta, o, S)
+    with pytest.raises(ValueError):
+        call(q, k[:-1], v, alpha, beta, o, S)
+    with pytest.raises(ValueError):
+        call(q, k, v, alpha, beta, o, S[:, :1])
+    with pytest.raises(ValueError):
+        call(q.cpu(), k, v, alpha, beta, o, S)
+    with pytest.raises(ValueError):
+        call(q, k, v.transpose(1, 2), alpha, beta, o, S)
+    with pytest.raises(ValueError):
+        call(q, k, v[:, :, :60], alpha, beta, o[:, :, :60], S)
+    with pytest.raises(TypeError):
+        call(q, k, v, alpha, beta.bfloat16(), o, S)
+    with pytest.raises(ValueError):
+        call(q, k, v, alpha, beta, o, S, state_in=S, in_ids=torch.zeros(1, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
+        call(q, k, v, alpha, beta, o, S, in_ids=torch.zeros(1, dtype=torch.int32, device=DEV))
+    with pytest.raises(stepq.StepqError):
+        call(q, k, v, alpha, beta, o, S, rule=2)
+    wide = torch.empty((T, hv, 96), dtype=BF16, device=DEV)
+    with pytest.raises(stepq.StepqError):
+        call(q, k, wide, alpha, beta, torch.empty_like(wide), torch.empty((1, hv, dk, 96), device=DEV))
+    ids = torch.zeros(T, dtype=torch.int32, device=DEV)
+    with pytest.raises(stepq.StepqError):          # more requests than states
+        stepq.stepq_state_step(S, ids, q, k, v, alpha, beta, torch.empty((T, hv, dv), device=DEV))
+    with pytest.raises(TypeError):
+        stepq.stepq_state_step(S, ids, q, k, v, alpha, beta, o)
