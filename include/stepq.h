@@ -344,7 +344,7 @@ typedef struct {
     int32_t rule;             /* stepq_rule */
     int32_t n_states_in;      /* states in state_in (0 without it) */
     /* elements from one token to the next (q, k, v may be slices of one
-     * projection's output); 0: tokens back to back */
+     * projection's output), at most 2^26; 0: tokens back to back */
     int64_t q_stride, k_stride, v_stride, o_stride;
 } stepq_prompt_desc;
 

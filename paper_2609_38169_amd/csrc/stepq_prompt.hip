@@ -1,5 +1,8 @@
 // Prompts: packed sequences through the gated recurrences of stepq_rule.
-#include "stepq_seq.h"
+#include <algorithm>
+#include <type_traits>
+
+#include "stepq_mma.h"
 
 namespace stepq {
 namespace {
@@ -16,69 +19,905 @@ struct PromptArgs {
     int32_t T, n_seq, Hv, Hqk, dk, dv, n_in;
 };
 
-// The recurrence itself, token by token: a thread holds one column of the
-// state, a workgroup 64 columns of one (sequence, head).
-template <typename T, int DK, bool DELTA>
-__global__ __launch_bounds__(64) void prompt_tokens_kernel(PromptArgs a)
+// ---------------------------------------------------------------------------
+// Chunks of 64 tokens.  With G_i the product of the gates from the chunk's
+// first token to token i, D_ij = G_i / G_j (i >= j, else 0), S the state
+// before the chunk, and V, K, Q, O the chunk's rows:
+//   R = V - G (K S)            (Delta; R = V for the decay rule)
+//   U = T' R,  T' = (I + M)^-1 diag(beta),  M = strict lower part of beta_i D_ij (k_i . k_j)
+//   O = G (Q S) + P U,  P = D (Q K^T)
+//   S <- G_last S + K^T (w U),  w_j = G_last / G_j
+// (the decay rule has U = beta V).
+// Operands on the matrix cores are binary16 planes of a value times a power of
+// two, two planes (22 bits) each but for bfloat16 keys and queries, which are
+// exact in one.  O gets the same as the states: with one plane (11 bits) its
+// error before the rounding to bfloat16 reached 2^-12 of a head's largest entry.
+// T' and the gates' products depend on no state: a first launch forms them
+// for every chunk at once; the second walks each sequence's chunks in order.
+constexpr int kC = 64;
+
+// Per (chunk, head) of the workspace: the gates' products, then for the Delta
+// rule the two planes of T', lane by lane as operand A wants them.
+struct ChunkGates {
+    double lg[kC];           // log2 G_i: differences of them stay exact where G itself is 0 or tiny
+    float g[kC], w[kC], b[kC];
+    int32_t bad;             // first token whose key or gate is not finite (Delta; kC: none)
+    uint32_t tmax;           // largest |T'|, as bits
+    int32_t pad[30];
+};
+static_assert(sizeof(ChunkGates) == 1408, "record size");
+constexpr size_t kTBytes = 2 * 6 * 1024;
+
+struct ChunkArgs {
+    PromptArgs p;
+    uint8_t *ws;
+    size_t record;           // bytes per (chunk, head)
+    int32_t slots;           // chunk slots: sequence s owns those from cu[s] / 64 + s on
+};
+
+__device__ __forceinline__ int2 seq_bounds(const PromptArgs &a, int s)
 {
-    constexpr int N = 16;
-    __shared__ float sk[N][DK], sq[N][DK], sa[N], sb[N];
-    const int blocks = a.dv / 64, x = blockIdx.x;
-    const int col = (x % blocks) * 64 + threadIdx.x, h = x / blocks % a.Hv, s = x / blocks / a.Hv;
-    const int hq = h / (a.Hv / a.Hqk);
-    const int from = min(max(a.cu[s], 0), a.T), to = min(max(a.cu[s + 1], from), a.T);
-    const int src = a.state_in ? (a.in_ids ? a.in_ids[s] : s) : -1;
-    float S[DK];
-    const float *in = a.state_in + (static_cast<size_t>(src) * a.Hv + h) * a.dk * a.dv + col;
-#pragma unroll
-    for (int i = 0; i < DK; ++i)
-        S[i] = src >= 0 && src < a.n_in && i < a.dk ? in[static_cast<size_t>(i) * a.dv] : 0.0f;
-    for (int t0 = from; t0 < to; t0 += N) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < N * DK; e += 64) {
-            const int t = t0 + e / DK, i = e % DK;
-            const bool in_range = t < to && i < a.dk;
-            sk[e / DK][i] = in_range ? widen(static_cast<const T *>(a.k)[t * a.sk + hq * a.dk + i]) : 0.0f;
-            sq[e / DK][i] = in_range ? widen(static_cast<const T *>(a.q)[t * a.sq + hq * a.dk + i]) : 0.0f;
-        }
-        if (threadIdx.x < N && t0 + threadIdx.x < to) {
-            const size_t g = static_cast<size_t>(t0 + threadIdx.x) * a.Hv + h;
-            sa[threadIdx.x] = a.alpha.at(g);
-            sb[threadIdx.x] = a.beta.p ? a.beta.at(g) : 1.0f;
-        }
-        __syncthreads();
-        for (int n = 0; n < N && t0 + n < to; ++n) {
-            const size_t t = t0 + n;
-            float u = widen(static_cast<const T *>(a.v)[t * a.sv + h * a.dv + col]), ks = 0.0f, y = 0.0f;
-#pragma unroll
-            for (int i = 0; i < DK; ++i) {
-                if (i % 32 == 0) __builtin_amdgcn_sched_barrier(0);   // few rows of k in flight: no spills
-                S[i] *= sa[n];
-                if (DELTA) ks = fmaf(S[i], sk[n][i], ks);
-            }
-            u = sb[n] * (u - ks);
-#pragma unroll
-            for (int i = 0; i < DK; ++i) {
-                if (i % 32 == 0) __builtin_amdgcn_sched_barrier(0);
-                S[i] = fmaf(sk[n][i], u, S[i]);
-                y = fmaf(S[i], sq[n][i], y);
-            }
-            static_cast<T *>(a.o)[t * a.so + h * a.dv + col] = narrow<T>(y);
-        }
-    }
-    float *out = a.state_out + (static_cast<size_t>(s) * a.Hv + h) * a.dk * a.dv + col;
-#pragma unroll
-    for (int i = 0; i < DK; ++i)
-        if (i < a.dk) out[static_cast<size_t>(i) * a.dv] = S[i];
+    const int from = min(max(a.cu[s], 0), a.T);
+    return make_int2(from, min(max(a.cu[s + 1], from), a.T));
 }
 
-template <typename T, int DK>
-void launch(const PromptArgs &a, bool delta, hipStream_t s)
+__device__ __forceinline__ int first_slot(const PromptArgs &a, int s)
 {
-    const dim3 grid(static_cast<unsigned>(a.n_seq) * a.Hv * (a.dv / 64));
-    if (delta) prompt_tokens_kernel<T, DK, true><<<grid, 64, 0, s>>>(a);
-    else prompt_tokens_kernel<T, DK, false><<<grid, 64, 0, s>>>(a);
+    return min(max(a.cu[s], 0), a.T) / kC + s;
 }
+
+// The sequence that owns a chunk slot: the last one whose first slot is at most
+// x, found by the wave's 64 lanes at a time.
+__device__ __forceinline__ int owner(const PromptArgs &a, int x, int lane)
+{
+    int lo = 0, n = a.n_seq;            // the answer lies in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lo + lane * step;
+        const bool le = at < lo + n && first_slot(a, at) <= x;
+        const uint64_t yes = __ballot(le);
+        const int k = yes ? 63 - __clzll(yes) : 0;
+        const int end = lo + n;
+        lo += k * step;
+        n = min(step, end - lo);
+    }
+    return lo;
+}
+
+template <typename T>
+struct Act;
+template <>
+struct Act<bf16_t> {
+    static constexpr int planes = 1;
+    u32x4 x;
+};
+template <>
+struct Act<float> {
+    static constexpr int planes = 2;
+    f32x4 x[2];
+};
+
+// Row r of rows `stride` elements apart: one 64-bit multiply-add per lane, so
+// that no row's address is kept in scalar registers.
+template <typename T>
+__device__ __forceinline__ T *row_of(T *base, uint32_t r, int64_t stride)
+{
+    const uint64_t at = static_cast<uint64_t>(r) * static_cast<uint32_t>(stride * sizeof(T));
+    using B = std::conditional_t<std::is_const_v<T>, const uint8_t, uint8_t>;
+    return reinterpret_cast<T *>(reinterpret_cast<B *>(base) + at);
+}
+
+// 8 elements of a row of n valid ones from element i on.
+template <bool VEC, typename T>
+__device__ __forceinline__ Act<T> load8(const T *row, int i, int n)
+{
+    Act<T> r = {};
+    if constexpr (VEC) {
+        // n is a multiple of 8: past it, the first elements are read and dropped (no branch around the load)
+        const T *p = row + (i < n ? i : 0);
+        if constexpr (sizeof(T) == 2) {
+            r.x = *reinterpret_cast<const u32x4 *>(p);
+        } else {
+            r.x[0] = reinterpret_cast<const f32x4 *>(p)[0];
+            r.x[1] = reinterpret_cast<const f32x4 *>(p)[1];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (i + e < n) {
+                if constexpr (sizeof(T) == 2) r.x[e / 2] |= static_cast<uint32_t>(row[i + e]) << (16 * (e % 2));
+                else r.x[e / 4][e % 4] = row[i + e];
+            }
+    }
+    return r;
+}
+
+// A thread's share of a tile of 64 rows of C8 8-element units, N threads: unit c8 of the rows row + step u.
+template <int C8, int N>
+struct Share {
+    int row, c8;
+    __device__ __forceinline__ Share(int tid) : row(tid / C8), c8(tid % C8) {}
+    static constexpr int step = N / C8, units = kC / step;
+
+    // unit u of the `len` rows from `base` on; past the last row that one is read (valid() tells)
+    template <bool VEC, typename T>
+    __device__ __forceinline__ Act<T> load(const T *base, int64_t stride, int u, int n, int len) const
+    {
+        int r = row;
+        asm volatile("" : "+v"(r));          // the offset is formed at the load, not kept in registers from chunk to chunk
+        return load8<VEC>(row_of(base, min(r + step * u, len - 1), stride), 8 * c8, n);
+    }
+    __device__ __forceinline__ Share again() const
+    {
+        Share s = *this;
+        asm volatile("" : "+v"(s.row));
+        return s;
+    }
+    __device__ __forceinline__ bool valid(int u, int n, int len) const { return row + step * u < len && 8 * c8 < n; }
+};
+
+// Four outputs of a lane in their type.
+template <typename T>
+struct Out4;
+template <>
+struct Out4<float> {
+    f32x4 x;
+    __device__ __forceinline__ void set(const f32x4 &v) { x = v; }
+    __device__ __forceinline__ float at(int r) const { return x[r]; }
+};
+template <>
+struct Out4<bf16_t> {
+    using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+    uint32_t x[2];
+    __device__ __forceinline__ void set(const f32x4 &v)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            x[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2 * i], v[2 * i + 1]}), bf16x2));
+    }
+    __device__ __forceinline__ bf16_t at(int r) const { return static_cast<bf16_t>(r % 2 ? x[r / 2] >> 16 : x[r / 2]); }
+};
+
+template <typename T>
+__device__ __forceinline__ Act<T> zero_unless(bool keep, const Act<T> &v)
+{
+    Act<T> r;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.x[i] = keep ? v.x[i] : 0u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.x[i / 4][i % 4] = keep ? v.x[i / 4][i % 4] : 0.0f;
+    }
+    return r;
+}
+
+// |x|'s largest of 8 elements, as bits; what is not finite counts as nothing
+template <typename T>
+__device__ __forceinline__ uint32_t max8(uint32_t m, const Act<T> &v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a, b;
+        if constexpr (sizeof(T) == 2) a = lower_bf16(v.x[i]), b = upper_bf16(v.x[i]);
+        else a = v.x[i / 2][2 * (i % 2)], b = v.x[i / 2][2 * (i % 2) + 1];
+        m = max(m, max(__float_as_uint(fabsf(a)), __float_as_uint(fabsf(b))));
+    }
+    return m;
+}
+constexpr uint32_t kInfBits = 0x7f800000u;
+template <typename T>
+__device__ __forceinline__ uint32_t finite_max8(uint32_t m, const Act<T> &v)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float a;
+        if constexpr (sizeof(T) == 2) a = i % 2 ? upper_bf16(v.x[i / 2]) : lower_bf16(v.x[i / 2]);
+        else a = v.x[i / 4][i % 4];
+        const uint32_t u = __float_as_uint(fabsf(a));
+        m = u < kInfBits ? max(m, u) : m;
+    }
+    return m;
+}
+// of a thread's N units, over its wave
+template <int N, typename T>
+__device__ __forceinline__ uint32_t wave_max_of(const Act<T> (&v)[N])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = max8(m, v[i]);
+    uint32_t w = wave_max(m);
+    if (w >= kInfBits) {
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = finite_max8(m, v[i]);
+        w = wave_max(m);
+    }
+    return w;
+}
+
+// A tile of keys or queries: 64 rows of DKP elements in binary16 planes.  Their
+// summation slots are the elements in order (operands are 16-byte reads), so
+// the state, their partner, keeps element 32 kb + 8 g + 4 h + r of a column in
+// row 4 g + r of its block 2 kb + h.
+__device__ __forceinline__ int state_row(int block, int row)
+{
+    return 32 * (block >> 1) + 8 * (row >> 2) + 4 * (block & 1) + (row & 3);
+}
+
+template <typename T, int DKP>
+struct RowTile {
+    static constexpr int NA = Act<T>::planes, RB = DKP * 2;
+    alignas(16) uint8_t b[NA][kC * RB];
+
+    __device__ __forceinline__ void put(int row, int c8, const Act<T> &v, float up)
+    {
+        uint8_t *at = &b[0][row * RB + ((c8 ^ swizzle<RB>(row)) * 16)];
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (NA == 1) x[i] = i % 2 ? upper_bf16(v.x[i / 2]) : lower_bf16(v.x[i / 2]);
+            else x[i] = v.x[i / 4][i % 4];
+        }
+        f16x8 p[NA];
+        split(x, up, p);
+#pragma unroll
+        for (int n = 0; n < NA; ++n) *reinterpret_cast<f16x8 *>(at + n * kC * RB) = p[n];
+    }
+
+    // operand: row 16 rt + n, elements 32 kb .. 32 kb + 31
+    __device__ __forceinline__ void rows(int rt, int kb, int g, int n, f16x8 (&a)[NA]) const
+    {
+        const int row = 16 * rt + n;
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            a[i] = *reinterpret_cast<const f16x8 *>(&b[i][row * RB + (((4 * kb + g) ^ swizzle<RB>(n)) * 16)]);
+    }
+
+    // operand A of the transposed tile: tokens 32 kb .. 32 kb + 31 of state row state_row(dt, n)
+    __device__ __forceinline__ void columns(int dt, int kb, int g, int n, f16x8 (&a)[NA]) const
+    {
+        const int f = swizzle<RB>(4 * g + (n >> 2));
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            u32x4 w;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = 32 * kb + 16 * h + 4 * g + (n >> 2), slot = 4 * (dt / 2) + (n & 3);
+                const u32x2 x = read_columns(&b[i][row * RB + ((slot ^ f) * 16) + 8 * (dt & 1)]);
+                w[2 * h] = x[0], w[2 * h + 1] = x[1];
+            }
+            a[i] = __builtin_bit_cast(f16x8, w);
+        }
+    }
+};
+
+// A tile of values: 64 rows of W columns, bfloat16 or fp32 as given.
+template <typename T, int W>
+struct ValueTile {
+    static constexpr int RB = W * static_cast<int>(sizeof(T));
+    alignas(16) uint8_t b[kC * RB];
+
+    __device__ __forceinline__ void put(int row, int c8, const Act<T> &v)
+    {
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<u32x4 *>(&b[row * RB + ((c8 ^ swizzle<RB>(row)) * 16)]) = v.x;
+        } else {
+            // 16 columns at a time exchanged between the rows that one read takes together
+            const int col = (8 * c8) ^ (16 * ((row >> 2) & (W / 16 - 1)));
+            *reinterpret_cast<f32x4 *>(&b[row * RB + col * 4]) = v.x[0];
+            *reinterpret_cast<f32x4 *>(&b[row * RB + col * 4 + 16]) = v.x[1];
+        }
+    }
+
+    // rows 16 tt + 4 g .. + 3 of column col + n (col a multiple of 16)
+    __device__ __forceinline__ f32x4 four(int tt, int col, int g, int n) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            const int row = 16 * tt + 4 * g + (n >> 2), slot = col / 8 + ((n & 3) >> 1);
+            const u32x2 w = read_columns(&b[row * RB + ((slot ^ swizzle<RB>(row)) * 16) + 8 * (n & 1)]);
+            return f32x4{lower_bf16(w[0]), upper_bf16(w[0]), lower_bf16(w[1]), upper_bf16(w[1])};
+        } else {
+            f32x4 r;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = 16 * tt + 4 * g + j;
+                r[j] = *reinterpret_cast<const float *>(&b[row * RB + ((col ^ (16 * ((row >> 2) & (W / 16 - 1)))) + n) * 4]);
+            }
+            return r;
+        }
+    }
+};
+
+// Lower triangles of 64x64 as operand A: blocks 0 .. 5 of 16 rows x 32 columns, (0,0), (1,0), (2,0), (2,1), (3,0), (3,1)
+__device__ __forceinline__ constexpr int triangle_row(int b) { return b < 2 ? b : b < 4 ? 2 : 3; }
+__device__ __forceinline__ constexpr int triangle_block(int b) { return b < 2 ? 0 : b & 1; }
+
+template <int N>
+struct TriangleTile {
+    alignas(16) uint8_t b[N][6 * 1024];
+    __device__ __forceinline__ void put(int block, int lane, const f16x8 (&p)[N])
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<f16x8 *>(&b[i][block * 1024 + lane * 16]) = p[i];
+    }
+    __device__ __forceinline__ void put(int block, int lane, const f32x4 &lo, const f32x4 &hi, float up)
+    {
+        f16x8 p[N];
+        split(lo, hi, up, p);
+        put(block, lane, p);
+    }
+    __device__ __forceinline__ void rows(int rb, int kb, int lane, f16x8 (&a)[N]) const
+    {
+        const int block = rb < 2 ? rb : 2 * rb - 2 + kb;
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[i] = *reinterpret_cast<const f16x8 *>(&b[i][block * 1024 + lane * 16]);
+    }
+};
+
+__device__ __forceinline__ float decay(double from, double to) { return __builtin_amdgcn_exp2f(static_cast<float>(to - from)); }
+
+// log2 of a gate; 0 becomes a finite value whose powers are 0
+__device__ __forceinline__ double log2_gate(float a) { return a == 0.0f ? -1000.0 : log2(static_cast<double>(a)); }
+
+// The gates' products of a chunk of n tokens from t0 on, lane i token i: log2 G_i.
+__device__ __forceinline__ double scan_gates(const PromptArgs &a, int t0, int n, int h, int lane, float *beta, bool *fine)
+{
+    double lg = 0.0;
+    *beta = 0.0f;
+    *fine = true;
+    if (lane < n) {
+        const size_t at = static_cast<size_t>(t0 + lane) * a.Hv + h;
+        const float al = a.alpha.at(at);
+        *beta = a.beta.p ? a.beta.at(at) : 1.0f;
+        lg = log2_gate(al);
+        *fine = fabsf(al) < INFINITY && fabsf(*beta) < INFINITY;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const double up = __shfl_up(lg, d);
+        if (lane >= d) lg += up;
+    }
+    return lg;
+}
+
+__device__ __forceinline__ void put_gates(ChunkGates *r, int lane, double lg, float beta, int bad)
+{
+    const double last = __shfl(lg, 63);
+    r->lg[lane] = lg;
+    r->g[lane] = decay(0.0, lg);
+    r->w[lane] = decay(lg, last);
+    r->b[lane] = beta;
+    if (lane == 0) r->bad = bad;
+}
+
+// First launch, decay rule: a wave per (chunk, head).
+__global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int x = static_cast<int>(id / a.p.Hv), h = static_cast<int>(id - static_cast<int64_t>(x) * a.p.Hv);
+    if (x >= a.slots) return;
+    const int s = owner(a.p, x, lane);
+    const int2 be = seq_bounds(a.p, s);
+    const int t0 = be.x + (x - first_slot(a.p, s)) * kC, n = min(kC, be.y - t0);
+    if (n <= 0) return;
+    float beta;
+    bool fine;
+    const double lg = scan_gates(a.p, t0, n, h, lane, &beta, &fine);
+    put_gates(reinterpret_cast<ChunkGates *>(a.ws + id * a.record), lane, lg, beta, kC);
+}
+
+// First launch, Delta rule: a workgroup per (chunk, head) forms T'.  Wave w owns
+// the 16 rows of row block w: k_i . k_j on the matrix cores, the 16x16 diagonal
+// block's inverse by substitution, then the blocks left of it from
+//   T_wc = -T_ww sum_{c <= l < w} M_wl T_lc
+// in fp32 products, the blocks at equal distance from the diagonal together.
+template <typename T, int DKP, bool VEC>
+__global__ __launch_bounds__(256) void prompt_solve_kernel(ChunkArgs a)
+{
+    constexpr int NA = Act<T>::planes, U = DKP / 32, LD = 68;
+    __shared__ RowTile<T, DKP> K;
+    __shared__ alignas(16) float M[kC][LD], X[kC][LD];
+    __shared__ double lgs[kC];
+    __shared__ float bs[kC];
+    __shared__ int bad_s;
+    __shared__ uint32_t tmax_s, kmax_s[4];
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, n = lane & 15;
+    const Share<DKP / 8, 256> sh(tid);
+    const int x = blockIdx.x / a.p.Hv, h = blockIdx.x - x * a.p.Hv, hq = h / (a.p.Hv / a.p.Hqk);
+    const int s = owner(a.p, x, lane);
+    const int2 be = seq_bounds(a.p, s);
+    const int64_t t0 = be.x + (x - first_slot(a.p, s)) * kC;
+    const int len = min(kC, be.y - static_cast<int>(t0));
+    if (len <= 0) return;
+    if (tid == 0) bad_s = kC, tmax_s = 0;
+    Act<T> v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        v[i] = sh.template load<VEC>(static_cast<const T *>(a.p.k) + t0 * a.p.sk + hq * a.p.dk, a.p.sk, i, a.p.dk, len);
+    }
+    float beta;
+    bool fine;
+    const double lg = scan_gates(a.p, t0, len, h, lane, &beta, &fine);
+#pragma unroll
+    for (int i = 0; i < U; ++i) v[i] = zero_unless(sh.valid(i, a.p.dk, len), v[i]);
+    kmax_s[w] = wave_max_of(v);
+    __syncthreads();
+    const Pow2 sk = scale_for(max(max(kmax_s[0], kmax_s[1]), max(kmax_s[2], kmax_s[3])));
+    if (!fine) atomicMin(&bad_s, lane);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int row = sh.row + sh.step * i;
+        float z = 0.0f;                       // 0 x stays 0 for finite x alone
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (NA == 1) z = fmaf(lower_bf16(v[i].x[e]), 0.0f, fmaf(upper_bf16(v[i].x[e]), 0.0f, z));
+            else z = fmaf(v[i].x[0][e], 0.0f, fmaf(v[i].x[1][e], 0.0f, z));
+        }
+        if (z != 0.0f) atomicMin(&bad_s, row);
+        K.put(row, sh.c8, v[i], sk.up);
+    }
+    if (w == 0) lgs[lane] = lg, bs[lane] = beta;
+    __syncthreads();
+    const int bad = bad_s;
+    uint8_t *rec = a.ws + (static_cast<size_t>(x) * a.p.Hv + h) * a.record;
+    if (w == 0) put_gates(reinterpret_cast<ChunkGates *>(rec), lane, lg, beta, bad);
+    // M: lane (g, n) holds row i = 16 w + n, columns 16 tt + 4 g .. + 3
+    f16x8 mine[DKP / 32][NA];
+#pragma unroll
+    for (int kb = 0; kb < DKP / 32; ++kb) K.rows(w, kb, g, n, mine[kb]);
+    const int row_i = 16 * w + n;
+    const double lgi = lgs[row_i];
+    const float bi = bs[row_i];
+    for (int tt = 0; tt <= w; ++tt) {
+        f32x4 c = {};
+#pragma unroll
+        for (int kb = 0; kb < DKP / 32; ++kb) {
+            f16x8 k[NA];
+            K.rows(tt, kb, g, n, k);
+            mma<2>(c, k, mine[kb]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int j = 16 * tt + 4 * g + r;
+            c[r] = j < row_i && row_i < bad ? bi * decay(lgs[j], lgi) * (c[r] * sk.down * sk.down) : 0.0f;
+        }
+        *reinterpret_cast<f32x4 *>(&M[row_i][16 * tt + 4 * g]) = c;
+    }
+    __syncthreads();
+    {
+        // column n of the diagonal block's inverse (every group of 16 lanes forms it)
+        float t[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float y = i == n ? 1.0f : 0.0f;
+#pragma unroll
+            for (int l = 0; l < i; ++l) y = fmaf(-M[16 * w + i][16 * w + l], t[l], y);
+            t[i] = y;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if ((i >> 2) == g) X[16 * w + i][16 * w + n] = t[i];
+    }
+    for (int d = 1; d < 4; ++d) {
+        __syncthreads();
+        if (w >= d) {
+            const int c = w - d;
+            f32x4 y = {};
+            for (int l = c; l < w; ++l) {
+                const f32x4 m = *reinterpret_cast<const f32x4 *>(&M[16 * w + n][16 * l + 4 * g]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    y = __builtin_amdgcn_mfma_f32_16x16x4f32(m[r], X[16 * l + 4 * g + r][16 * c + n], y, 0, 0, 0);
+            }
+            const f32x4 tw = *reinterpret_cast<const f32x4 *>(&X[16 * w + n][16 * w + 4 * g]);
+            f32x4 z = {};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z = __builtin_amdgcn_mfma_f32_16x16x4f32(tw[r], y[r], z, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) X[16 * w + 4 * g + r][16 * c + n] = -z[r];
+        }
+    }
+    __syncthreads();
+    // beta into the columns, then block by block to the record
+    uint32_t top = 0;
+    for (int tt = 0; tt <= w; ++tt) {
+        f32x4 *at = reinterpret_cast<f32x4 *>(&X[row_i][16 * tt + 4 * g]);
+        f32x4 y = *at;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int j = 16 * tt + 4 * g + r;
+            y[r] = j < bad ? y[r] * bs[j] : 0.0f;
+            top = max(top, __float_as_uint(fabsf(y[r])));
+        }
+        *at = y;
+    }
+    top = wave_max(top);
+    if (lane == 0) atomicMax(&tmax_s, top);
+    __syncthreads();
+    const uint32_t tmax = tmax_s;
+    if (tid == 0) reinterpret_cast<ChunkGates *>(rec)->tmax = tmax;
+    for (int b = w; b < 6; b += 4) {
+        const int rb = triangle_row(b), kb = triangle_block(b);
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(&X[16 * rb + n][32 * kb + 4 * g]);
+        const f32x4 hi = 2 * kb + 1 <= rb ? *reinterpret_cast<const f32x4 *>(&X[16 * rb + n][32 * kb + 16 + 4 * g]) : f32x4{};
+        f16x8 pl[2];
+        split(lo, hi, scale_for(tmax).up, pl);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<f16x8 *>(rec + sizeof(ChunkGates) + i * 6144 + b * 1024 + lane * 16) = pl[i];
+    }
+}
+
+// f(address, rt, r) for the rows of a state that a lane holds, column n of `base`.
+template <int DKP, typename F, typename P>
+__device__ __forceinline__ void each_state_row(P *base, int dk, int dv, int g, int n, const F &f)
+{
+    int first = 8 * g;
+    asm volatile("" : "+v"(first));          // addresses and masks are formed here, not kept for the other call
+    const uint32_t at = static_cast<uint32_t>(first) * dv + n;
+#pragma unroll
+    for (int rt = 0; rt < DKP / 16; ++rt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int up = state_row(rt, r);
+            if (dk == DKP || first + up < dk) f(base + static_cast<int64_t>(up) * dv + at, rt, r);
+        }
+}
+
+__device__ __forceinline__ uint32_t tile_max(const f32x4 (&x)[4])
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[rb][r]));
+    return __float_as_uint(m);
+}
+
+// Second launch: a workgroup of NW waves walks the chunks of one (sequence, head)
+// for 16 NW value columns, a wave holds 16 columns of the state in registers
+// (result layout: lane n column n).  Every product with the state, and every
+// one after it, keeps the columns in their lanes, so that the waves share only
+// what is read, and each column of an operand has a power of two of its own.
+template <typename T, int DKP, int NW, bool DELTA, bool VEC>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void prompt_chunks_kernel(ChunkArgs a)
+{
+    constexpr int NA = Act<T>::planes, KB = DKP / 32, W = 16 * NW;
+    using ShareQ = Share<DKP / 8, 64 * NW>;
+    using ShareV = Share<W / 8, 64 * NW>;
+    constexpr int UQ = ShareQ::units, UV = ShareV::units;
+    __shared__ RowTile<T, DKP> K, Q;
+    __shared__ ValueTile<T, W> V;
+    __shared__ TriangleTile<2> P;
+    __shared__ std::conditional_t<DELTA, TriangleTile<2>, char> Tt;
+    __shared__ struct alignas(16) {
+        double lg[kC];
+        float g[kC], w[kC], b[kC];
+    } ga;
+    __shared__ uint32_t tops[2][NW];
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+    // Addresses in LDS follow from the lane: formed again in each phase, they do not hold registers from chunk to chunk.
+    const auto again = [&] {
+        asm volatile("" : "+v"(lane));
+        g = lane >> 4, n = lane & 15;
+    };
+    const ShareQ sh(threadIdx.x);
+    const ShareV sv(threadIdx.x);
+    const int blocks = a.p.dv / W;
+    const int cb = blockIdx.x % blocks, h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv;
+    const int hq = h / (a.p.Hv / a.p.Hqk);
+    const int col0 = cb * W, mycol = wv * 16;
+    const int2 be = seq_bounds(a.p, s);
+    const int chunks = (be.y - be.x + kC - 1) / kC;
+    const uint8_t *records = a.ws + (static_cast<size_t>(first_slot(a.p, s)) * a.p.Hv + h) * a.record;
+
+    f32x4 S[DKP / 16];
+    {
+        const int src = a.p.state_in ? (a.p.in_ids ? a.p.in_ids[s] : s) : -1;
+#pragma unroll
+        for (int rt = 0; rt < DKP / 16; ++rt) S[rt] = f32x4{};
+        if (src >= 0 && src < a.p.n_in)
+            each_state_row<DKP>(a.p.state_in + (static_cast<size_t>(src) * a.p.Hv + h) * a.p.dk * a.p.dv + col0 + mycol,
+                                a.p.dk, a.p.dv, g, n, [&](const float *at, int rt, int r) { S[rt][r] = *at; });
+    }
+
+    // What the next chunk needs is on its way while this one is computed, each
+    // part in registers for as short as its latency allows: keys and queries
+    // from the second barrier on, values and gates from the state's update on;
+    // T' from the chunk's own first barrier to its third.
+    Act<T> kx[UQ], qx[UQ], vx[UV];
+    f16x8 tx[8 / NW][2];
+    double lgx = 0.0;
+    float gx = 0.0f, wx = 0.0f, bx = 0.0f;
+    const auto record = [&](int c) { return records + static_cast<size_t>(c) * a.p.Hv * a.record; };
+    const auto fetch = [&](int c) {
+        const int64_t t0 = be.x + c * kC;
+        const int len = min(kC, be.y - static_cast<int>(t0));
+#pragma unroll
+        for (int i = 0; i < UQ; ++i) {
+            kx[i] = sh.template load<VEC>(static_cast<const T *>(a.p.k) + t0 * a.p.sk + hq * a.p.dk, a.p.sk, i, a.p.dk, len);
+            qx[i] = sh.template load<VEC>(static_cast<const T *>(a.p.q) + t0 * a.p.sq + hq * a.p.dk, a.p.sq, i, a.p.dk, len);
+        }
+    };
+    // values past the last token repeat it: their rows of U are 0 (beta is 0 there)
+    const auto fetch_values = [&](int c) {
+        const int64_t t0 = be.x + c * kC;
+        const int len = min(kC, be.y - static_cast<int>(t0));
+#pragma unroll
+        for (int i = 0; i < UV; ++i)
+            vx[i] = sv.template load<VEC>(static_cast<const T *>(a.p.v) + t0 * a.p.sv + h * a.p.dv + col0, a.p.sv, i, W, len);
+        const ChunkGates *cg = reinterpret_cast<const ChunkGates *>(record(c));
+        if (wv == 0) lgx = cg->lg[lane], gx = cg->g[lane], wx = cg->w[lane], bx = cg->b[lane];
+    };
+    if (chunks > 0) fetch(0), fetch_values(0);
+
+    for (int c = 0; c < chunks; ++c) {
+        const int64_t t0 = be.x + c * kC;
+        const int len = min(kC, be.y - static_cast<int>(t0));
+        if (len < kC || a.p.dk < DKP) {
+#pragma unroll
+            for (int i = 0; i < UQ; ++i) {
+                const bool keep = sh.valid(i, a.p.dk, len);
+                kx[i] = zero_unless(keep, kx[i]), qx[i] = zero_unless(keep, qx[i]);
+            }
+        }
+        again();
+        tops[0][wv] = wave_max_of(kx);
+        tops[1][wv] = wave_max_of(qx);
+        lds_barrier();
+        const ChunkGates *cg = reinterpret_cast<const ChunkGates *>(record(c));
+        int bad = kC;
+        uint32_t tmax = 0;
+        if constexpr (DELTA) {
+            const f16x8 *from = reinterpret_cast<const f16x8 *>(cg + 1) + lane;
+#pragma unroll
+            for (int i = 0; i < 8 / NW; ++i)
+                if (wv + NW * i < 6) tx[i][0] = from[(wv + NW * i) * 64], tx[i][1] = from[(wv + NW * i + 6) * 64];
+            bad = cg->bad, tmax = cg->tmax;
+        }
+        uint32_t mk = 0, mq = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) mk = max(mk, tops[0][i]), mq = max(mq, tops[1][i]);
+        const Pow2 sk = scale_for(mk), sq = scale_for(mq);
+        const auto at = sh.again();
+#pragma unroll
+        for (int i = 0; i < UQ; ++i) {
+            K.put(at.row + at.step * i, at.c8, kx[i], sk.up);
+            Q.put(at.row + at.step * i, at.c8, qx[i], sq.up);
+        }
+        const auto av = sv.again();
+#pragma unroll
+        for (int i = 0; i < UV; ++i) V.put(av.row + av.step * i, av.c8, vx[i]);
+        if (wv == 0) ga.lg[lane] = lgx, ga.g[lane] = gx, ga.w[lane] = wx, ga.b[lane] = bx;
+        lds_barrier();
+        if (c + 1 < chunks) fetch(c + 1);
+
+        again();
+        // P times 2^-22 of the scales (|q.k| < 2^35 scaled), a block of 16 rows x 32 columns to a wave:
+        // lane (g, n) forms row i = 16 rb + n, columns 16 tt + 4 g .. + 3
+#pragma unroll
+        for (int b = wv; b < 6; b += NW) {
+            const int rb = triangle_row(b), pb = triangle_block(b);
+            f16x8 q[KB][NA];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) Q.rows(rb, kb, g, n, q[kb]);
+            const double lgi = ga.lg[16 * rb + n];
+            f32x4 y[2] = {};
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int tt = 2 * pb + hh;
+                if (tt <= rb) {
+                    f32x4 x = {};
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) {
+                        f16x8 k[NA];
+                        K.rows(tt, kb, g, n, k);
+                        mma<2>(x, k, q[kb]);
+                    }
+                    float d[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) d[r] = x[r] * decay(ga.lg[16 * tt + 4 * g + r], lgi);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[hh][r] = ((tt < rb) | (4 * g + r <= n)) ? d[r] : 0.0f;
+                }
+            }
+            P.put(b, lane, y[0], y[1], 0x1p-22f);
+        }
+        again();
+        // K S and Q S
+        f32x4 ks[4], o[4];
+        float sm = 0.0f;
+#pragma unroll
+        for (int rt = 0; rt < DKP / 16; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sm = fmaxf(sm, fabsf(S[rt][r]));
+        const Pow2 ss = scale_for(column_max(__float_as_uint(sm)));
+#pragma unroll
+        for (int rb = 0; rb < 4; ++rb) ks[rb] = o[rb] = f32x4{};
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            f16x8 sp[2];
+            split(S[2 * kb], S[2 * kb + 1], ss.up, sp);
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb) {
+                f16x8 q[NA];
+                Q.rows(rb, kb, g, n, q);
+                mma<2>(o[rb], q, sp);
+                if constexpr (DELTA) {
+                    f16x8 k[NA];
+                    K.rows(rb, kb, g, n, k);
+                    mma<2>(ks[rb], k, sp);
+                }
+            }
+        }
+        again();
+        // R (Delta) or U (decay), and whether it is finite; O's part from the state
+        float z = 0.0f;
+#pragma unroll
+        for (int rb = 0; rb < 4; ++rb) {
+            const f32x4 gg = *reinterpret_cast<const f32x4 *>(&ga.g[16 * rb + 4 * g]);
+            f32x4 bb = {};
+            if (!DELTA) bb = *reinterpret_cast<const f32x4 *>(&ga.b[16 * rb + 4 * g]);
+            const f32x4 v = V.four(rb, mycol, g, n);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (DELTA) ks[rb][r] = fmaf(-(gg[r] * sk.down), ks[rb][r] * ss.down, v[r]);
+                else ks[rb][r] = v[r] * bb[r];
+                z = fmaf(ks[rb][r], 0.0f, z);
+                o[rb][r] = (gg[r] * sq.down) * (o[rb][r] * ss.down);
+            }
+        }
+        // tokens from `from` on are lost in their column: what is not finite there may not reach the others
+        // through products with zeros, so it is taken out and put in its place at the end
+        const bool lost = bad < kC || __any(z != 0.0f);
+        int from = kC;
+        if (lost) {
+            from = bad;
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (!(fabsf(ks[rb][r]) < INFINITY)) from = min(from, 16 * rb + 4 * g + r);
+            from = kC - static_cast<int>(column_max(kC - from));
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * rb + 4 * g + r >= from) ks[rb][r] = 0.0f;
+        }
+        if constexpr (DELTA)
+#pragma unroll
+            for (int i = 0; i < 8 / NW; ++i)
+                if (wv + NW * i < 6) Tt.put(wv + NW * i, lane, tx[i]);
+        lds_barrier();
+        again();
+        // U = T' R: in ks, times fu
+        float fu = 1.0f;
+        if constexpr (DELTA) {
+            const Pow2 sr = scale_for(column_max(tile_max(ks)));
+            const Pow2 st = scale_for(tmax);
+            fu = st.down * sr.down;
+            f16x8 rp[2][2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], sr.up, rp[kb]);
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb) {
+                ks[rb] = f32x4{};
+#pragma unroll
+                for (int kb = 0; kb <= rb / 2; ++kb) {
+                    f16x8 t[2];
+                    Tt.rows(rb, kb, lane, t);
+                    mma<2>(ks[rb], t, rp[kb]);
+                }
+            }
+        }
+        const Pow2 su = scale_for(column_max(tile_max(ks)));
+        fu *= su.down;
+        again();
+        // O += P U
+        {
+            f16x8 up[2][2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], su.up, up[kb]);
+            const float f = (sk.down * sq.down * 0x1p22f) * fu;
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb) {
+                f32x4 y = {};
+#pragma unroll
+                for (int kb = 0; kb <= rb / 2; ++kb) {
+                    f16x8 p[2];
+                    P.rows(rb, kb, lane, p);
+                    mma<2>(y, p, up[kb]);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[rb][r] = fmaf(y[r], f, o[rb][r]);
+            }
+        }
+        if (lost)
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * rb + 4 * g + r >= from) o[rb][r] = NAN;
+        Out4<T> y[4];
+#pragma unroll
+        for (int rb = 0; rb < 4; ++rb) y[rb].set(o[rb]);
+        const auto store = [&] {
+            T *out = static_cast<T *>(a.p.o) + t0 * a.p.so + h * a.p.dv + col0 + mycol + n;
+            const int row4 = 4 * g;
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * rb + row4 + r;
+                    if (len == kC || row < len) *row_of(out, row, a.p.so) = y[rb].at(r);
+                }
+        };
+        // bfloat16 outputs wait in half the registers, so that what the next chunk needs is asked for first
+        if constexpr (sizeof(T) == 4) again(), store();
+        if (c + 1 < chunks) fetch_values(c + 1);
+        again();
+        // S <- G_last S + K^T (w U)
+        {
+            const float glast = ga.g[kC - 1], f = sk.down * fu;
+            f16x8 up[2][2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&ga.w[32 * kb + 4 * g]);
+                const f32x4 w1 = *reinterpret_cast<const f32x4 *>(&ga.w[32 * kb + 16 + 4 * g]);
+                split(ks[2 * kb] * w0, ks[2 * kb + 1] * w1, su.up, up[kb]);
+            }
+#pragma unroll
+            for (int rt = 0; rt < DKP / 16; ++rt) {
+                f32x4 y = {};
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    f16x8 k[NA];
+                    K.columns(rt, kb, g, n, k);
+                    mma<2>(y, k, up[kb]);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[rt][r] = fmaf(S[rt][r], glast, y[r] * f);
+            }
+        }
+        if (lost && from < kC)
+#pragma unroll
+            for (int rt = 0; rt < DKP / 16; ++rt) S[rt] = f32x4{NAN, NAN, NAN, NAN};
+        if constexpr (sizeof(T) == 2) again(), store();
+    }
+
+    each_state_row<DKP>(a.p.state_out + (static_cast<size_t>(s) * a.p.Hv + h) * a.p.dk * a.p.dv + col0 + mycol, a.p.dk, a.p.dv,
+                        g, n, [&](float *at, int rt, int r) { *at = S[rt][r]; });
+}
+
+template <typename T, int DKP, bool DELTA, bool VEC>
+void launch_rule(const ChunkArgs &a, hipStream_t s)
+{
+    const int64_t items = static_cast<int64_t>(a.slots) * a.p.Hv;
+    if constexpr (DELTA) prompt_solve_kernel<T, DKP, VEC><<<dim3(static_cast<unsigned>(items)), 256, 0, s>>>(a);
+    else prompt_gates_kernel<<<dim3(static_cast<unsigned>((items + 3) / 4)), 256, 0, s>>>(a);
+    const dim3 grid(static_cast<unsigned>(a.p.n_seq) * a.p.Hv);
+    if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC><<<grid, 512, 0, s>>>(a);
+    else prompt_chunks_kernel<T, DKP, 4, DELTA, VEC><<<grid, 256, 0, s>>>(a);
+}
+
+template <typename T, int DKP>
+void launch(const ChunkArgs &a, bool delta, bool vec, hipStream_t s)
+{
+    if (delta) {
+        if (vec) launch_rule<T, DKP, true, true>(a, s);
+        else launch_rule<T, DKP, true, false>(a, s);
+    } else {
+        if (vec) launch_rule<T, DKP, false, true>(a, s);
+        else launch_rule<T, DKP, false, false>(a, s);
+    }
+}
+
+// Sequence s has its chunks from slot cu[s] / 64 + s on: enough for any lengths
+// that add up to n_tokens, and known without reading cu_seqlens on the host.
+int64_t slots(const stepq_prompt_desc *d) { return d->n_tokens / kC + d->n_seq; }
 
 stepq_status check(const stepq_prompt_desc *d)
 {
@@ -98,7 +937,17 @@ stepq_status check(const stepq_prompt_desc *d)
     if ((d->q_stride && d->q_stride < qk) || (d->k_stride && d->k_stride < qk) || (d->v_stride && d->v_stride < vo) ||
         (d->o_stride && d->o_stride < vo))
         return bad("a token stride is smaller than a token");
+    // the kernels' offsets within a wave's rows are 32-bit
+    if (std::max({d->q_stride, d->k_stride, d->v_stride, d->o_stride, qk, vo}) > (int64_t(1) << 26))
+        return set_error(STEPQ_E_UNSUPPORTED, "tokens more than 2^26 elements apart");
+    if (slots(d) * d->n_v_heads >= (int64_t(1) << 31))
+        return set_error(STEPQ_E_UNSUPPORTED, "2^31 (chunk, head) pairs or more in one call: split the batch");
     return STEPQ_OK;
+}
+
+size_t record_bytes(const stepq_prompt_desc *d)
+{
+    return sizeof(ChunkGates) + (d->rule == STEPQ_RULE_DELTA ? kTBytes : 0);
 }
 
 }  // namespace
@@ -110,7 +959,7 @@ extern "C" stepq_status stepq_prompt_workspace(const stepq_prompt_desc *d, size_
 {
     if (const stepq_status st = check(d)) return st;
     if (!bytes) return bad("bytes is NULL");
-    *bytes = 0;
+    *bytes = static_cast<size_t>(slots(d)) * d->n_v_heads * record_bytes(d);
     return STEPQ_OK;
 }
 
@@ -126,20 +975,30 @@ extern "C" stepq_status stepq_prompt(const stepq_prompt_desc *d, const int32_t *
     if (!state_in && in_ids) return bad("in_ids without state_in");
     if (state_in && !in_ids && d->n_states_in < d->n_seq) return bad("fewer states in state_in than sequences");
     if (state_in == state_out && in_ids) return bad("state_out must not be state_in where in_ids chooses the states");
+    size_t need = 0;
+    stepq_prompt_workspace(d, &need);
+    if (!workspace || workspace_bytes < need) return bad("workspace is smaller than stepq_prompt_workspace()");
+    if (!aligned(workspace, 256) || !aligned(state_out, 4)) return bad("workspace must be 256-byte aligned");
     const int64_t qk = int64_t(d->n_qk_heads) * d->d_k, vo = int64_t(d->n_v_heads) * d->d_v;
     const int32_t gf = d->gate_dtype == STEPQ_F32;
-    PromptArgs a{cu_seqlens, q, k, v, {alpha, gf}, {beta, gf}, o, state_in, in_ids, state_out,
-                 d->q_stride ? d->q_stride : qk, d->k_stride ? d->k_stride : qk, d->v_stride ? d->v_stride : vo,
-                 d->o_stride ? d->o_stride : vo, static_cast<int32_t>(d->n_tokens), d->n_seq, d->n_v_heads,
-                 d->n_qk_heads, d->d_k, d->d_v, d->n_states_in};
+    ChunkArgs a{};
+    a.p = PromptArgs{cu_seqlens, q, k, v, {alpha, gf}, {beta, gf}, o, state_in, in_ids, state_out,
+                     d->q_stride ? d->q_stride : qk, d->k_stride ? d->k_stride : qk, d->v_stride ? d->v_stride : vo,
+                     d->o_stride ? d->o_stride : vo, static_cast<int32_t>(d->n_tokens), d->n_seq, d->n_v_heads,
+                     d->n_qk_heads, d->d_k, d->d_v, d->n_states_in};
+    a.ws = static_cast<uint8_t *>(workspace);
+    a.record = record_bytes(d);
+    a.slots = static_cast<int32_t>(slots(d));
+    const int e = d->act_dtype == STEPQ_BF16 ? 8 : 4;   // elements in 16 bytes
+    const bool vec = d->d_k % 8 == 0 && (a.p.sq | a.p.sk | a.p.sv) % e == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool delta = d->rule == STEPQ_RULE_DELTA;
     if (d->act_dtype == STEPQ_BF16) {
-        if (d->d_k > 64) launch<bf16_t, 128>(a, delta, s);
-        else launch<bf16_t, 64>(a, delta, s);
+        if (d->d_k > 64) launch<bf16_t, 128>(a, delta, vec, s);
+        else launch<bf16_t, 64>(a, delta, vec, s);
     } else {
-        if (d->d_k > 64) launch<float, 128>(a, delta, s);
-        else launch<float, 64>(a, delta, s);
+        if (d->d_k > 64) launch<float, 128>(a, delta, vec, s);
+        else launch<float, 64>(a, delta, vec, s);
     }
     return launched("prompt launch");
 }
