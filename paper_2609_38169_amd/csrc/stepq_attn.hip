@@ -1,19 +1,29 @@
 // Attention of single tokens over a shared prefix and each request's own pages.
+#include <algorithm>
 #include <cmath>
+#include <type_traits>
 
+#include "stepq_mma.h"
 #include "stepq_plan.h"
-#include "stepq_seq.h"
 
 namespace stepq {
 namespace {
+
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using f32x16 = __attribute__((ext_vector_type(16))) float;
 
 struct AttnArgs {
     const void *q, *k, *v;
     const int32_t *prefix_pages, *table, *lengths;
     void *o;
     float *lse;
+    float2 *ml;              // [parts][batch * Hq]: a part's maximum (in powers of two) and sum
+    float *acc;              // [parts][batch * Hq][D]: its unnormalised output
     int64_t prefix;
-    int32_t batch, Hq, Hkv, n_pages, page, max_pages;
+    int32_t batch, Hq, Hkv, G, n_pages, page, max_pages;
+    int32_t prefix_parts, own_parts;   // parts 0 .. prefix_parts - 1 of the prefix, then the requests' own
+    int32_t prefix_items;    // workgroups of attn_rows_kernel that read the prefix (0: attn_prefix_kernel does)
     FastDiv div_page;
     float scale;             // times log2 e: scores are kept in powers of two
 };
@@ -26,58 +36,440 @@ __device__ __forceinline__ int fdiv(int n, FastDiv d)
 
 constexpr float kLn2 = 0.6931471805599453f;
 
-// One workgroup per (request, query head), a wave per key: the lanes hold the
-// query, the key's product is summed over the wave, the running maximum and
-// sum rescale the accumulator.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs a)
+// Row of the caches ([n_pages * Hkv * page][D]) of token t of `pages`; -1: none.
+__device__ __forceinline__ int token_row(const AttnArgs &a, const int32_t *pages, int t, int hk, bool valid)
 {
-    constexpr int E = D / 64;
-    __shared__ float sm[4], sl[4], sacc[4][D];
-    const int b = blockIdx.x / a.Hq, h = blockIdx.x - b * a.Hq, hk = h / (a.Hq / a.Hkv);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const size_t row = (static_cast<size_t>(b) * a.Hq + h) * D;
-    float q[E], acc[E] = {}, m = -INFINITY, l = 0.0f;
+    if (!valid) return -1;
+    const int p = fdiv(t, a.div_page), id = pages[p];
+    return id >= 0 && id < a.n_pages ? (id * a.Hkv + hk) * a.page + (t - p * a.page) : -1;
+}
+
+__device__ __forceinline__ float swap_max16(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float swap_max32(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float swap_add16(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ float swap_add32(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// A running softmax: maximum and sum of what was seen; next() returns the
+// factor on everything so far when scores of maximum m join.
+struct Running {
+    float m = -INFINITY, l = 0.0f, base = 0.0f;
+    __device__ __forceinline__ float next(float top)
+    {
+        const float to = fmaxf(m, top), b = to == -INFINITY ? 0.0f : to, f = __builtin_amdgcn_exp2f(m - b);
+        m = to, base = b, l *= f;
+        return f;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// Few queries per key: a workgroup takes 16 query rows (the group's heads of
+// one request over a range of its own tokens, or 16 rows of all requests over a
+// range of the prefix) and its waves take key tiles in turn.  Scores are formed
+// transposed, keys x queries, so that a query's weights lie in one lane group
+// and go into the second product as they are; values pass through LDS of the
+// wave's own to be read by columns.  Bound by the bytes of the caches.
+template <typename T>
+struct Tile;
+template <>
+struct Tile<bf16_t> {
+    static constexpr int keys = 32;
+};
+template <>
+struct Tile<float> {
+    static constexpr int keys = 16;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnArgs a)
+{
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int KT = Tile<T>::keys, RB = D * static_cast<int>(sizeof(T)), SL = RB / 16;   // bytes and 16-byte slots of a row
+    constexpr int RT = KT / 16;                       // row blocks of keys
+    constexpr int QF = RB / 64;                       // 16-byte pieces of a row per lane group: operand reads
+    constexpr int VL = KT * SL / 64;                  // 16-byte loads of values per lane
+    constexpr int SW = SL < 16 ? 128 : 256;
+    __shared__ alignas(16) uint8_t vs[4][KT * RB];
+    __shared__ float sm[4][16], sl[4][16];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+    int x = blockIdx.x, part, hk, row0, rows, from, to;
+    const int32_t *pages;
+    if (x < a.prefix_items) {
+        const int blocks = (a.batch * a.G + 15) / 16;
+        hk = x % a.Hkv, x /= a.Hkv;
+        row0 = x % blocks * 16, part = x / blocks;
+        rows = a.batch * a.G;
+        pages = a.prefix_pages;
+        const int len = static_cast<int>(a.prefix), step = ((len + a.prefix_parts - 1) / a.prefix_parts + KT - 1) / KT * KT;
+        from = min(len, part * step), to = min(len, from + step);
+    } else {
+        x -= a.prefix_items;
+        const int blocks = (a.G + 15) / 16;
+        part = x % a.own_parts, x /= a.own_parts;
+        row0 = x % blocks * 16, x /= blocks;
+        hk = x % a.Hkv;
+        const int b = x / a.Hkv;
+        rows = a.G;
+        pages = a.table + static_cast<size_t>(b) * a.max_pages;
+        const int len = min(max(a.lengths[b], 0), a.max_pages * a.page);
+        const int step = ((len + a.own_parts - 1) / a.own_parts + KT - 1) / KT * KT;
+        from = min(len, part * step), to = min(len, from + step);
+        row0 += b * a.G;
+        rows += b * a.G;
+        part += a.prefix_parts;
+    }
+    // row r of (all requests, group) is request r / G, head r % G of the group
+    const bool live = row0 + n < rows;
+    const int rr = live ? row0 + n : row0, rb = rr / a.G;
+    const size_t qrow = static_cast<size_t>(rb) * a.Hq + hk * a.G + (rr - rb * a.G);
+    using Piece = std::conditional_t<BF, bf16x8, f32x4>;
+    Piece q[QF];
 #pragma unroll
-    for (int e = 0; e < E; ++e) q[e] = widen(static_cast<const T *>(a.q)[row + e * 64 + lane]) * a.scale;
-    const int mine = static_cast<int>(min(static_cast<int64_t>(max(a.lengths[b], 0)), static_cast<int64_t>(a.max_pages) * a.page));
-    for (int part = 0; part < 2; ++part) {
-        const int n = part ? mine : static_cast<int>(a.prefix);
-        const int32_t *pages = part ? a.table + static_cast<size_t>(b) * a.max_pages : a.prefix_pages;
-        for (int t = wave; t < n; t += 4) {
-            const int p = fdiv(t, a.div_page), id = pages[p];
-            if (id < 0 || id >= a.n_pages) continue;
-            const size_t at = ((static_cast<size_t>(id) * a.Hkv + hk) * a.page + (t - p * a.page)) * D;
-            float s = 0.0f;
+    for (int i = 0; i < QF; ++i)
+        q[i] = reinterpret_cast<const Piece *>(static_cast<const T *>(a.q) + qrow * D)[4 * i + g];
+
+    const uint8_t *K = static_cast<const uint8_t *>(a.k), *V = static_cast<const uint8_t *>(a.v);
+    Running run;
+    f32x4 acc[D / 16] = {};
+    Piece kx[RT][QF];
+    int at = -1;                 // lane l < KT: the cache row of key l of the tile whose keys are in kx
+    const auto rows_of = [&](int t0) { return token_row(a, pages, t0 + lane, hk, lane < KT && t0 + lane < to); };
+    const auto fetch_keys = [&] {
 #pragma unroll
-            for (int e = 0; e < E; ++e) s = fmaf(q[e], widen(static_cast<const T *>(a.k)[at + e * 64 + lane]), s);
+        for (int rt = 0; rt < RT; ++rt) {
+            const int r = max(__shfl(at, 16 * rt + n), 0);
 #pragma unroll
-            for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
-            const float top = fmaxf(m, s), base = top == -INFINITY ? 0.0f : top;
-            const float f = exp2f(m - base), w = exp2f(s - base);
-            l = fmaf(l, f, w);
+            for (int i = 0; i < QF; ++i)
+                kx[rt][i] = reinterpret_cast<const Piece *>(K + static_cast<size_t>(r) * RB)[4 * i + g];
+        }
+    };
+    int t0 = from + wave * KT;
+    int next_at = t0 < to ? rows_of(t0) : -1;
+    if (t0 < to) at = next_at, fetch_keys();
+    for (; t0 < to; t0 += 4 * KT) {
+        // the tile's values, and the rows of the next tile
+        u32x4 vx[VL];
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                acc[e] = fmaf(w, widen(static_cast<const T *>(a.v)[at + e * 64 + lane]), acc[e] * f);
-            m = top;
+        for (int i = 0; i < VL; ++i) {
+            const int piece = i * 64 + lane, row = piece / SL, r = __shfl(at, row);
+            const u32x4 y = *reinterpret_cast<const u32x4 *>(V + static_cast<size_t>(max(r, 0)) * RB + piece % SL * 16);
+            vx[i] = r >= 0 ? y : u32x4{};
+        }
+        const bool more = t0 + 4 * KT < to;
+        if (more) next_at = rows_of(t0 + 4 * KT);
+        // scores: lane (g, n) holds keys 16 rt + 4 g .. + 3 of query n
+        f32x4 s[RT];
+        float top = -INFINITY;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            s[rt] = f32x4{};
+#pragma unroll
+            for (int i = 0; i < QF; ++i) {
+                if constexpr (BF) {
+                    s[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kx[rt][i], q[i], s[rt], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        s[rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[rt][i][r], q[i][r], s[rt], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool none = __shfl(at, 16 * rt + 4 * g + r) < 0;
+                s[rt][r] = none ? -INFINITY : s[rt][r] * a.scale;
+                top = fmaxf(top, s[rt][r]);
+            }
+        }
+        if (more) at = next_at, fetch_keys();
+        const float f = run.next(swap_max32(swap_max16(top)));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[rt][r] = __builtin_amdgcn_exp2f(s[rt][r] - run.base);
+                run.l += s[rt][r];
+            }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int piece = i * 64 + lane, row = piece / SL, slot = piece % SL;
+            *reinterpret_cast<u32x4 *>(&vs[wave][row * RB + ((slot ^ (BF ? swizzle<SW>(row) : row & 3)) * 16)]) = vx[i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        if constexpr (BF) {
+            // the weights in two bfloat16 planes (16 bits): their rounding is then far below the output's
+            bf16x8 p[2];
+            {
+                float y[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[RT - 1][0], s[RT - 1][1], s[RT - 1][2], s[RT - 1][3]};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[0][i] = static_cast<__bf16>(y[i]);
+                    p[1][i] = static_cast<__bf16>(y[i] - static_cast<float>(p[0][i]));
+                }
+            }
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) {
+                u32x4 w;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = 16 * h + 4 * g + (n >> 2), slot = 2 * dt + ((n & 3) >> 1);
+                    const u32x2 y = read_columns(&vs[wave][row * RB + ((slot ^ swizzle<SW>(row)) * 16) + 8 * (n & 1)]);
+                    w[2 * h] = y[0], w[2 * h + 1] = y[1];
+                }
+                const bf16x8 v = __builtin_bit_cast(bf16x8, w);
+                acc[dt] *= f;
+#pragma unroll
+                for (int i = 1; i >= 0; --i) acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i], acc[dt], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) {
+                acc[dt] *= f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 4 * g + r, slot = 4 * dt + (n >> 2);
+                    const float v = *reinterpret_cast<const float *>(&vs[wave][row * RB + ((slot ^ (row & 3)) * 16) + (n & 3) * 4]);
+                    acc[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[0][r], acc[dt], 0, 0, 0);
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+    // the four waves' parts: lane (g, n) holds dimensions 16 dt + 4 g .. + 3 of query n
+    run.l = swap_add32(swap_add16(run.l));
+    if (g == 0) sm[wave][n] = run.m, sl[wave][n] = run.l;
+    __syncthreads();
+    float top = -INFINITY, z = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w][n]);
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) z += sl[w][n] * __builtin_amdgcn_exp2f(sm[w][n] - base);
+    const float mine = __builtin_amdgcn_exp2f(run.m - base);
+    constexpr int LD = D + 4;
+    static_assert(16 * LD * 4 <= static_cast<int>(sizeof(vs)), "the sum fits the values' place");
+    float *sum = reinterpret_cast<float *>(vs);
+#pragma unroll 1
+    for (int w = 0; w < 4; ++w) {
+        if (wave == w)
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) {
+                f32x4 *to4 = reinterpret_cast<f32x4 *>(sum + n * LD + 16 * dt + 4 * g);
+                const f32x4 y = acc[dt] * mine;
+                *to4 = w == 0 ? y : *to4 + y;
+            }
+        __syncthreads();
+    }
+    const size_t total = static_cast<size_t>(a.batch) * a.Hq;
+    for (int e = threadIdx.x; e < 16 * (D / 4); e += 256) {
+        const int r = e / (D / 4), c = e % (D / 4);
+        if (row0 + r < rows) {
+            const int b = (row0 + r) / a.G;
+            const size_t at_row = part * total + static_cast<size_t>(b) * a.Hq + hk * a.G + (row0 + r - b * a.G);
+            reinterpret_cast<f32x4 *>(a.acc + at_row * D)[c] = *reinterpret_cast<const f32x4 *>(sum + r * LD + 4 * c);
         }
     }
-    if (lane == 0) sm[wave] = m, sl[wave] = l;
+    if (wave == 0 && g == 0 && live) a.ml[part * total + qrow] = make_float2(top, z);
+}
+
+// ---------------------------------------------------------------------------
+// Many queries per key: the prefix of a large batch, a matrix product.  A
+// workgroup takes 256 query rows (32 to a wave, their queries in registers) and
+// a range of the prefix, 64 (D = 256: 32) keys at a time in LDS; the next ones are
+// on their way in registers meanwhile.  Scores transposed as above, in 32x32 blocks.  The
+// running maximum follows only when it is passed by 2^6, so that the outputs
+// are rescaled a few times in all.  The weights are rounded to bfloat16 once,
+// as the output is; their sum is taken before.
+template <int D>
+__global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
+{
+    constexpr int KT = D == 256 ? 32 : 64;            // as many as the registers of 2 waves per SIMD allow
+    constexpr int KK = KT / 32, RB = 2 * D, SL = RB / 16, L = KT * SL / 512, KB = D / 16, DT = D / 32;
+    constexpr int SW = SL < 16 ? 128 : 256;
+    __shared__ alignas(16) uint8_t ks[KT * RB], vs[KT * RB];
+    __shared__ uint64_t invalid_s;
+    int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int lane = tid & 63, h = lane >> 5, n = lane & 31;
+    // Addresses in LDS are formed again for each use, not kept in registers.
+    const auto again = [&] {
+        asm volatile("" : "+v"(lane), "+v"(tid));
+        h = lane >> 5, n = lane & 31;
+    };
+    const int rows = a.batch * a.G, tiles = (rows + 255) / 256, pieces = a.Hkv * a.prefix_parts;
+    // pieces of the prefix stay on one XCD, whose cache then serves all query tiles that read them
+    int piece, tile;
+    if (pieces % 8 == 0) piece = blockIdx.x % 8 + 8 * (blockIdx.x / 8 / tiles), tile = blockIdx.x / 8 % tiles;
+    else piece = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+    const int hk = piece % a.Hkv, part = piece / a.Hkv;
+    const int len = static_cast<int>(a.prefix), step = ((len + a.prefix_parts - 1) / a.prefix_parts + KT - 1) / KT * KT;
+    const int from = min(len, part * step), to = min(len, from + step);
+    const int row = tile * 256 + wave * 32 + n, rr = min(row, rows - 1), b = rr / a.G;
+    const size_t qrow = static_cast<size_t>(b) * a.Hq + hk * a.G + (rr - b * a.G);
+    // operand B: query n, elements 16 kb + 8 h .. + 7
+    bf16x8 q[KB];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sacc[wave][e * 64 + lane] = acc[e];
-    __syncthreads();
-    float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float z = 0.0f, f[4];
+    for (int kb = 0; kb < KB; ++kb)
+        q[kb] = reinterpret_cast<const bf16x8 *>(static_cast<const bf16_t *>(a.q) + qrow * D)[2 * kb + h];
+    const uint8_t *K = static_cast<const uint8_t *>(a.k), *V = static_cast<const uint8_t *>(a.v);
+    u32x4 kx[L], vx[L];
+    const auto fetch = [&](int t0) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) f[w] = exp2f(sm[w] - base), z += sl[w] * f[w];
-    for (int e = threadIdx.x; e < D; e += 256) {
-        float y = 0.0f;
+        for (int i = 0; i < L; ++i) {
+            const int piece_i = i * 512 + tid, t = t0 + piece_i / SL;
+            const int r = token_row(a, a.prefix_pages, t, hk, t < to);
+            const size_t at = static_cast<size_t>(max(r, 0)) * RB + piece_i % SL * 16;
+            kx[i] = *reinterpret_cast<const u32x4 *>(K + at);
+            const u32x4 y = *reinterpret_cast<const u32x4 *>(V + at);
+            vx[i] = r >= 0 ? y : u32x4{};
+        }
+    };
+    f32x16 acc[DT] = {};
+    float m = -INFINITY, base = 0.0f, l = 0.0f;
+    if (from < to) fetch(from);
+    for (int t0 = from; t0 < to; t0 += KT) {
+        __syncthreads();
+        again();
 #pragma unroll
-        for (int w = 0; w < 4; ++w) y = fmaf(f[w], sacc[w][e], y);
-        static_cast<T *>(a.o)[row + e] = narrow<T>(z == 0.0f ? 0.0f : y / z);
+        for (int i = 0; i < L; ++i) {
+            const int piece_i = i * 512 + tid, kr = piece_i / SL, at = kr * RB + ((piece_i % SL ^ swizzle<SW>(kr)) * 16);
+            *reinterpret_cast<u32x4 *>(ks + at) = kx[i];
+            *reinterpret_cast<u32x4 *>(vs + at) = vx[i];
+        }
+        if (wave == 0) {
+            const uint64_t none = __ballot(token_row(a, a.prefix_pages, t0 + lane, hk, t0 + lane < to && lane < KT) < 0 && lane < KT);
+            if (lane == 0) invalid_s = none;
+        }
+        __syncthreads();
+        if (t0 + KT < to) fetch(t0 + KT);
+        again();
+        // scores: lane (h, n) holds keys 32 kt + 8 (r / 4) + 4 h + r % 4 of query n
+        f32x16 s[KK];
+#pragma unroll
+        for (int kt = 0; kt < KK; ++kt) {
+            s[kt] = f32x16{};
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const int kr = 32 * kt + n;
+                const bf16x8 k = *reinterpret_cast<const bf16x8 *>(ks + kr * RB + (((2 * kb + h) ^ swizzle<SW>(kr)) * 16));
+                s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kb], s[kt], 0, 0, 0);
+            }
+        }
+        float top = -INFINITY;
+        const uint64_t none = invalid_s;
+#pragma unroll
+        for (int kt = 0; kt < KK; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kt][r] *= a.scale;
+        if (none) {
+#pragma unroll
+            for (int kt = 0; kt < KK; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (none >> (32 * kt + 8 * (r / 4) + 4 * h + r % 4) & 1) s[kt][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int kt = 0; kt < KK; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kt][r]);
+        top = swap_max32(top);
+        if (__any(!(top <= base + 6.0f)) || m == -INFINITY) {
+            const float to_m = fmaxf(m, top), nb = to_m == -INFINITY ? 0.0f : to_m, f = __builtin_amdgcn_exp2f(m == -INFINITY ? m : base - nb);
+            l *= f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) acc[dt] *= f;
+            base = nb;
+        }
+        m = fmaxf(m, top);
+        bf16x8 p[2 * KK];
+#pragma unroll
+        for (int kt = 0; kt < KK; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const f32x2 e = {__builtin_amdgcn_exp2f(s[kt][r] - base), __builtin_amdgcn_exp2f(s[kt][r + 1] - base)};
+                l += e[0] + e[1];
+                const bf16x2 w = __builtin_convertvector(e, bf16x2);
+                p[2 * kt + r / 8][r % 8] = w[0], p[2 * kt + r / 8][r % 8 + 1] = w[1];
+            }
+        again();
+        // O^T += V^T P: summation slot 8 h + 4 u + j of a block of 16 keys is key 8 u + 4 h + j
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int kb = 0; kb < 2 * KK; ++kb) {
+                u32x4 w;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int ln = lane & 15, kr = 16 * kb + 8 * u + 4 * h + (ln >> 2);
+                    const int slot = 4 * dt + 2 * ((lane >> 4) & 1) + ((ln & 3) >> 1);
+                    const u32x2 y = read_columns(vs + kr * RB + ((slot ^ swizzle<SW>(kr)) * 16) + 8 * (ln & 1));
+                    w[2 * u] = y[0], w[2 * u + 1] = y[1];
+                }
+                acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p[kb], acc[dt], 0, 0, 0);
+            }
     }
-    if (threadIdx.x == 0 && a.lse) a.lse[row / D] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
+    l = swap_add32(l);
+    if (row < rows) {
+        const size_t at = part * (static_cast<size_t>(a.batch) * a.Hq) + qrow;
+        if (h == 0) a.ml[at] = make_float2(m == -INFINITY ? m : base, l);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<f32x4 *>(a.acc + at * D + 32 * dt + 2 * r + 4 * h) =
+                    f32x4{acc[dt][r], acc[dt][r + 1], acc[dt][r + 2], acc[dt][r + 3]};
+    }
+}
+
+// The parts of each row joined: a wave per row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+{
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    const size_t total = static_cast<size_t>(a.batch) * a.Hq, row = static_cast<size_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= total) return;
+    const int parts = a.prefix_parts + a.own_parts;
+    float top = -INFINITY;
+    for (int i = lane; i < parts; i += 64) top = fmaxf(top, a.ml[i * total + row].x);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float base = top == -INFINITY ? 0.0f : top;
+    float y[E] = {}, z = 0.0f;
+    for (int i = 0; i < parts; ++i) {
+        const float2 ml = a.ml[i * total + row];
+        const float f = __builtin_amdgcn_exp2f(ml.x - base);
+        z = fmaf(ml.y, f, z);
+        const float *at = a.acc + (i * total + row) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = fmaf(f, at[e], y[e]);
+    }
+    T *o = static_cast<T *>(a.o) + row * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = narrow<T>(z == 0.0f ? 0.0f : y[e] / z);
+    if (lane == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
 }
 
 stepq_status check(const stepq_attn_desc *d)
@@ -95,16 +487,65 @@ stepq_status check(const stepq_attn_desc *d)
         return set_error(STEPQ_E_UNSUPPORTED, "2^30 tokens or more in the prefix or a request's pages");
     if (static_cast<int64_t>(d->batch) * d->n_q_heads > (int64_t(1) << 24))
         return set_error(STEPQ_E_UNSUPPORTED, "more than 2^24 (request, head) rows in one call: split the batch");
+    if (static_cast<double>(d->n_pages) * d->n_kv_heads * d->page_size >= 2147483648.0)
+        return set_error(STEPQ_E_UNSUPPORTED, "2^31 rows or more in a cache");
     return STEPQ_OK;
 }
 
-template <typename T>
-void launch(const AttnArgs &a, int D, hipStream_t s)
+// How the keys are split over workgroups.
+struct Split {
+    int prefix_parts, own_parts, prefix_items;
+    bool product;            // the prefix by attn_prefix_kernel
+};
+
+Split split_of(const stepq_attn_desc *d)
 {
-    const dim3 grid(static_cast<unsigned>(a.batch) * a.Hq);
-    if (D == 64) attn_rows_kernel<T, 64><<<grid, 256, 0, s>>>(a);
-    else if (D == 128) attn_rows_kernel<T, 128><<<grid, 256, 0, s>>>(a);
-    else attn_rows_kernel<T, 256><<<grid, 256, 0, s>>>(a);
+    Split s{};
+    const int64_t G = d->n_q_heads / d->n_kv_heads, rows = d->batch * G;
+    const auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    // enough workgroups for the chip's 256 CUs, ranges of at least 256 keys
+    if (d->prefix_len) {
+        // beyond 64 rows a head, rereading the prefix for every 16 rows costs more than a 256-row tile leaves idle
+        s.product = d->act_dtype == STEPQ_BF16 && rows > 64;
+        const int64_t blocks = d->n_kv_heads * ceil_div(rows, s.product ? 256 : 16), most = ceil_div(d->prefix_len, 256);
+        int64_t parts = std::clamp<int64_t>(ceil_div(s.product ? 256 : 512, blocks), 1, most);
+        // whole rounds of the 8 XCDs where that costs few parts
+        if (s.product)
+            while (parts < most && d->n_kv_heads * parts % 8 != 0 && parts < 2 * ceil_div(256, blocks)) ++parts;
+        s.prefix_parts = static_cast<int>(parts);
+        if (!s.product) s.prefix_items = static_cast<int>(blocks * parts);
+    }
+    const int64_t blocks = d->batch * static_cast<int64_t>(d->n_kv_heads) * ceil_div(G, 16);
+    const int64_t most = std::max<int64_t>(1, ceil_div(static_cast<int64_t>(d->max_pages) * d->page_size, 256));
+    s.own_parts = static_cast<int>(std::clamp<int64_t>(ceil_div(512, blocks), 1, most));
+    return s;
+}
+
+size_t part_bytes(const stepq_attn_desc *d)
+{
+    return static_cast<size_t>(d->batch) * d->n_q_heads * (d->head_dim * sizeof(float) + sizeof(float2));
+}
+
+template <typename T, int D>
+void launch(AttnArgs a, const Split &s, hipStream_t st)
+{
+    const int blocks = (a.G + 15) / 16;
+    const int64_t own = static_cast<int64_t>(a.batch) * a.Hkv * blocks * a.own_parts;
+    if constexpr (sizeof(T) == 2)
+        if (s.product) {
+            const int64_t grid = static_cast<int64_t>((a.batch * a.G + 255) / 256) * a.Hkv * a.prefix_parts;
+            attn_prefix_kernel<D><<<dim3(static_cast<unsigned>(grid)), 512, 0, st>>>(a);
+        }
+    attn_rows_kernel<T, D><<<dim3(static_cast<unsigned>(a.prefix_items + own)), 256, 0, st>>>(a);
+    attn_join_kernel<T, D><<<dim3(static_cast<unsigned>((static_cast<int64_t>(a.batch) * a.Hq + 3) / 4)), 256, 0, st>>>(a);
+}
+
+template <typename T>
+void launch(const AttnArgs &a, const Split &s, int D, hipStream_t st)
+{
+    if (D == 64) launch<T, 64>(a, s, st);
+    else if (D == 128) launch<T, 128>(a, s, st);
+    else launch<T, 256>(a, s, st);
 }
 
 }  // namespace
@@ -116,7 +557,8 @@ extern "C" stepq_status stepq_prefix_attention_workspace(const stepq_attn_desc *
 {
     if (const stepq_status st = check(d)) return st;
     if (!bytes) return bad("bytes is NULL");
-    *bytes = 0;
+    const Split s = split_of(d);
+    *bytes = d->batch ? part_bytes(d) * (s.prefix_parts + s.own_parts) : 0;
     return STEPQ_OK;
 }
 
@@ -131,11 +573,27 @@ extern "C" stepq_status stepq_prefix_attention(const stepq_attn_desc *d, const v
     if (d->n_pages && (!k_cache || !v_cache)) return bad("NULL cache");
     if (d->prefix_len && !prefix_pages) return bad("prefix_pages is NULL");
     if (d->max_pages && !page_table) return bad("page_table is NULL");
-    AttnArgs a{q, k_cache, v_cache, prefix_pages, page_table, lengths, o, lse, d->prefix_len, d->batch, d->n_q_heads,
-               d->n_kv_heads, d->n_pages, d->page_size, d->max_pages, fast_div(static_cast<uint32_t>(d->page_size)),
-               d->scale * 1.4426950408889634f};
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
+        return bad("q and the caches must be 16-byte aligned");
+    const Split sp = split_of(d);
+    const size_t need = part_bytes(d) * (sp.prefix_parts + sp.own_parts);
+    if (!workspace || workspace_bytes < need) return bad("workspace is smaller than stepq_prefix_attention_workspace()");
+    if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
+    const size_t rows = static_cast<size_t>(d->batch) * d->n_q_heads;
+    AttnArgs a{};
+    a.q = q, a.k = k_cache, a.v = v_cache;
+    a.prefix_pages = prefix_pages, a.table = page_table, a.lengths = lengths;
+    a.o = o, a.lse = lse;
+    a.acc = static_cast<float *>(workspace);
+    a.ml = reinterpret_cast<float2 *>(a.acc + rows * d->head_dim * (sp.prefix_parts + sp.own_parts));
+    a.prefix = d->prefix_len;
+    a.batch = d->batch, a.Hq = d->n_q_heads, a.Hkv = d->n_kv_heads, a.G = d->n_q_heads / d->n_kv_heads;
+    a.n_pages = d->n_pages, a.page = d->page_size, a.max_pages = d->max_pages;
+    a.prefix_parts = sp.prefix_parts, a.own_parts = sp.own_parts, a.prefix_items = sp.prefix_items;
+    a.div_page = fast_div(static_cast<uint32_t>(d->page_size));
+    a.scale = d->scale * 1.4426950408889634f;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (d->act_dtype == STEPQ_BF16) launch<bf16_t>(a, d->head_dim, s);
-    else launch<float>(a, d->head_dim, s);
+    if (d->act_dtype == STEPQ_BF16) launch<bf16_t>(a, sp, d->head_dim, s);
+    else launch<float>(a, sp, d->head_dim, s);
     return launched("prefix attention launch");
 }
