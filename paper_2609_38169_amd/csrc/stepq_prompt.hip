@@ -47,12 +47,17 @@ struct ChunkGates {
 };
 static_assert(sizeof(ChunkGates) == 1408, "record size");
 constexpr size_t kTBytes = 2 * 6 * 1024;
+constexpr int kGateWords = 5 * kC;       // lg, g, w, b
 
 struct ChunkArgs {
     PromptArgs p;
     uint8_t *ws;
     size_t record;           // bytes per (chunk, head)
     int32_t slots;           // chunk slots: sequence s owns those from cu[s] / 64 + s on
+    int32_t seg;             // chunks per segment; 0: sequences are not cut
+    int32_t seg_slots;       // segment slots, numbered as the chunks' are, with 64 seg tokens each
+    float *segs;             // per (segment, head): SegmentHead, B or the state after it [dk][dv], A [DKP][DKP] (Delta)
+    size_t seg_floats;
 };
 
 __device__ __forceinline__ int2 seq_bounds(const PromptArgs &a, int s)
@@ -61,19 +66,20 @@ __device__ __forceinline__ int2 seq_bounds(const PromptArgs &a, int s)
     return make_int2(from, min(max(a.cu[s + 1], from), a.T));
 }
 
-__device__ __forceinline__ int first_slot(const PromptArgs &a, int s)
+// First slot of sequence s where a slot holds `unit` tokens.
+__device__ __forceinline__ int first_slot(const PromptArgs &a, int s, int unit = kC)
 {
-    return min(max(a.cu[s], 0), a.T) / kC + s;
+    return min(max(a.cu[s], 0), a.T) / unit + s;
 }
 
 // The sequence that owns a chunk slot: the last one whose first slot is at most
 // x, found by the wave's 64 lanes at a time.
-__device__ __forceinline__ int owner(const PromptArgs &a, int x, int lane)
+__device__ __forceinline__ int owner(const PromptArgs &a, int x, int lane, int unit = kC)
 {
     int lo = 0, n = a.n_seq;            // the answer lies in [lo, lo + n)
     while (n > 1) {
         const int step = (n + 63) / 64, at = lo + lane * step;
-        const bool le = at < lo + n && first_slot(a, at) <= x;
+        const bool le = at < lo + n && first_slot(a, at, unit) <= x;
         const uint64_t yes = __ballot(le);
         const int k = yes ? 63 - __clzll(yes) : 0;
         const int end = lo + n;
@@ -565,6 +571,13 @@ __device__ __forceinline__ void each_state_row(P *base, int dk, int dv, int g, i
         }
 }
 
+// The state sequence s starts from; NULL: zeros.
+__device__ __forceinline__ const float *initial_state(const PromptArgs &a, int s, int h)
+{
+    const int src = a.state_in ? (a.in_ids ? a.in_ids[s] : s) : -1;
+    return src >= 0 && src < a.n_in ? a.state_in + (static_cast<size_t>(src) * a.Hv + h) * a.dk * a.dv : nullptr;
+}
+
 __device__ __forceinline__ uint32_t tile_max(const f32x4 (&x)[4])
 {
     float m = 0.0f;
@@ -575,21 +588,30 @@ __device__ __forceinline__ uint32_t tile_max(const f32x4 (&x)[4])
     return __float_as_uint(m);
 }
 
+// Long sequences with too few heads to fill the chip are cut into segments of
+// whole chunks.  A segment takes a state S to A S + B (decay rule: A = gamma I),
+// whatever S is, so that: a launch forms B of every segment by walking it from
+// a zero state, and for the Delta rule A by walking it from the identity with
+// all values zero; one applies them in order (prompt_join kernels), leaving the
+// state after each segment in B's place; and then all segments are walked at once.
+constexpr int kSegmentHead = 64;         // floats; [0] = gamma
+
 // Second launch: a workgroup of NW waves walks the chunks of one (sequence, head)
-// for 16 NW value columns, a wave holds 16 columns of the state in registers
+// or of a segment of it (OUT false: for B and A, without outputs) for 16 NW value columns, a wave holds 16 columns of the state in registers
 // (result layout: lane n column n).  Every product with the state, and every
 // one after it, keeps the columns in their lanes, so that the waves share only
 // what is read, and each column of an operand has a power of two of its own.
-template <typename T, int DKP, int NW, bool DELTA, bool VEC>
+template <typename T, int DKP, int NW, bool DELTA, bool VEC, bool OUT>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void prompt_chunks_kernel(ChunkArgs a)
 {
     constexpr int NA = Act<T>::planes, KB = DKP / 32, W = 16 * NW;
     using ShareQ = Share<DKP / 8, 64 * NW>;
     using ShareV = Share<W / 8, 64 * NW>;
     constexpr int UQ = ShareQ::units, UV = ShareV::units;
-    __shared__ RowTile<T, DKP> K, Q;
+    __shared__ RowTile<T, DKP> K;
+    __shared__ std::conditional_t<OUT, RowTile<T, DKP>, char> Q;
     __shared__ ValueTile<T, W> V;
-    __shared__ TriangleTile<2> P;
+    __shared__ std::conditional_t<OUT, TriangleTile<2>, char> P;
     __shared__ std::conditional_t<DELTA, TriangleTile<2>, char> Tt;
     __shared__ struct alignas(16) {
         double lg[kC];
@@ -605,32 +627,45 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     };
     const ShareQ sh(threadIdx.x);
     const ShareV sv(threadIdx.x);
-    const int blocks = a.p.dv / W;
-    const int cb = blockIdx.x % blocks, h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv;
+    const int value_blocks = a.p.dv / W, blocks = value_blocks + (OUT || !DELTA ? 0 : (DKP + W - 1) / W);
+    const int cb = blockIdx.x % blocks, h = blockIdx.x / blocks % a.p.Hv, item = blockIdx.x / blocks / a.p.Hv;
     const int hq = h / (a.p.Hv / a.p.Hqk);
-    const int col0 = cb * W, mycol = wv * 16;
+    const bool values = OUT || !DELTA || cb < value_blocks;      // B; else A
+    const int col0 = (values ? cb : cb - value_blocks) * W, mycol = wv * 16;
+    const int s = a.seg ? owner(a.p, item, lane, kC * a.seg) : item;
     const int2 be = seq_bounds(a.p, s);
-    const int chunks = (be.y - be.x + kC - 1) / kC;
+    const int total = (be.y - be.x + kC - 1) / kC, part = a.seg ? item - first_slot(a.p, s, kC * a.seg) : 0;
+    const int first = part * a.seg, chunks = a.seg ? min(total, first + a.seg) : total;
+    if (part > 0 && first >= total) return;
+    if (!OUT && chunks == total) return;         // nothing follows it
+    float *rec = a.seg ? a.segs + (static_cast<size_t>(item) * a.p.Hv + h) * a.seg_floats : nullptr;
     const uint8_t *records = a.ws + (static_cast<size_t>(first_slot(a.p, s)) * a.p.Hv + h) * a.record;
 
     f32x4 S[DKP / 16];
-    {
-        const int src = a.p.state_in ? (a.p.in_ids ? a.p.in_ids[s] : s) : -1;
 #pragma unroll
-        for (int rt = 0; rt < DKP / 16; ++rt) S[rt] = f32x4{};
-        if (src >= 0 && src < a.p.n_in)
-            each_state_row<DKP>(a.p.state_in + (static_cast<size_t>(src) * a.p.Hv + h) * a.p.dk * a.p.dv + col0 + mycol,
-                                a.p.dk, a.p.dv, g, n, [&](const float *at, int rt, int r) { S[rt][r] = *at; });
+    for (int rt = 0; rt < DKP / 16; ++rt) S[rt] = f32x4{};
+    if constexpr (OUT) {
+        const float *from = part == 0 ? initial_state(a.p, s, h) : rec - a.p.Hv * a.seg_floats + kSegmentHead;
+        if (from)
+            each_state_row<DKP>(from + col0 + mycol, a.p.dk, a.p.dv, g, n,
+                                [&](const float *at, int rt, int r) { S[rt][r] = *at; });
+    } else if (!values) {
+#pragma unroll
+        for (int rt = 0; rt < DKP / 16; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[rt][r] = state_row(rt, 4 * g + r) == col0 + mycol + n ? 1.0f : 0.0f;
     }
+    float gamma = 1.0f;
 
     // What the next chunk needs is on its way while this one is computed, each
     // part in registers for as short as its latency allows: keys and queries
     // from the second barrier on, values and gates from the state's update on;
     // T' from the chunk's own first barrier to its third.
-    Act<T> kx[UQ], qx[UQ], vx[UV];
-    f16x8 tx[8 / NW][2];
-    double lgx = 0.0;
-    float gx = 0.0f, wx = 0.0f, bx = 0.0f;
+    Act<T> kx[UQ], qx[OUT ? UQ : 1], vx[UV] = {};
+    constexpr int NP = (12 + NW - 1) / NW;           // 1 KB pieces of T' per wave
+    f16x8 tx[NP];
+    constexpr int NG = (kGateWords + 64 * NW - 1) / (64 * NW);
+    uint32_t gx[NG];
     const auto record = [&](int c) { return records + static_cast<size_t>(c) * a.p.Hv * a.record; };
     const auto fetch = [&](int c) {
         const int64_t t0 = be.x + c * kC;
@@ -638,34 +673,38 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
         for (int i = 0; i < UQ; ++i) {
             kx[i] = sh.template load<VEC>(static_cast<const T *>(a.p.k) + t0 * a.p.sk + hq * a.p.dk, a.p.sk, i, a.p.dk, len);
-            qx[i] = sh.template load<VEC>(static_cast<const T *>(a.p.q) + t0 * a.p.sq + hq * a.p.dk, a.p.sq, i, a.p.dk, len);
+            if constexpr (OUT)
+                qx[i] = sh.template load<VEC>(static_cast<const T *>(a.p.q) + t0 * a.p.sq + hq * a.p.dk, a.p.sq, i, a.p.dk, len);
         }
     };
     // values past the last token repeat it: their rows of U are 0 (beta is 0 there)
     const auto fetch_values = [&](int c) {
         const int64_t t0 = be.x + c * kC;
         const int len = min(kC, be.y - static_cast<int>(t0));
+        if (values)
 #pragma unroll
         for (int i = 0; i < UV; ++i)
             vx[i] = sv.template load<VEC>(static_cast<const T *>(a.p.v) + t0 * a.p.sv + h * a.p.dv + col0, a.p.sv, i, W, len);
-        const ChunkGates *cg = reinterpret_cast<const ChunkGates *>(record(c));
-        if (wv == 0) lgx = cg->lg[lane], gx = cg->g[lane], wx = cg->w[lane], bx = cg->b[lane];
+        const uint32_t *words = reinterpret_cast<const uint32_t *>(record(c));
+#pragma unroll
+        for (int i = 0; i < NG; ++i) gx[i] = words[min(static_cast<int>(threadIdx.x) + 64 * NW * i, kGateWords - 1)];
     };
-    if (chunks > 0) fetch(0), fetch_values(0);
+    if (chunks > first) fetch(first), fetch_values(first);
 
-    for (int c = 0; c < chunks; ++c) {
+    for (int c = first; c < chunks; ++c) {
         const int64_t t0 = be.x + c * kC;
         const int len = min(kC, be.y - static_cast<int>(t0));
         if (len < kC || a.p.dk < DKP) {
 #pragma unroll
             for (int i = 0; i < UQ; ++i) {
                 const bool keep = sh.valid(i, a.p.dk, len);
-                kx[i] = zero_unless(keep, kx[i]), qx[i] = zero_unless(keep, qx[i]);
+                kx[i] = zero_unless(keep, kx[i]);
+                if constexpr (OUT) qx[i] = zero_unless(keep, qx[i]);
             }
         }
         again();
         tops[0][wv] = wave_max_of(kx);
-        tops[1][wv] = wave_max_of(qx);
+        if constexpr (OUT) tops[1][wv] = wave_max_of(qx);
         lds_barrier();
         const ChunkGates *cg = reinterpret_cast<const ChunkGates *>(record(c));
         int bad = kC;
@@ -673,30 +712,35 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         if constexpr (DELTA) {
             const f16x8 *from = reinterpret_cast<const f16x8 *>(cg + 1) + lane;
 #pragma unroll
-            for (int i = 0; i < 8 / NW; ++i)
-                if (wv + NW * i < 6) tx[i][0] = from[(wv + NW * i) * 64], tx[i][1] = from[(wv + NW * i + 6) * 64];
+            for (int i = 0; i < NP; ++i) tx[i] = from[(wv + NW * i) % 12 * 64];
             bad = cg->bad, tmax = cg->tmax;
         }
         uint32_t mk = 0, mq = 0;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) mk = max(mk, tops[0][i]), mq = max(mq, tops[1][i]);
+        for (int i = 0; i < NW; ++i) {
+            mk = max(mk, tops[0][i]);
+            if constexpr (OUT) mq = max(mq, tops[1][i]);
+        }
         const Pow2 sk = scale_for(mk), sq = scale_for(mq);
         const auto at = sh.again();
 #pragma unroll
         for (int i = 0; i < UQ; ++i) {
             K.put(at.row + at.step * i, at.c8, kx[i], sk.up);
-            Q.put(at.row + at.step * i, at.c8, qx[i], sq.up);
+            if constexpr (OUT) Q.put(at.row + at.step * i, at.c8, qx[i], sq.up);
         }
         const auto av = sv.again();
 #pragma unroll
         for (int i = 0; i < UV; ++i) V.put(av.row + av.step * i, av.c8, vx[i]);
-        if (wv == 0) ga.lg[lane] = lgx, ga.g[lane] = gx, ga.w[lane] = wx, ga.b[lane] = bx;
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+            reinterpret_cast<uint32_t *>(&ga)[min(static_cast<int>(threadIdx.x) + 64 * NW * i, kGateWords - 1)] = gx[i];
         lds_barrier();
         if (c + 1 < chunks) fetch(c + 1);
 
         again();
         // P times 2^-22 of the scales (|q.k| < 2^35 scaled), a block of 16 rows x 32 columns to a wave:
         // lane (g, n) forms row i = 16 rb + n, columns 16 tt + 4 g .. + 3
+        if constexpr (OUT)
 #pragma unroll
         for (int b = wv; b < 6; b += NW) {
             const int rb = triangle_row(b), pb = triangle_block(b);
@@ -729,6 +773,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         // K S and Q S
         f32x4 ks[4], o[4];
         float sm = 0.0f;
+        if (OUT || DELTA)
 #pragma unroll
         for (int rt = 0; rt < DKP / 16; ++rt)
 #pragma unroll
@@ -737,14 +782,16 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
         for (int rb = 0; rb < 4; ++rb) ks[rb] = o[rb] = f32x4{};
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
+        for (int kb = 0; kb < (OUT || DELTA ? KB : 0); ++kb) {
             f16x8 sp[2];
             split(S[2 * kb], S[2 * kb + 1], ss.up, sp);
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb) {
-                f16x8 q[NA];
-                Q.rows(rb, kb, g, n, q);
-                mma<2>(o[rb], q, sp);
+                if constexpr (OUT) {
+                    f16x8 q[NA];
+                    Q.rows(rb, kb, g, n, q);
+                    mma<2>(o[rb], q, sp);
+                }
                 if constexpr (DELTA) {
                     f16x8 k[NA];
                     K.rows(rb, kb, g, n, k);
@@ -766,7 +813,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
                 if (DELTA) ks[rb][r] = fmaf(-(gg[r] * sk.down), ks[rb][r] * ss.down, v[r]);
                 else ks[rb][r] = v[r] * bb[r];
                 z = fmaf(ks[rb][r], 0.0f, z);
-                o[rb][r] = (gg[r] * sq.down) * (o[rb][r] * ss.down);
+                if (OUT) o[rb][r] = (gg[r] * sq.down) * (o[rb][r] * ss.down);
             }
         }
         // tokens from `from` on are lost in their column: what is not finite there may not reach the others
@@ -789,8 +836,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         }
         if constexpr (DELTA)
 #pragma unroll
-            for (int i = 0; i < 8 / NW; ++i)
-                if (wv + NW * i < 6) Tt.put(wv + NW * i, lane, tx[i]);
+            for (int i = 0; i < NP; ++i)
+                *reinterpret_cast<f16x8 *>(&Tt.b[0][0] + (wv + NW * i) % 12 * 1024 + lane * 16) = tx[i];
         lds_barrier();
         again();
         // U = T' R: in ks, times fu
@@ -817,7 +864,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         fu *= su.down;
         again();
         // O += P U
-        {
+        if constexpr (OUT) {
             f16x8 up[2][2];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], su.up, up[kb]);
@@ -835,7 +882,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
                 for (int r = 0; r < 4; ++r) o[rb][r] = fmaf(y[r], f, o[rb][r]);
             }
         }
-        if (lost)
+        if (OUT && lost)
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
 #pragma unroll
@@ -844,7 +891,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         Out4<T> y[4];
 #pragma unroll
         for (int rb = 0; rb < 4; ++rb) y[rb].set(o[rb]);
-        const auto store = [&] {
+        const auto store = [&](int m) {
             T *out = static_cast<T *>(a.p.o) + t0 * a.p.so + h * a.p.dv + col0 + mycol + n;
             const int row4 = 4 * g;
 #pragma unroll
@@ -852,16 +899,17 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = 16 * rb + row4 + r;
-                    if (len == kC || row < len) *row_of(out, row, a.p.so) = y[rb].at(r);
+                    if (row < m) *row_of(out, row, a.p.so) = y[rb].at(r);
                 }
         };
         // bfloat16 outputs wait in half the registers, so that what the next chunk needs is asked for first
-        if constexpr (sizeof(T) == 4) again(), store();
+        if constexpr (OUT && sizeof(T) == 4) again(), len == kC ? store(kC) : store(len);
         if (c + 1 < chunks) fetch_values(c + 1);
         again();
         // S <- G_last S + K^T (w U)
         {
             const float glast = ga.g[kC - 1], f = sk.down * fu;
+            if (!OUT) gamma *= glast;
             f16x8 up[2][2];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
@@ -885,11 +933,91 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         if (lost && from < kC)
 #pragma unroll
             for (int rt = 0; rt < DKP / 16; ++rt) S[rt] = f32x4{NAN, NAN, NAN, NAN};
-        if constexpr (sizeof(T) == 2) again(), store();
+        if constexpr (OUT && sizeof(T) == 2) again(), len == kC ? store(kC) : store(len);
     }
 
-    each_state_row<DKP>(a.p.state_out + (static_cast<size_t>(s) * a.p.Hv + h) * a.p.dk * a.p.dv + col0 + mycol, a.p.dk, a.p.dv,
-                        g, n, [&](float *at, int rt, int r) { *at = S[rt][r]; });
+    const auto put = [&](float *at, int rt, int r) { *at = S[rt][r]; };
+    if constexpr (OUT) {
+        if (chunks == total)
+            each_state_row<DKP>(a.p.state_out + (static_cast<size_t>(s) * a.p.Hv + h) * a.p.dk * a.p.dv + col0 + mycol, a.p.dk,
+                                a.p.dv, g, n, put);
+    } else {
+        if (cb == 0 && threadIdx.x == 0) rec[0] = gamma;
+        float *to = rec + kSegmentHead + col0 + mycol;
+        if (values) each_state_row<DKP>(to, a.p.dk, a.p.dv, g, n, put);
+        else if (col0 + mycol < DKP) each_state_row<DKP>(to + a.p.dk * a.p.dv, DKP, DKP, g, n, put);
+    }
+}
+
+// The states after the segments of a sequence, in order, decay rule: 4 elements a thread.
+__global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
+{
+    const int quads = a.p.dk * a.p.dv / 4, blocks = (quads + 255) / 256;
+    const int h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv, e = blockIdx.x % blocks * 256 + threadIdx.x;
+    const int2 be = seq_bounds(a.p, s);
+    const int total = (be.y - be.x + kC - 1) / kC, parts = (total + a.seg - 1) / a.seg;
+    if (e >= quads) return;
+    const float *from = initial_state(a.p, s, h);
+    f32x4 S = {};
+    if (from)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[i] = from[4 * e + i];
+    float *rec = a.segs + (static_cast<size_t>(first_slot(a.p, s, kC * a.seg)) * a.p.Hv + h) * a.seg_floats;
+    for (int j = 0; j + 1 < parts; ++j, rec += a.p.Hv * a.seg_floats) {
+        f32x4 *B = reinterpret_cast<f32x4 *>(rec + kSegmentHead) + e;
+        S = *B + S * rec[0];
+        *B = S;
+    }
+}
+
+// The same for the Delta rule: S <- A S + B in fp32 products, a wave 16 columns
+// of the state (its rows here in order: 16 kt + 4 g + r).
+template <int DKP>
+__global__ __launch_bounds__(256) void prompt_join_delta_kernel(ChunkArgs a)
+{
+    constexpr int KT = DKP / 16;
+    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+    const int blocks = a.p.dv / 64, h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv;
+    const int col = blockIdx.x % blocks * 64 + wv * 16 + n;
+    const int2 be = seq_bounds(a.p, s);
+    const int total = (be.y - be.x + kC - 1) / kC, parts = (total + a.seg - 1) / a.seg;
+    const float *from = initial_state(a.p, s, h);
+    f32x4 S[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * kt + 4 * g + r;
+            S[kt][r] = from && i < a.p.dk ? from[i * a.p.dv + col] : 0.0f;
+        }
+    float *rec = a.segs + (static_cast<size_t>(first_slot(a.p, s, kC * a.seg)) * a.p.Hv + h) * a.seg_floats;
+    for (int j = 0; j + 1 < parts; ++j, rec += a.p.Hv * a.seg_floats) {
+        float *B = rec + kSegmentHead + col;
+        const f32x4 *A = reinterpret_cast<const f32x4 *>(rec + kSegmentHead + a.p.dk * a.p.dv) + n * (DKP / 4) + g;
+        f32x4 y[KT];
+#pragma unroll
+        for (int rt = 0; rt < KT; ++rt) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * rt + 4 * g + r;
+                y[rt][r] = i < a.p.dk ? B[i * a.p.dv] : 0.0f;
+            }
+            f32x4 x[KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) x[kt] = A[rt * 16 * (DKP / 4) + 4 * kt];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[kt][r], S[kt][r], y[rt], 0, 0, 0);
+        }
+#pragma unroll
+        for (int rt = 0; rt < KT; ++rt) {
+            S[rt] = y[rt];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * rt + 4 * g + r < a.p.dk) B[(16 * rt + 4 * g + r) * a.p.dv] = y[rt][r];
+        }
+    }
 }
 
 template <typename T, int DKP, bool DELTA, bool VEC>
@@ -898,9 +1026,16 @@ void launch_rule(const ChunkArgs &a, hipStream_t s)
     const int64_t items = static_cast<int64_t>(a.slots) * a.p.Hv;
     if constexpr (DELTA) prompt_solve_kernel<T, DKP, VEC><<<dim3(static_cast<unsigned>(items)), 256, 0, s>>>(a);
     else prompt_gates_kernel<<<dim3(static_cast<unsigned>((items + 3) / 4)), 256, 0, s>>>(a);
-    const dim3 grid(static_cast<unsigned>(a.p.n_seq) * a.p.Hv);
-    if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC><<<grid, 512, 0, s>>>(a);
-    else prompt_chunks_kernel<T, DKP, 4, DELTA, VEC><<<grid, 256, 0, s>>>(a);
+    const unsigned pairs = static_cast<unsigned>(a.p.n_seq) * a.p.Hv, walks = static_cast<unsigned>(a.seg ? a.seg_slots : a.p.n_seq) * a.p.Hv;
+    if (a.seg) {
+        const unsigned blocks = 1 + (DELTA ? (DKP + a.p.dv - 1) / a.p.dv : 0);
+        if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC, false><<<dim3(walks * blocks), 512, 0, s>>>(a);
+        else prompt_chunks_kernel<T, DKP, 4, DELTA, VEC, false><<<dim3(walks * blocks), 256, 0, s>>>(a);
+        if constexpr (DELTA) prompt_join_delta_kernel<DKP><<<dim3(pairs * (a.p.dv / 64)), 256, 0, s>>>(a);
+        else prompt_join_decay_kernel<<<dim3(pairs * ((a.p.dk * a.p.dv / 4 + 255) / 256)), 256, 0, s>>>(a);
+    }
+    if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC, true><<<dim3(walks), 512, 0, s>>>(a);
+    else prompt_chunks_kernel<T, DKP, 4, DELTA, VEC, true><<<dim3(walks), 256, 0, s>>>(a);
 }
 
 template <typename T, int DKP>
@@ -945,10 +1080,43 @@ stepq_status check(const stepq_prompt_desc *d)
     return STEPQ_OK;
 }
 
+// Chunks per segment; 0: sequences are walked whole.  Lengths are not known
+// here: the average decides.
+int32_t segment_chunks(const stepq_prompt_desc *d)
+{
+    const int64_t pairs = int64_t(d->n_seq) * d->n_v_heads, each = d->n_seq ? slots(d) / d->n_seq : 0;
+    const bool delta = d->rule == STEPQ_RULE_DELTA;
+    if (pairs < 1 || pairs >= 160) return 0;
+    const int64_t parts = std::min((delta ? 256 : 768) / pairs, each / (delta ? 8 : 4));
+    return parts < (delta ? 4 : 2) ? 0 : static_cast<int32_t>((each + parts - 1) / parts);
+}
+
 size_t record_bytes(const stepq_prompt_desc *d)
 {
     return sizeof(ChunkGates) + (d->rule == STEPQ_RULE_DELTA ? kTBytes : 0);
 }
+
+struct Layout {              // of the workspace
+    size_t record, chunks;   // bytes per (chunk, head), of all
+    int32_t seg, seg_slots;
+    size_t seg_floats, bytes;
+};
+
+Layout layout_of(const stepq_prompt_desc *d)
+{
+    Layout l{};
+    l.record = record_bytes(d);
+    l.chunks = (static_cast<size_t>(slots(d)) * d->n_v_heads * l.record + 255) / 256 * 256;
+    l.seg = segment_chunks(d);
+    if (l.seg) {
+        l.seg_slots = static_cast<int32_t>(d->n_tokens / (kC * int64_t(l.seg)) + d->n_seq);
+        const size_t dkp = d->d_k > 64 ? 128 : 64;
+        l.seg_floats = kSegmentHead + (size_t(d->d_k) * d->d_v + (d->rule == STEPQ_RULE_DELTA ? dkp * dkp : 0) + 63) / 64 * 64;
+    }
+    l.bytes = l.chunks + static_cast<size_t>(l.seg_slots) * d->n_v_heads * l.seg_floats * sizeof(float);
+    return l;
+}
+
 
 }  // namespace
 }  // namespace stepq
@@ -959,7 +1127,7 @@ extern "C" stepq_status stepq_prompt_workspace(const stepq_prompt_desc *d, size_
 {
     if (const stepq_status st = check(d)) return st;
     if (!bytes) return bad("bytes is NULL");
-    *bytes = static_cast<size_t>(slots(d)) * d->n_v_heads * record_bytes(d);
+    *bytes = layout_of(d).bytes;
     return STEPQ_OK;
 }
 
@@ -975,9 +1143,8 @@ extern "C" stepq_status stepq_prompt(const stepq_prompt_desc *d, const int32_t *
     if (!state_in && in_ids) return bad("in_ids without state_in");
     if (state_in && !in_ids && d->n_states_in < d->n_seq) return bad("fewer states in state_in than sequences");
     if (state_in == state_out && in_ids) return bad("state_out must not be state_in where in_ids chooses the states");
-    size_t need = 0;
-    stepq_prompt_workspace(d, &need);
-    if (!workspace || workspace_bytes < need) return bad("workspace is smaller than stepq_prompt_workspace()");
+    const Layout l = layout_of(d);
+    if (!workspace || workspace_bytes < l.bytes) return bad("workspace is smaller than stepq_prompt_workspace()");
     if (!aligned(workspace, 256) || !aligned(state_out, 4)) return bad("workspace must be 256-byte aligned");
     const int64_t qk = int64_t(d->n_qk_heads) * d->d_k, vo = int64_t(d->n_v_heads) * d->d_v;
     const int32_t gf = d->gate_dtype == STEPQ_F32;
@@ -987,8 +1154,10 @@ extern "C" stepq_status stepq_prompt(const stepq_prompt_desc *d, const int32_t *
                      d->o_stride ? d->o_stride : vo, static_cast<int32_t>(d->n_tokens), d->n_seq, d->n_v_heads,
                      d->n_qk_heads, d->d_k, d->d_v, d->n_states_in};
     a.ws = static_cast<uint8_t *>(workspace);
-    a.record = record_bytes(d);
+    a.record = l.record;
     a.slots = static_cast<int32_t>(slots(d));
+    a.seg = l.seg, a.seg_slots = l.seg_slots, a.seg_floats = l.seg_floats;
+    a.segs = reinterpret_cast<float *>(a.ws + l.chunks);
     const int e = d->act_dtype == STEPQ_BF16 ? 8 : 4;   // elements in 16 bytes
     const bool vec = d->d_k % 8 == 0 && (a.p.sq | a.p.sk | a.p.sv) % e == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16);
     const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -122,6 +122,35 @@ def test_long(rule):
 
 @pytest.mark.parametrize("rule", [DECAY, DELTA])
 @pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("dk,dv", [(128, 128), (77, 64), (64, 128), (96, 128), (33, 64)])
+def test_few_long_sequences(dk, dv, act, rule):
+    """Few heads and many tokens: sequences are cut into segments that are walked side by side."""
+    check([4100, 0, 2049, 3], 1, 1, dk, dv, act, F32, rule, start="shared", low=0.98, seed=dk)
+    check([3000], 2, 1, dk, dv, act, F32, rule, start="own", low=0.98, in_place=True)
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("what", ["v", "k", "alpha"])
+def test_not_finite_in_a_long_sequence(what, rule):
+    """What holds inside a chunk holds across the segments."""
+    j, T = 1500, 4100
+    clean = run([T], 1, 1, 64, 64, BF16, F32, rule, low=0.98)
+
+    def edit(q, k, v, alpha, beta):
+        if what == "v":
+            v[j, 0, 9] = math.nan
+        else:
+            dict(k=k, alpha=alpha)[what].view(T, -1)[j, 0] = math.nan
+    o, out, _, _ = run([T], 1, 1, 64, 64, BF16, F32, rule, low=0.98, edit=edit)
+    hit = torch.zeros(T, 1, 64, dtype=torch.bool)
+    hit[j:, 0, 9 if what == "v" else slice(None)] = True
+    assert torch.isnan(o.cpu()[hit]).all()
+    assert torch.equal(o.cpu()[~hit], clean[0].cpu()[~hit])
+    assert torch.isnan(out[0, 0, :, 9]).any()
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
 def test_without_beta(act, rule):
     check([100], 2, 2, 64, 64, act, F32, rule, beta=False)
 
