@@ -970,53 +970,70 @@ __global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
     }
 }
 
-// The same for the Delta rule: S <- A S + B in fp32 products, a wave 16 columns
-// of the state (its rows here in order: 16 kt + 4 g + r).
+// The same for the Delta rule, S <- A S + B in fp32 products: a workgroup 16
+// columns of the state, a wave a quarter of its rows.  The state goes around
+// through LDS; A does not depend on it and is asked for one segment ahead.
 template <int DKP>
 __global__ __launch_bounds__(256) void prompt_join_delta_kernel(ChunkArgs a)
 {
-    constexpr int KT = DKP / 16;
+    constexpr int KT = DKP / 16, RT = KT / 4, LD = DKP + 4;
+    __shared__ alignas(16) float st[2][16 * LD];      // [column][row]
     const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
-    const int blocks = a.p.dv / 64, h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv;
-    const int col = blockIdx.x % blocks * 64 + wv * 16 + n;
+    const int blocks = a.p.dv / 16, h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv;
+    const int col = blockIdx.x % blocks * 16 + n, row0 = 16 * RT * wv + 4 * g;     // + 16 rt + r
     const int2 be = seq_bounds(a.p, s);
     const int total = (be.y - be.x + kC - 1) / kC, parts = (total + a.seg - 1) / a.seg;
+    if (parts < 2) return;
     const float *from = initial_state(a.p, s, h);
-    f32x4 S[KT];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+    for (int rt = 0; rt < RT; ++rt) {
+        f32x4 x;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = 16 * kt + 4 * g + r;
-            S[kt][r] = from && i < a.p.dk ? from[i * a.p.dv + col] : 0.0f;
+            const int i = row0 + 16 * rt + r;
+            x[r] = from && i < a.p.dk ? from[i * a.p.dv + col] : 0.0f;
         }
+        *reinterpret_cast<f32x4 *>(&st[0][n * LD + row0 + 16 * rt]) = x;
+    }
+    const size_t step = a.p.Hv * a.seg_floats;
     float *rec = a.segs + (static_cast<size_t>(first_slot(a.p, s, kC * a.seg)) * a.p.Hv + h) * a.seg_floats;
-    for (int j = 0; j + 1 < parts; ++j, rec += a.p.Hv * a.seg_floats) {
-        float *B = rec + kSegmentHead + col;
-        const f32x4 *A = reinterpret_cast<const f32x4 *>(rec + kSegmentHead + a.p.dk * a.p.dv) + n * (DKP / 4) + g;
-        f32x4 y[KT];
+    f32x4 x[RT][KT], y[RT];
+    const auto fetch = [&](const float *at) {
+        const f32x4 *A = reinterpret_cast<const f32x4 *>(at + kSegmentHead + a.p.dk * a.p.dv) + (16 * RT * wv + n) * (DKP / 4) + g;
 #pragma unroll
-        for (int rt = 0; rt < KT; ++rt) {
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) x[rt][kt] = A[rt * 16 * (DKP / 4) + 4 * kt];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * rt + 4 * g + r;
-                y[rt][r] = i < a.p.dk ? B[i * a.p.dv] : 0.0f;
+                const int i = row0 + 16 * rt + r;
+                y[rt][r] = i < a.p.dk ? at[kSegmentHead + i * a.p.dv + col] : 0.0f;
             }
-            f32x4 x[KT];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) x[kt] = A[rt * 16 * (DKP / 4) + 4 * kt];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) y[rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[kt][r], S[kt][r], y[rt], 0, 0, 0);
         }
+    };
+    fetch(rec);
+    for (int j = 0; j + 1 < parts; ++j, rec += step) {
+        __syncthreads();
 #pragma unroll
-        for (int rt = 0; rt < KT; ++rt) {
-            S[rt] = y[rt];
+        for (int kt = 0; kt < KT; ++kt) {
+            const f32x4 S = *reinterpret_cast<const f32x4 *>(&st[j & 1][n * LD + 16 * kt + 4 * g]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[rt][kt][r], S[r], y[rt], 0, 0, 0);
+        }
+        f32x4 z[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            z[rt] = y[rt];
+            *reinterpret_cast<f32x4 *>(&st[~j & 1][n * LD + row0 + 16 * rt]) = z[rt];
+        }
+        if (j + 2 < parts) fetch(rec + step);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (16 * rt + 4 * g + r < a.p.dk) B[(16 * rt + 4 * g + r) * a.p.dv] = y[rt][r];
-        }
+                if (row0 + 16 * rt + r < a.p.dk) rec[kSegmentHead + (row0 + 16 * rt + r) * a.p.dv + col] = z[rt][r];
     }
 }
 
@@ -1031,7 +1048,7 @@ void launch_rule(const ChunkArgs &a, hipStream_t s)
         const unsigned blocks = 1 + (DELTA ? (DKP + a.p.dv - 1) / a.p.dv : 0);
         if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC, false><<<dim3(walks * blocks), 512, 0, s>>>(a);
         else prompt_chunks_kernel<T, DKP, 4, DELTA, VEC, false><<<dim3(walks * blocks), 256, 0, s>>>(a);
-        if constexpr (DELTA) prompt_join_delta_kernel<DKP><<<dim3(pairs * (a.p.dv / 64)), 256, 0, s>>>(a);
+        if constexpr (DELTA) prompt_join_delta_kernel<DKP><<<dim3(pairs * (a.p.dv / 16)), 256, 0, s>>>(a);
         else prompt_join_decay_kernel<<<dim3(pairs * ((a.p.dk * a.p.dv / 4 + 255) / 256)), 256, 0, s>>>(a);
     }
     if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC, true><<<dim3(walks), 512, 0, s>>>(a);
