@@ -58,6 +58,7 @@ struct ChunkArgs {
     int32_t seg_slots;       // segment slots, numbered as the chunks' are, with 64 seg tokens each
     float *segs;             // per (segment, head): SegmentHead, B or the state after it [dk][dv], A [DKP][DKP] (Delta)
     size_t seg_floats;
+    int32_t near;            // 64 tokens of q, k and v lie within 2^32 bytes
 };
 
 __device__ __forceinline__ int2 seq_bounds(const PromptArgs &a, int s)
@@ -112,29 +113,79 @@ __device__ __forceinline__ T *row_of(T *base, uint32_t r, int64_t stride)
     return reinterpret_cast<T *>(reinterpret_cast<B *>(base) + at);
 }
 
-// 8 elements of a row of n valid ones from element i on.
+// 8 elements from an address that is a multiple of ALIGN bytes (the hardware
+// takes 16-byte loads at any).
+template <int ALIGN, typename T>
+__device__ __forceinline__ Act<T> load_wide(const T *p)
+{
+    struct __attribute__((packed, aligned(ALIGN))) Raw {
+        u32x4 x;
+    };
+    const Raw *r = reinterpret_cast<const Raw *>(p);
+    if constexpr (sizeof(T) == 2) return Act<T>{r[0].x};
+    else return Act<T>{{__builtin_bit_cast(f32x4, r[0].x), __builtin_bit_cast(f32x4, r[1].x)}};
+}
+
+// 8 elements of a row of n valid ones from element i on; elements past n are
+// anything until settle() (nothing here waits for the data).  VEC: everything is
+// 16-byte aligned and n a multiple of 8.
 template <bool VEC, typename T>
 __device__ __forceinline__ Act<T> load8(const T *row, int i, int n)
 {
+    // past n, the first elements are read (no branch around the load)
+    if constexpr (VEC) return load_wide<16>(row + (i < n ? i : 0));
+    if (n >= 8) return load_wide<sizeof(T)>(row + min(i, n - 8));
     Act<T> r = {};
-    if constexpr (VEC) {
-        // n is a multiple of 8: past it, the first elements are read and dropped (no branch around the load)
-        const T *p = row + (i < n ? i : 0);
-        if constexpr (sizeof(T) == 2) {
-            r.x = *reinterpret_cast<const u32x4 *>(p);
-        } else {
-            r.x[0] = reinterpret_cast<const f32x4 *>(p)[0];
-            r.x[1] = reinterpret_cast<const f32x4 *>(p)[1];
-        }
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (i + e < n) {
-                if constexpr (sizeof(T) == 2) r.x[e / 2] |= static_cast<uint32_t>(row[i + e]) << (16 * (e % 2));
-                else r.x[e / 4][e % 4] = row[i + e];
-            }
+    for (int e = 0; e < 8; ++e) {
+        const T x = row[min(e, n - 1)];
+        if constexpr (sizeof(T) == 2) r.x[e / 2] |= static_cast<uint32_t>(x) << (16 * (e % 2));
+        else r.x[e / 4][e % 4] = x;
     }
     return r;
+}
+
+// What load8<false> gave for elements i .. i + 7, in place, zeros past n: the
+// unit that n ends in was read from n - 8 on.
+template <typename T>
+__device__ __forceinline__ Act<T> settle(const Act<T> &v, int i, int n)
+{
+    const bool tail = i < n && i + 8 > n;
+    const int shift = n >= 8 ? (8 - n % 8) % 8 : 0;       // the same for all lanes
+    if constexpr (sizeof(T) == 2) {
+        u32x4 x = v.x;
+        if (shift & 4) x = u32x4{x[2], x[3], 0u, 0u};
+        if (shift & 2) x = u32x4{x[1], x[2], x[3], 0u};
+        if (shift & 1)
+            x = u32x4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16),
+                      __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
+        Act<T> r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t keep = (i + 2 * e < n ? 0xffffu : 0u) | (i + 2 * e + 1 < n ? 0xffff0000u : 0u);
+            r.x[e] = (tail ? x[e] : v.x[e]) & keep;
+        }
+        return r;
+    } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = v.x[e / 4][e % 4];
+#pragma unroll
+        for (int b = 4; b > 0; b >>= 1)
+            if (shift & b)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = e + b < 8 ? x[e + b] : 0.0f;
+        Act<T> r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.x[e / 4][e % 4] = i + e < n ? (tail ? x[e] : v.x[e / 4][e % 4]) : 0.0f;
+        return r;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ Act<T> load_at(const T *base, uint32_t at)
+{
+    return load_wide<16>(reinterpret_cast<const T *>(reinterpret_cast<const uint8_t *>(base) + at));
 }
 
 // A thread's share of a tile of 64 rows of C8 8-element units, N threads: unit c8 of the rows row + step u.
@@ -197,19 +248,29 @@ __device__ __forceinline__ Act<T> zero_unless(bool keep, const Act<T> &v)
     return r;
 }
 
-// |x|'s largest of 8 elements, as bits; what is not finite counts as nothing
-template <typename T>
-__device__ __forceinline__ uint32_t max8(uint32_t m, const Act<T> &v)
+// |x|'s largest of a thread's N units, as the bits of a float
+template <int N>
+__device__ __forceinline__ uint32_t max_of(const Act<bf16_t> (&v)[N])
 {
+    using u16x2 = __attribute__((ext_vector_type(2))) uint16_t;
+    u16x2 m = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a, b;
-        if constexpr (sizeof(T) == 2) a = lower_bf16(v.x[i]), b = upper_bf16(v.x[i]);
-        else a = v.x[i / 2][2 * (i % 2)], b = v.x[i / 2][2 * (i % 2) + 1];
-        m = max(m, max(__float_as_uint(fabsf(a)), __float_as_uint(fabsf(b))));
-    }
-    return m;
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i].x[e] & 0x7fff7fffu));
+    return static_cast<uint32_t>(max(m[0], m[1])) << 16;
 }
+template <int N>
+__device__ __forceinline__ uint32_t max_of(const Act<float> (&v)[N])
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[i].x[e / 4][e % 4]));
+    return __float_as_uint(m);
+}
+// the same without what is not finite
 constexpr uint32_t kInfBits = 0x7f800000u;
 template <typename T>
 __device__ __forceinline__ uint32_t finite_max8(uint32_t m, const Act<T> &v)
@@ -228,12 +289,9 @@ __device__ __forceinline__ uint32_t finite_max8(uint32_t m, const Act<T> &v)
 template <int N, typename T>
 __device__ __forceinline__ uint32_t wave_max_of(const Act<T> (&v)[N])
 {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = max8(m, v[i]);
-    uint32_t w = wave_max(m);
+    uint32_t w = wave_max(max_of(v));
     if (w >= kInfBits) {
-        m = 0;
+        uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) m = finite_max8(m, v[i]);
         w = wave_max(m);
@@ -446,7 +504,10 @@ __global__ __launch_bounds__(256) void prompt_solve_kernel(ChunkArgs a)
     bool fine;
     const double lg = scan_gates(a.p, t0, len, h, lane, &beta, &fine);
 #pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = zero_unless(sh.valid(i, a.p.dk, len), v[i]);
+    for (int i = 0; i < U; ++i) {
+        if constexpr (!VEC) v[i] = settle(v[i], 8 * sh.c8, a.p.dk);
+        v[i] = zero_unless(sh.valid(i, a.p.dk, len), v[i]);
+    }
     kmax_s[w] = wave_max_of(v);
     __syncthreads();
     const Pow2 sk = scale_for(max(max(kmax_s[0], kmax_s[1]), max(kmax_s[2], kmax_s[3])));
@@ -667,9 +728,23 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     constexpr int NG = (kGateWords + 64 * NW - 1) / (64 * NW);
     uint32_t gx[NG];
     const auto record = [&](int c) { return records + static_cast<size_t>(c) * a.p.Hv * a.record; };
+    // Whole chunks whose rows lie within 32-bit offsets: one lane offset per
+    // array for all chunks, the rest in scalar registers.
+    const bool near = VEC && a.near && a.p.dk == DKP;
+    const uint32_t at_k = (sh.row * static_cast<uint32_t>(a.p.sk) + 8 * sh.c8) * static_cast<uint32_t>(sizeof(T));
+    const uint32_t at_q = (sh.row * static_cast<uint32_t>(a.p.sq) + 8 * sh.c8) * static_cast<uint32_t>(sizeof(T));
+    const uint32_t at_v = (sv.row * static_cast<uint32_t>(a.p.sv) + 8 * sv.c8) * static_cast<uint32_t>(sizeof(T));
     const auto fetch = [&](int c) {
         const int64_t t0 = be.x + c * kC;
         const int len = min(kC, be.y - static_cast<int>(t0));
+        if (near && len == kC) {
+#pragma unroll
+            for (int i = 0; i < UQ; ++i) {
+                kx[i] = load_at(static_cast<const T *>(a.p.k) + (t0 + i * sh.step) * a.p.sk + hq * a.p.dk, at_k);
+                if constexpr (OUT) qx[i] = load_at(static_cast<const T *>(a.p.q) + (t0 + i * sh.step) * a.p.sq + hq * a.p.dk, at_q);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < UQ; ++i) {
             kx[i] = sh.template load<VEC>(static_cast<const T *>(a.p.k) + t0 * a.p.sk + hq * a.p.dk, a.p.sk, i, a.p.dk, len);
@@ -681,7 +756,11 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     const auto fetch_values = [&](int c) {
         const int64_t t0 = be.x + c * kC;
         const int len = min(kC, be.y - static_cast<int>(t0));
-        if (values)
+        if (values && near && len == kC) {
+#pragma unroll
+            for (int i = 0; i < UV; ++i)
+                vx[i] = load_at(static_cast<const T *>(a.p.v) + (t0 + i * sv.step) * a.p.sv + h * a.p.dv + col0, at_v);
+        } else if (values)
 #pragma unroll
         for (int i = 0; i < UV; ++i)
             vx[i] = sv.template load<VEC>(static_cast<const T *>(a.p.v) + t0 * a.p.sv + h * a.p.dv + col0, a.p.sv, i, W, len);
@@ -698,6 +777,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
             for (int i = 0; i < UQ; ++i) {
                 const bool keep = sh.valid(i, a.p.dk, len);
+                if constexpr (!VEC) {
+                    kx[i] = settle(kx[i], 8 * sh.c8, a.p.dk);
+                    if constexpr (OUT) qx[i] = settle(qx[i], 8 * sh.c8, a.p.dk);
+                }
                 kx[i] = zero_unless(keep, kx[i]);
                 if constexpr (OUT) qx[i] = zero_unless(keep, qx[i]);
             }
@@ -802,6 +885,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         again();
         // R (Delta) or U (decay), and whether it is finite; O's part from the state
         float z = 0.0f;
+        const float fk = -(sk.down * ss.down), fq = sq.down * ss.down;
 #pragma unroll
         for (int rb = 0; rb < 4; ++rb) {
             const f32x4 gg = *reinterpret_cast<const f32x4 *>(&ga.g[16 * rb + 4 * g]);
@@ -810,10 +894,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
             const f32x4 v = V.four(rb, mycol, g, n);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (DELTA) ks[rb][r] = fmaf(-(gg[r] * sk.down), ks[rb][r] * ss.down, v[r]);
+                if (DELTA) ks[rb][r] = fmaf(gg[r] * fk, ks[rb][r], v[r]);
                 else ks[rb][r] = v[r] * bb[r];
                 z = fmaf(ks[rb][r], 0.0f, z);
-                if (OUT) o[rb][r] = (gg[r] * sq.down) * (o[rb][r] * ss.down);
+                if (OUT) o[rb][r] *= gg[r] * fq;
             }
         }
         // tokens from `from` on are lost in their column: what is not finite there may not reach the others
@@ -892,15 +976,15 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
         for (int rb = 0; rb < 4; ++rb) y[rb].set(o[rb]);
         const auto store = [&](int m) {
-            T *out = static_cast<T *>(a.p.o) + t0 * a.p.so + h * a.p.dv + col0 + mycol + n;
-            const int row4 = 4 * g;
+            // each row's address is the wave's own (scalar) plus this lane's fixed part
+            uint8_t *out = reinterpret_cast<uint8_t *>(static_cast<T *>(a.p.o) + t0 * a.p.so + h * a.p.dv + col0 + mycol);
+            const uint32_t at = (4 * g * static_cast<uint32_t>(a.p.so) + n) * static_cast<uint32_t>(sizeof(T));
+            const int64_t step = a.p.so * static_cast<int64_t>(sizeof(T));
 #pragma unroll
-            for (int rb = 0; rb < 4; ++rb)
+            for (int rb = 0; rb < 4; ++rb, out += 12 * step)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * rb + row4 + r;
-                    if (row < m) *row_of(out, row, a.p.so) = y[rb].at(r);
-                }
+                for (int r = 0; r < 4; ++r, out += step)
+                    if (16 * rb + 4 * g + r < m) *reinterpret_cast<T *>(out + at) = y[rb].at(r);
         };
         // bfloat16 outputs wait in half the registers, so that what the next chunk needs is asked for first
         if constexpr (OUT && sizeof(T) == 4) again(), len == kC ? store(kC) : store(len);
@@ -1173,6 +1257,7 @@ extern "C" stepq_status stepq_prompt(const stepq_prompt_desc *d, const int32_t *
     a.ws = static_cast<uint8_t *>(workspace);
     a.record = l.record;
     a.slots = static_cast<int32_t>(slots(d));
+    a.near = std::max({a.p.sq, a.p.sk, a.p.sv}) <= (int64_t(1) << 23);
     a.seg = l.seg, a.seg_slots = l.seg_slots, a.seg_floats = l.seg_floats;
     a.segs = reinterpret_cast<float *>(a.ws + l.chunks);
     const int e = d->act_dtype == STEPQ_BF16 ? 8 : 4;   // elements in 16 bytes
