@@ -11,9 +11,11 @@
 // the error or handles the case.  Nothing is kept between calls.
 #include <Python.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "stepq.h"
@@ -30,6 +32,11 @@ struct Entry {
     decltype(&stepq_pool_import_pivots) import_pivots;
     int (*get_device)(int *);                  // the runtime's current device
     PyObject *raw_stream, *stream_type;        // torch's raw current-stream query and stream class
+    decltype(&stepq_state_step) state_step;
+    decltype(&stepq_prompt_workspace) prompt_workspace;
+    decltype(&stepq_prompt) prompt;
+    decltype(&stepq_prefix_attention_workspace) attention_workspace;
+    decltype(&stepq_prefix_attention) attention;
 } g{};
 
 struct Plain {
@@ -234,6 +241,210 @@ PyObject *py_tiles(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
+// ---------------------------------------------------------------------------
+// The calls without a pool: everything is on the current device, sizes follow
+// from the tensors.
+
+// bind_calls(state_step, prompt_workspace, prompt, attention_workspace, attention)
+PyObject *py_bind_calls(PyObject *, PyObject *args)
+{
+    unsigned long long f[5];
+    if (!PyArg_ParseTuple(args, "KKKKK", &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+    auto set = [&f](auto &fn, int i) { fn = reinterpret_cast<std::remove_reference_t<decltype(fn)>>(f[i]); };
+    set(g.state_step, 0);
+    set(g.prompt_workspace, 1);
+    set(g.prompt, 2);
+    set(g.attention_workspace, 3);
+    set(g.attention, 4);
+    Py_RETURN_NONE;
+}
+
+bool take_long(PyObject *o, int64_t *out)
+{
+    if (!PyLong_CheckExact(o)) return false;
+    *out = PyLong_AsLongLong(o);
+    if (!PyErr_Occurred()) return true;
+    PyErr_Clear();
+    return false;
+}
+
+const at::Tensor *tensor_of(PyObject *o, int64_t dims)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.dim() == dims && t.layout() == at::kStrided ? &t : nullptr;
+}
+
+bool known(at::ScalarType t) { return t == at::kFloat || t == at::kBFloat16; }
+int code_of(at::ScalarType t) { return t == at::kFloat ? STEPQ_F32 : STEPQ_BF16; }
+
+// The device that q lies on, if it is the current one.
+bool take_device(const at::Tensor &q, Plain *p)
+{
+    int device;
+    if (!q.is_cuda() || !known(q.scalar_type()) || g.get_device(&device) != 0 || q.get_device() != device) return false;
+    p->device = device;
+    return true;
+}
+
+// Tokens whose heads are contiguous: their data and the elements from one to the next.
+bool take_tokens(PyObject *o, const Plain &p, at::ScalarType dt, at::IntArrayRef shape, void **out, int64_t *stride)
+{
+    const at::Tensor *t = tensor_of(o, 3);
+    if (!t || !t->is_cuda() || t->get_device() != p.device || t->scalar_type() != dt || t->sizes() != shape) return false;
+    const auto st = t->strides();
+    const int64_t n = shape[0], h = shape[1], d = shape[2];
+    if (n && ((d > 1 && st[2] != 1) || (h > 1 && st[1] != d) || (n > 1 && st[0] < h * d))) return false;
+    *out = t->data_ptr();
+    *stride = n > 1 ? st[0] : 0;
+    return true;
+}
+
+// alpha, and beta or None
+bool take_gates(PyObject *alpha, PyObject *beta, const Plain &p, at::IntArrayRef shape, void **a, void **b, int *code)
+{
+    const at::Tensor *t = tensor_of(alpha, static_cast<int64_t>(shape.size()));
+    if (!t || !known(t->scalar_type())) return false;
+    *code = code_of(t->scalar_type());
+    *b = nullptr;
+    return take(alpha, p, t->scalar_type(), shape, a) && (beta == Py_None || take(beta, p, t->scalar_type(), shape, b));
+}
+
+// Memory of the current stream for one call (the next owner there comes after it).
+at::Tensor space(size_t bytes, int device)
+{
+    return at::empty({static_cast<int64_t>(bytes)},
+                     at::TensorOptions().dtype(at::kByte).device(at::Device(at::kCUDA, static_cast<at::DeviceIndex>(device))));
+}
+
+// state_step(state, ids, q, k, v, alpha, beta, o, rule, stream) -> status or -1
+PyObject *py_state_step(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded([&]() -> long {
+        if (n_args != 10 || !g.state_step) return -1;
+        const at::Tensor *S = tensor_of(a[0], 4), *q = tensor_of(a[2], 3), *v = tensor_of(a[4], 3);
+        Plain p{};
+        int64_t rule;
+        if (!S || !q || !v || !take_device(*q, &p) || !take_long(a[8], &rule)) return -1;
+        const int64_t B = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2), n = S->size(0);
+        const at::ScalarType dt = q->scalar_type();
+        void *sp, *ip, *qp, *kp, *vp, *ap, *bp, *op, *st;
+        int gate;
+        if (B > INT32_MAX || n > INT32_MAX || !take(a[0], p, at::kFloat, {n, Hv, dk, dv}, &sp) ||
+            !take(a[1], p, at::kInt, {B}, &ip) || !take(a[2], p, dt, {B, Hqk, dk}, &qp) ||
+            !take(a[3], p, dt, {B, Hqk, dk}, &kp) || !take(a[4], p, dt, {B, Hv, dv}, &vp) ||
+            !take_gates(a[5], a[6], p, {B, Hv}, &ap, &bp, &gate) || !take(a[7], p, at::kFloat, {B, Hv, dv}, &op) ||
+            !take_stream(a[9], &st))
+            return -1;
+        const stepq_state_desc d{static_cast<int32_t>(n),  static_cast<int32_t>(Hv), static_cast<int32_t>(Hqk),
+                                 static_cast<int32_t>(dk), static_cast<int32_t>(dv), code_of(dt), gate,
+                                 static_cast<int32_t>(rule)};
+        stepq_status e;
+        Py_BEGIN_ALLOW_THREADS;
+        e = g.state_step(&d, static_cast<float *>(sp), static_cast<const int32_t *>(ip), static_cast<int32_t>(B), qp, kp, vp,
+                         ap, bp, static_cast<float *>(op), st);
+        Py_END_ALLOW_THREADS;
+        return e;
+    });
+}
+
+// prompt(q, k, v, alpha, beta, o, state_out, rule, cu_seqlens, state_in, in_ids): on the current stream, in torch's memory
+PyObject *py_prompt(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded([&]() -> long {
+        if (n_args != 11 || !g.prompt) return -1;
+        const at::Tensor *q = tensor_of(a[0], 3), *v = tensor_of(a[2], 3), *cu = tensor_of(a[8], 1);
+        Plain p{};
+        int64_t rule;
+        if (!q || !v || !cu || cu->size(0) < 1 || !take_device(*q, &p) || !take_long(a[7], &rule)) return -1;
+        const int64_t T = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2), n = cu->size(0) - 1;
+        const at::ScalarType dt = q->scalar_type();
+        stepq_prompt_desc d{};
+        void *qp, *kp, *vp, *op, *ap, *bp, *cp, *out, *in = nullptr, *ids = nullptr, *st;
+        int gate;
+        int64_t m = 0;
+        if (n > INT32_MAX || !take_tokens(a[0], p, dt, {T, Hqk, dk}, &qp, &d.q_stride) ||
+            !take_tokens(a[1], p, dt, {T, Hqk, dk}, &kp, &d.k_stride) ||
+            !take_tokens(a[2], p, dt, {T, Hv, dv}, &vp, &d.v_stride) ||
+            !take_tokens(a[5], p, dt, {T, Hv, dv}, &op, &d.o_stride) ||
+            !take_gates(a[3], a[4], p, {T, Hv}, &ap, &bp, &gate) || !take(a[8], p, at::kInt, {n + 1}, &cp) ||
+            !take(a[6], p, at::kFloat, {n, Hv, dk, dv}, &out))
+            return -1;
+        if (a[9] != Py_None) {
+            const at::Tensor *s = tensor_of(a[9], 4);
+            if (!s) return -1;
+            m = a[10] == Py_None ? n : s->size(0);
+            if (m > INT32_MAX || !take(a[9], p, at::kFloat, {m, Hv, dk, dv}, &in) ||
+                (a[10] != Py_None && !take(a[10], p, at::kInt, {n}, &ids)))
+                return -1;
+            const auto lo = reinterpret_cast<uintptr_t>(in), hi = reinterpret_cast<uintptr_t>(out);
+            const uintptr_t each = static_cast<uintptr_t>(Hv * dk * dv) * sizeof(float);
+            if ((ids || lo != hi) && lo < hi + n * each && hi < lo + m * each) return -1;
+        } else if (a[10] != Py_None) {
+            return -1;
+        }
+        d.n_tokens = T, d.n_seq = static_cast<int32_t>(n);
+        d.n_v_heads = static_cast<int32_t>(Hv), d.n_qk_heads = static_cast<int32_t>(Hqk);
+        d.d_k = static_cast<int32_t>(dk), d.d_v = static_cast<int32_t>(dv);
+        d.act_dtype = code_of(dt), d.gate_dtype = gate, d.rule = static_cast<int32_t>(rule);
+        d.n_states_in = static_cast<int32_t>(m);
+        size_t bytes = 0;
+        stepq_status e = g.prompt_workspace(&d, &bytes);
+        if (e != STEPQ_OK) return e;
+        if (!take_stream(Py_None, &st)) return -1;
+        const at::Tensor ws = space(bytes, p.device);
+        void *wp = bytes ? ws.data_ptr() : nullptr;
+        Py_BEGIN_ALLOW_THREADS;
+        e = g.prompt(&d, static_cast<const int32_t *>(cp), qp, kp, vp, ap, bp, op, static_cast<const float *>(in),
+                     static_cast<const int32_t *>(ids), static_cast<float *>(out), wp, bytes, st);
+        Py_END_ALLOW_THREADS;
+        return e;
+    });
+}
+
+// attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, lengths, o, lse, scale): as prompt
+PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded([&]() -> long {
+        if (n_args != 10 || !g.attention) return -1;
+        const at::Tensor *q = tensor_of(a[0], 3), *kc = tensor_of(a[1], 4), *table = tensor_of(a[5], 2);
+        Plain p{};
+        int64_t prefix;
+        if (!q || !kc || !table || !take_device(*q, &p) || !take_long(a[4], &prefix) || prefix < 0 || !(a[9] == Py_None || PyFloat_CheckExact(a[9])))
+            return -1;
+        const int64_t B = q->size(0), Hq = q->size(1), D = q->size(2), M = table->size(1);
+        const int64_t pages = kc->size(0), Hkv = kc->size(1), page = kc->size(2);
+        const at::ScalarType dt = q->scalar_type();
+        if (page < 1 || B > INT32_MAX || M > INT32_MAX || pages > INT32_MAX || page > INT32_MAX) return -1;
+        const int64_t P = (prefix + page - 1) / page;
+        void *qp, *kp, *vp, *pp = nullptr, *tp, *lp, *op, *ep = nullptr, *st;
+        if (P) {
+            const at::Tensor *t = tensor_of(a[3], 1);
+            if (!t || t->size(0) < P || !take(a[3], p, at::kInt, t->sizes(), &pp)) return -1;
+        }
+        if (!take(a[0], p, dt, {B, Hq, D}, &qp) || !take(a[1], p, dt, {pages, Hkv, page, D}, &kp) ||
+            !take(a[2], p, dt, {pages, Hkv, page, D}, &vp) || !take(a[5], p, at::kInt, {B, M}, &tp) ||
+            !take(a[6], p, at::kInt, {B}, &lp) || !take(a[7], p, dt, {B, Hq, D}, &op) ||
+            (a[8] != Py_None && !take(a[8], p, at::kFloat, {B, Hq}, &ep)))
+            return -1;
+        const stepq_attn_desc d{static_cast<int32_t>(B),     static_cast<int32_t>(Hq),   static_cast<int32_t>(Hkv),
+                                static_cast<int32_t>(D),     static_cast<int32_t>(pages), static_cast<int32_t>(page), prefix,
+                                static_cast<int32_t>(M),     code_of(dt),
+                                static_cast<float>(a[9] == Py_None ? std::pow(static_cast<double>(D), -0.5) : PyFloat_AS_DOUBLE(a[9]))};
+        size_t bytes = 0;
+        stepq_status e = g.attention_workspace(&d, &bytes);
+        if (e != STEPQ_OK) return e;
+        if (!take_stream(Py_None, &st)) return -1;
+        const at::Tensor ws = space(bytes, p.device);
+        void *wp = bytes ? ws.data_ptr() : nullptr;
+        Py_BEGIN_ALLOW_THREADS;
+        e = g.attention(&d, qp, kp, vp, static_cast<const int32_t *>(pp), static_cast<const int32_t *>(tp),
+                        static_cast<const int32_t *>(lp), op, static_cast<float *>(ep), wp, bytes, st);
+        Py_END_ALLOW_THREADS;
+        return e;
+    });
+}
+
 PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, "addresses of the C calls, torch's raw stream query and stream class"},
     {"plain", py_plain, METH_VARARGS, "a pool's handle, device and sizes"},
@@ -242,6 +453,12 @@ PyMethodDef methods[] = {
      "load, import or export"},
     {"tiles", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_tiles)), METH_FASTCALL,
      "dequant, export or import of pivot rows"},
+    {"bind_calls", py_bind_calls, METH_VARARGS, "addresses of the C calls that need no pool"},
+    {"state_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_state_step)), METH_FASTCALL,
+     "one token on full-precision states"},
+    {"prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_prompt)), METH_FASTCALL, "packed prompts"},
+    {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_attention)), METH_FASTCALL,
+     "attention over a shared prefix"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_stepq_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -135,6 +135,7 @@ class _PythonChecks:
     every device call goes through the checks below."""
     plain = staticmethod(lambda *a: None)
     decode = scaled = tiles = staticmethod(lambda *a: -1)
+    state_step = prompt = attention = staticmethod(lambda *a: -1)
 
 
 def native():
@@ -153,6 +154,9 @@ def native():
             "stepq_decode_step_ex", "stepq_pool_load", "stepq_pool_import", "stepq_pool_export", "stepq_pool_dequant",
             "stepq_pool_export_pivots", "stepq_pool_import_pivots", "hipGetDevice")),
             torch._C._cuda_getCurrentRawStream, torch.cuda.Stream)
+        _stepq_args.bind_calls(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
+            "stepq_state_step", "stepq_prompt_workspace", "stepq_prompt", "stepq_prefix_attention_workspace",
+            "stepq_prefix_attention")))
         _native = _stepq_args
     return _native
 
@@ -574,6 +578,9 @@ def stepq_prompt(q, k, v, alpha, beta, o, state_out, rule=STEPQ_RULE_DELTA, cu_s
     1).  cu_seqlens [n+1] int32 (None: one sequence), state_in
     [m][Hv][d_k][d_v] float32 (None: zeros), in_ids [n] int32 the state each
     sequence starts from (None: its own), state_out [n][Hv][d_k][d_v]."""
+    if workspace is None and stream is None and _done(native().prompt(
+            q, k, v, alpha, beta, o, state_out, rule, cu_seqlens, state_in, in_ids)):
+        return
     dt, code = _act_dtype(q, "q")
     dev = q.device
     if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3:
@@ -616,6 +623,8 @@ def stepq_state_step(state, ids, q, k, v, alpha, beta, o, rule=STEPQ_RULE_DELTA,
     [n][Hv][d_k][d_v] float32, ids [B] int32 (distinct; outside [0, n): an
     empty row), q, k [B][Hqk][d_k], v [B][Hv][d_v], alpha, beta [B][Hv]
     (beta None: 1), o [B][Hv][d_v] float32."""
+    if _done(native().state_step(state, ids, q, k, v, alpha, beta, o, rule, stream)):
+        return
     dt, code = _act_dtype(q, "q")
     dev = q.device
     if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3 or not isinstance(state, torch.Tensor) or state.dim() != 4:
@@ -647,6 +656,9 @@ def stepq_prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_t
     [n_pages][Hkv][page][D] of q's dtype, prefix_pages [P] int32 (None
     without a prefix), page_table [B][M] int32, lengths [B] int32, lse
     [B][Hq] float32 (None: not wanted); scale defaults to D ** -0.5."""
+    if workspace is None and stream is None and _done(native().attention(
+            q, k_cache, v_cache, prefix_pages, prefix_len, page_table, lengths, o, lse, scale)):
+        return
     dt, code = _act_dtype(q, "q")
     dev = q.device
     if q.dim() != 3 or not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:

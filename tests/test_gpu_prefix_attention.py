@@ -271,3 +271,13 @@ def test_refusals():
         f(q[:, :3].contiguous(), k, v, pre, prefix, table, lengths, o[:, :3].contiguous())
     with pytest.raises((ValueError, TypeError)):
         f(q, k, v, pre, prefix, table, lengths, o, workspace=torch.empty(4, device=DEV))
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_binding_paths_agree(act, monkeypatch):
+    """The native argument path and the Python one make the same calls."""
+    x = inputs(3, 4, 2, 128, 90, [40, 3, 65], 16, act)
+    a, b = call(x), call(x, scale=0.25)
+    monkeypatch.setattr(stepq, "_native", stepq._PythonChecks)
+    c, d = call(x), call(x, scale=0.25)
+    assert all(torch.equal(p, q) for p, q in zip(a + b, c + d))

@@ -384,3 +384,23 @@ def test_refusals():
         stepq.stepq_state_step(S, ids, q, k, v, alpha, beta, torch.empty((T, hv, dv), device=DEV))
     with pytest.raises(TypeError):
         stepq.stepq_state_step(S, ids, q, k, v, alpha, beta, o)
+
+
+def test_binding_paths_agree(monkeypatch):
+    """The native argument path and the Python one make the same calls."""
+    T, hv = 70, 2
+    x = [t.to(DEV) for t in tokens(T, hv, 2, 64, 64, BF16, F32, 3)]
+    cu = torch.tensor([0, 33, T], dtype=torch.int32, device=DEV)
+    ids = torch.tensor([1, 0], dtype=torch.int32, device=DEV)
+    start = torch.randn((2, hv, 64, 64), device=DEV)
+
+    def both():
+        o, out = torch.zeros((T, hv, 64), dtype=BF16, device=DEV), torch.zeros((2, hv, 64, 64), device=DEV)
+        stepq.stepq_prompt(*x, o, out, DELTA, cu_seqlens=cu, state_in=start, in_ids=ids)
+        y = torch.zeros((2, hv, 64), device=DEV)
+        stepq.stepq_state_step(out, ids, *(t[:2] for t in x), y, DELTA)
+        return o, out, y
+    a = both()
+    monkeypatch.setattr(stepq, "_native", stepq._PythonChecks)
+    b = both()
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
