@@ -309,7 +309,7 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
     constexpr int KK = KT / 32, RB = 2 * D, SL = RB / 16, L = KT * SL / 512, KB = D / 16, DT = D / 32;
     constexpr int SW = SL < 16 ? 128 : 256;
     __shared__ alignas(16) uint8_t ks[KT * RB], vs[KT * RB];
-    __shared__ uint64_t invalid_s;
+    __shared__ uint8_t missing[KT];
     int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int lane = tid & 63, h = lane >> 5, n = lane & 31;
@@ -333,37 +333,59 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
         q[kb] = reinterpret_cast<const bf16x8 *>(static_cast<const bf16_t *>(a.q) + qrow * D)[2 * kb + h];
+    // the scale goes into the exponent, which needs it positive (the maximum is taken before): its sign goes
+    // into the queries, and 0 makes them 0
+    const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
+    if (!(a.scale > 0.0f)) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const u32x4 w = __builtin_bit_cast(u32x4, q[kb]);
+            q[kb] = __builtin_bit_cast(bf16x8, a.scale == 0.0f ? u32x4{} : w ^ 0x80008000u);
+        }
+    }
     const uint8_t *K = static_cast<const uint8_t *>(a.k), *V = static_cast<const uint8_t *>(a.v);
+    // a thread's 16-byte pieces of the next tile, on their way; and the cache rows
+    // of those of the tile after it, so that no load waits for a page id
     u32x4 kx[L], vx[L];
-    const auto fetch = [&](int t0) {
+    int at[L], ahead[L];
+    const auto rows_of = [&](int t0) {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int piece_i = i * 512 + tid, t = t0 + piece_i / SL;
-            const int r = token_row(a, a.prefix_pages, t, hk, t < to);
-            const size_t at = static_cast<size_t>(max(r, 0)) * RB + piece_i % SL * 16;
-            kx[i] = *reinterpret_cast<const u32x4 *>(K + at);
-            const u32x4 y = *reinterpret_cast<const u32x4 *>(V + at);
-            vx[i] = r >= 0 ? y : u32x4{};
+            const int t = t0 + (i * 512 + tid) / SL;
+            ahead[i] = token_row(a, a.prefix_pages, t, hk, t < to);
+        }
+    };
+    const auto fetch = [&] {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            at[i] = ahead[i];
+            const size_t from_byte = static_cast<size_t>(max(at[i], 0)) * RB + (i * 512 + tid) % SL * 16;
+            kx[i] = *reinterpret_cast<const u32x4 *>(K + from_byte);
+            vx[i] = *reinterpret_cast<const u32x4 *>(V + from_byte);
         }
     };
     f32x16 acc[DT] = {};
     float m = -INFINITY, base = 0.0f, l = 0.0f;
-    if (from < to) fetch(from);
+    if (from < to) {
+        rows_of(from);
+        fetch();
+        rows_of(from + KT);
+    }
     for (int t0 = from; t0 < to; t0 += KT) {
         __syncthreads();
         again();
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int piece_i = i * 512 + tid, kr = piece_i / SL, at = kr * RB + ((piece_i % SL ^ swizzle<SW>(kr)) * 16);
-            *reinterpret_cast<u32x4 *>(ks + at) = kx[i];
-            *reinterpret_cast<u32x4 *>(vs + at) = vx[i];
-        }
-        if (wave == 0) {
-            const uint64_t none = __ballot(token_row(a, a.prefix_pages, t0 + lane, hk, t0 + lane < to && lane < KT) < 0 && lane < KT);
-            if (lane == 0) invalid_s = none;
+            const int piece_i = i * 512 + tid, kr = piece_i / SL, to_byte = kr * RB + ((piece_i % SL ^ swizzle<SW>(kr)) * 16);
+            *reinterpret_cast<u32x4 *>(ks + to_byte) = kx[i];
+            *reinterpret_cast<u32x4 *>(vs + to_byte) = at[i] >= 0 ? vx[i] : u32x4{};
+            if (piece_i % SL == 0) missing[kr] = at[i] < 0;
         }
         __syncthreads();
-        if (t0 + KT < to) fetch(t0 + KT);
+        if (t0 + KT < to) {
+            fetch();
+            rows_of(t0 + 2 * KT);
+        }
         again();
         // scores: lane (h, n) holds keys 32 kt + 8 (r / 4) + 4 h + r % 4 of query n
         f32x16 s[KK];
@@ -378,11 +400,7 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
             }
         }
         float top = -INFINITY;
-        const uint64_t none = invalid_s;
-#pragma unroll
-        for (int kt = 0; kt < KK; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] *= a.scale;
+        const uint64_t none = __ballot(missing[lane % KT] != 0);
         if (none) {
 #pragma unroll
             for (int kt = 0; kt < KK; ++kt)
@@ -394,7 +412,7 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
         for (int kt = 0; kt < KK; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kt][r]);
-        top = swap_max32(top);
+        top = swap_max32(top) * scale;
         if (__any(!(top <= base + 6.0f)) || m == -INFINITY) {
             const float to_m = fmaxf(m, top), nb = to_m == -INFINITY ? 0.0f : to_m, f = __builtin_amdgcn_exp2f(m == -INFINITY ? m : base - nb);
             l *= f;
@@ -408,7 +426,8 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
         for (int kt = 0; kt < KK; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const f32x2 e = {__builtin_amdgcn_exp2f(s[kt][r] - base), __builtin_amdgcn_exp2f(s[kt][r + 1] - base)};
+                const f32x2 e = {__builtin_amdgcn_exp2f(fmaf(s[kt][r], scale, -base)),
+                                 __builtin_amdgcn_exp2f(fmaf(s[kt][r + 1], scale, -base))};
                 l += e[0] + e[1];
                 const bf16x2 w = __builtin_convertvector(e, bf16x2);
                 p[2 * kt + r / 8][r % 8] = w[0], p[2 * kt + r / 8][r % 8 + 1] = w[1];
