@@ -326,8 +326,11 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
     const int hk = piece % a.Hkv, part = piece / a.Hkv;
     const int len = static_cast<int>(a.prefix), step = ((len + a.prefix_parts - 1) / a.prefix_parts + KT - 1) / KT * KT;
     const int from = min(len, part * step), to = min(len, from + step);
-    const int row = tile * 256 + wave * 32 + n, rr = min(row, rows - 1), b = rr / a.G;
-    const size_t qrow = static_cast<size_t>(b) * a.Hq + hk * a.G + (rr - b * a.G);
+    const auto query_row = [&](int row) {
+        const int b = row / a.G;
+        return static_cast<size_t>(b) * a.Hq + hk * a.G + (row - b * a.G);
+    };
+    const size_t qrow = query_row(min(tile * 256 + wave * 32 + n, rows - 1));
     // operand B: query n, elements 16 kb + 8 h .. + 7
     bf16x8 q[KB];
 #pragma unroll
@@ -450,8 +453,10 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
             }
     }
     l = swap_add32(l);
+    again();
+    const int row = tile * 256 + wave * 32 + n;
     if (row < rows) {
-        const size_t at = part * (static_cast<size_t>(a.batch) * a.Hq) + qrow;
+        const size_t at = part * (static_cast<size_t>(a.batch) * a.Hq) + query_row(row);
         if (h == 0) a.ml[at] = make_float2(m == -INFINITY ? m : base, l);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)

@@ -263,12 +263,12 @@ __device__ __forceinline__ uint32_t max_of(const Act<bf16_t> (&v)[N])
 template <int N>
 __device__ __forceinline__ uint32_t max_of(const Act<float> (&v)[N])
 {
-    float m = 0.0f;
+    uint32_t m = 0;                          // as integers, in which a NaN is above all
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[i].x[e / 4][e % 4]));
-    return __float_as_uint(m);
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(fabsf(v[i].x[e / 4][e % 4])));
+    return m;
 }
 // the same without what is not finite
 constexpr uint32_t kInfBits = 0x7f800000u;
@@ -285,11 +285,25 @@ __device__ __forceinline__ uint32_t finite_max8(uint32_t m, const Act<T> &v)
     }
     return m;
 }
-// of a thread's N units, over its wave
+template <typename T>
+__device__ __forceinline__ bool all_finite(const Act<T> &v)
+{
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float a;
+        if constexpr (sizeof(T) == 2) a = i % 2 ? upper_bf16(v.x[i / 2]) : lower_bf16(v.x[i / 2]);
+        else a = v.x[i / 4][i % 4];
+        ok &= fabsf(a) < INFINITY;
+    }
+    return ok;
+}
+// of a thread's N units, over its wave; *fine: all are finite
 template <int N, typename T>
-__device__ __forceinline__ uint32_t wave_max_of(const Act<T> (&v)[N])
+__device__ __forceinline__ uint32_t wave_max_of(const Act<T> (&v)[N], bool *fine = nullptr)
 {
     uint32_t w = wave_max(max_of(v));
+    if (fine) *fine = w < kInfBits;
     if (w >= kInfBits) {
         uint32_t m = 0;
 #pragma unroll
@@ -477,11 +491,17 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
 //   T_wc = -T_ww sum_{c <= l < w} M_wl T_lc
 // in fp32 products, the blocks at equal distance from the diagonal together.
 template <typename T, int DKP, bool VEC>
-__global__ __launch_bounds__(256) void prompt_solve_kernel(ChunkArgs a)
+__global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prompt_solve_kernel(ChunkArgs a)
 {
     constexpr int NA = Act<T>::planes, U = DKP / 32, LD = 68;
-    __shared__ RowTile<T, DKP> K;
-    __shared__ alignas(16) float M[kC][LD], X[kC][LD];
+    // the keys are not needed once M is formed: the inverse takes their place
+    __shared__ union Place {
+        RowTile<T, DKP> K;
+        alignas(16) float X[kC][LD];
+    } place;
+    __shared__ alignas(16) float M[kC][LD];
+    RowTile<T, DKP> &K = place.K;
+    auto &X = place.X;
     __shared__ double lgs[kC];
     __shared__ float bs[kC];
     __shared__ int bad_s;
@@ -500,28 +520,25 @@ __global__ __launch_bounds__(256) void prompt_solve_kernel(ChunkArgs a)
     for (int i = 0; i < U; ++i) {
         v[i] = sh.template load<VEC>(static_cast<const T *>(a.p.k) + t0 * a.p.sk + hq * a.p.dk, a.p.sk, i, a.p.dk, len);
     }
-    float beta;
-    bool fine;
-    const double lg = scan_gates(a.p, t0, len, h, lane, &beta, &fine);
+    // the gates' products: one wave's work
+    float beta = 0.0f;
+    bool fine = true;
+    double lg = 0.0;
+    if (w == 0) lg = scan_gates(a.p, t0, len, h, lane, &beta, &fine);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         if constexpr (!VEC) v[i] = settle(v[i], 8 * sh.c8, a.p.dk);
         v[i] = zero_unless(sh.valid(i, a.p.dk, len), v[i]);
     }
-    kmax_s[w] = wave_max_of(v);
+    bool keys_fine;
+    kmax_s[w] = wave_max_of(v, &keys_fine);
     __syncthreads();
     const Pow2 sk = scale_for(max(max(kmax_s[0], kmax_s[1]), max(kmax_s[2], kmax_s[3])));
     if (!fine) atomicMin(&bad_s, lane);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int row = sh.row + sh.step * i;
-        float z = 0.0f;                       // 0 x stays 0 for finite x alone
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (NA == 1) z = fmaf(lower_bf16(v[i].x[e]), 0.0f, fmaf(upper_bf16(v[i].x[e]), 0.0f, z));
-            else z = fmaf(v[i].x[0][e], 0.0f, fmaf(v[i].x[1][e], 0.0f, z));
-        }
-        if (z != 0.0f) atomicMin(&bad_s, row);
+        if (!keys_fine && !all_finite(v[i])) atomicMin(&bad_s, row);
         K.put(row, sh.c8, v[i], sk.up);
     }
     if (w == 0) lgs[lane] = lg, bs[lane] = beta;
@@ -557,6 +574,7 @@ __global__ __launch_bounds__(256) void prompt_solve_kernel(ChunkArgs a)
         float t[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
+            if (i % 8 == 0) __builtin_amdgcn_sched_barrier(0);     // half of the rows of M in registers at a time
             float y = i == n ? 1.0f : 0.0f;
 #pragma unroll
             for (int l = 0; l < i; ++l) y = fmaf(-M[16 * w + i][16 * w + l], t[l], y);
