@@ -302,14 +302,29 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnAr
 // running maximum follows only when it is passed by 2^6, so that the outputs
 // are rescaled a few times in all.  The weights are rounded to bfloat16 once,
 // as the output is; their sum is taken before.
+// The order of N products and the LDS reads of their operands, R each: A operands are read ahead.
+template <int N, int R, int A>
+__device__ __forceinline__ void reads_ahead()
+{
+    constexpr int product = 0x8, read = 0x100;
+    __builtin_amdgcn_sched_group_barrier(read, R * A, 0);
+#pragma unroll
+    for (int i = 0; i < N - A; ++i) {
+        __builtin_amdgcn_sched_group_barrier(product, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(read, R, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(product, A, 0);
+}
+
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
 {
     constexpr int KT = D == 256 ? 32 : 64;            // as many as the registers of 2 waves per SIMD allow
     constexpr int KK = KT / 32, RB = 2 * D, SL = RB / 16, L = KT * SL / 512, KB = D / 16, DT = D / 32;
-    constexpr int SW = SL < 16 ? 128 : 256;
-    __shared__ alignas(16) uint8_t ks[KT * RB], vs[KT * RB];
-    __shared__ uint8_t missing[KT];
+    // rows in LDS: 16 keys one 16-byte slot apart, and 4 rows of values read by columns 64 bytes apart, fill the banks
+    constexpr int KR = RB + 16, VR = RB + 64;
+    __shared__ alignas(16) uint8_t ks[2][KT * KR], vs[2][KT * VR];
+    __shared__ uint8_t missing[3][KT];                // of tile t in t % 3: written two tiles ahead
     int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int lane = tid & 63, h = lane >> 5, n = lane & 31;
@@ -346,50 +361,57 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
             q[kb] = __builtin_bit_cast(bf16x8, a.scale == 0.0f ? u32x4{} : w ^ 0x80008000u);
         }
     }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(q[kb]));   // there before the loop: nothing in it waits for them
     const uint8_t *K = static_cast<const uint8_t *>(a.k), *V = static_cast<const uint8_t *>(a.v);
-    // a thread's 16-byte pieces of the next tile, on their way; and the cache rows
-    // of those of the tile after it, so that no load waits for a page id
+    // a thread's 16-byte pieces of the next tile, on their way with the page ids of the tile after it
     u32x4 kx[L], vx[L];
-    int at[L], ahead[L];
-    const auto rows_of = [&](int t0) {
+    int id[L];
+    uint64_t gone[L];            // lanes whose key there is not: their values are made 0
+    const auto token = [&](int i) { return (i * 512 + tid) / SL; };
+    const auto ids_of = [&](int t0) {
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-            const int t = t0 + (i * 512 + tid) / SL;
-            ahead[i] = token_row(a, a.prefix_pages, t, hk, t < to);
-        }
+        for (int i = 0; i < L; ++i) id[i] = a.prefix_pages[fdiv(min(t0 + token(i), to - 1), a.div_page)];
     };
-    const auto fetch = [&] {
+    const auto fetch = [&](int t0, int ring) {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            at[i] = ahead[i];
-            const size_t from_byte = static_cast<size_t>(max(at[i], 0)) * RB + (i * 512 + tid) % SL * 16;
+            const int t = t0 + token(i), slot = (i * 512 + tid) % SL;
+            const bool there = t < to && id[i] >= 0 && id[i] < a.n_pages;
+            const int row = there ? (id[i] * a.Hkv + hk) * a.page + t - fdiv(t, a.div_page) * a.page : 0;
+            const size_t from_byte = static_cast<size_t>(row) * RB + slot * 16;
             kx[i] = *reinterpret_cast<const u32x4 *>(K + from_byte);
             vx[i] = *reinterpret_cast<const u32x4 *>(V + from_byte);
+            gone[i] = __ballot(!there);
+            if (slot == 0) missing[ring][token(i)] = !there;
+        }
+    };
+    const auto store = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            if (gone[i] && (gone[i] >> lane & 1)) vx[i] = u32x4{};
+            const int kr = token(i), slot = (i * 512 + tid) % SL;
+            *reinterpret_cast<u32x4 *>(ks[buf] + kr * KR + slot * 16) = kx[i];
+            *reinterpret_cast<u32x4 *>(vs[buf] + kr * VR + slot * 16) = vx[i];
         }
     };
     f32x16 acc[DT] = {};
     float m = -INFINITY, base = 0.0f, l = 0.0f;
     if (from < to) {
-        rows_of(from);
-        fetch();
-        rows_of(from + KT);
+        ids_of(from);
+        fetch(from, 0);
+        ids_of(from + KT);
+        store(0);
+        if (from + KT < to) {
+            fetch(from + KT, 1);
+            ids_of(from + 2 * KT);
+        }
     }
-    for (int t0 = from; t0 < to; t0 += KT) {
-        __syncthreads();
+    int buf = 0, ring = 0;
+    for (int t0 = from; t0 < to; t0 += KT, buf ^= 1, ring = ring == 2 ? 0 : ring + 1) {
+        lds_barrier();
         again();
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-            const int piece_i = i * 512 + tid, kr = piece_i / SL, to_byte = kr * RB + ((piece_i % SL ^ swizzle<SW>(kr)) * 16);
-            *reinterpret_cast<u32x4 *>(ks + to_byte) = kx[i];
-            *reinterpret_cast<u32x4 *>(vs + to_byte) = at[i] >= 0 ? vx[i] : u32x4{};
-            if (piece_i % SL == 0) missing[kr] = at[i] < 0;
-        }
-        __syncthreads();
-        if (t0 + KT < to) {
-            fetch();
-            rows_of(t0 + 2 * KT);
-        }
-        again();
+        const uint8_t *kb0 = ks[buf] + n * KR + h * 16;
         // scores: lane (h, n) holds keys 32 kt + 8 (r / 4) + 4 h + r % 4 of query n
         f32x16 s[KK];
 #pragma unroll
@@ -397,13 +419,13 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
             s[kt] = f32x16{};
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const int kr = 32 * kt + n;
-                const bf16x8 k = *reinterpret_cast<const bf16x8 *>(ks + kr * RB + (((2 * kb + h) ^ swizzle<SW>(kr)) * 16));
+                const bf16x8 k = *reinterpret_cast<const bf16x8 *>(kb0 + 32 * kt * KR + kb * 32);
                 s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kb], s[kt], 0, 0, 0);
             }
         }
+        reads_ahead<KK * KB, 1, 3>();
         float top = -INFINITY;
-        const uint64_t none = __ballot(missing[lane % KT] != 0);
+        const uint64_t none = __ballot(missing[ring][lane % KT] != 0);
         if (none) {
 #pragma unroll
             for (int kt = 0; kt < KK; ++kt)
@@ -435,7 +457,19 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
                 const bf16x2 w = __builtin_convertvector(e, bf16x2);
                 p[2 * kt + r / 8][r % 8] = w[0], p[2 * kt + r / 8][r % 8 + 1] = w[1];
             }
+#pragma unroll
+        for (int i = 0; i < 2 * KK; ++i) asm volatile("" : "+v"(p[i]));   // formed here, not after the next tile's loads
+        if (t0 + KT < to) {
+            again();
+            store(buf ^ 1);
+            if (t0 + 2 * KT < to) {
+                again();
+                fetch(t0 + 2 * KT, ring == 0 ? 2 : ring - 1);
+                ids_of(t0 + 3 * KT);
+            }
+        }
         again();
+        const uint8_t *vb0 = vs[buf] + (4 * h + (lane & 15) / 4) * VR + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
         // O^T += V^T P: summation slot 8 h + 4 u + j of a block of 16 keys is key 8 u + 4 h + j
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -444,13 +478,12 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
                 u32x4 w;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int ln = lane & 15, kr = 16 * kb + 8 * u + 4 * h + (ln >> 2);
-                    const int slot = 4 * dt + 2 * ((lane >> 4) & 1) + ((ln & 3) >> 1);
-                    const u32x2 y = read_columns(vs + kr * RB + ((slot ^ swizzle<SW>(kr)) * 16) + 8 * (ln & 1));
+                    const u32x2 y = read_columns(vb0 + (16 * kb + 8 * u) * VR + dt * 64);
                     w[2 * u] = y[0], w[2 * u + 1] = y[1];
                 }
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p[kb], acc[dt], 0, 0, 0);
             }
+        reads_ahead<DT * 2 * KK, 2, 2>();
     }
     l = swap_add32(l);
     again();
@@ -606,6 +639,8 @@ extern "C" stepq_status stepq_prefix_attention(const stepq_attn_desc *d, const v
     const size_t rows = static_cast<size_t>(d->batch) * d->n_q_heads;
     AttnArgs a{};
     a.q = q, a.k = k_cache, a.v = v_cache;
+    // what is not there is read as row 0 and left out; without a page, the queries stand in for that row
+    if (d->n_pages == 0) a.k = a.v = q;
     a.prefix_pages = prefix_pages, a.table = page_table, a.lengths = lengths;
     a.o = o, a.lse = lse;
     a.acc = static_cast<float *>(workspace);
