@@ -302,20 +302,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnAr
 // running maximum follows only when it is passed by 2^6, so that the outputs
 // are rescaled a few times in all.  The weights are rounded to bfloat16 once,
 // as the output is; their sum is taken before.
-// The order of N products and the LDS reads of their operands, R each: A operands are read ahead.
-template <int N, int R, int A>
-__device__ __forceinline__ void reads_ahead()
-{
-    constexpr int product = 0x8, read = 0x100;
-    __builtin_amdgcn_sched_group_barrier(read, R * A, 0);
-#pragma unroll
-    for (int i = 0; i < N - A; ++i) {
-        __builtin_amdgcn_sched_group_barrier(product, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(read, R, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(product, A, 0);
-}
-
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
 {
@@ -423,7 +409,7 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
                 s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kb], s[kt], 0, 0, 0);
             }
         }
-        reads_ahead<KK * KB, 1, 3>();
+        reads_ahead<KK * KB, 1, 1, 3>();
         float top = -INFINITY;
         const uint64_t none = __ballot(missing[ring][lane % KT] != 0);
         if (none) {
@@ -483,7 +469,7 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
                 }
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p[kb], acc[dt], 0, 0, 0);
             }
-        reads_ahead<DT * 2 * KK, 2, 2>();
+        reads_ahead<DT * 2 * KK, 2, 1, 2>();
     }
     l = swap_add32(l);
     again();

@@ -99,6 +99,20 @@ __device__ __forceinline__ u32x2 read_columns(const uint8_t *lds)
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds)));
 }
 
+// The order of N steps of M products and the R reads of LDS that each needs: A steps are read ahead.
+template <int N, int R, int M, int A>
+__device__ __forceinline__ void reads_ahead()
+{
+    constexpr int product = 0x8, read = 0x100;
+    __builtin_amdgcn_sched_group_barrier(read, R * A, 0);
+#pragma unroll
+    for (int i = 0; i < N - A; ++i) {
+        __builtin_amdgcn_sched_group_barrier(product, M, 0);
+        __builtin_amdgcn_sched_group_barrier(read, R, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(product, M * A, 0);
+}
+
 // A barrier that orders the waves' LDS accesses, and does not wait for copies and other global accesses under way.
 __device__ __forceinline__ void lds_barrier()
 {

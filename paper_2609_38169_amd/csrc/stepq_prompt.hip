@@ -47,7 +47,7 @@ struct ChunkGates {
 };
 static_assert(sizeof(ChunkGates) == 1408, "record size");
 constexpr size_t kTBytes = 2 * 6 * 1024;
-constexpr int kGateWords = 5 * kC;       // lg, g, w, b
+constexpr int kGateWords = 5 * kC + 2;   // lg, g, w, b, bad, tmax
 
 struct ChunkArgs {
     PromptArgs p;
@@ -695,6 +695,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     __shared__ struct alignas(16) {
         double lg[kC];
         float g[kC], w[kC], b[kC];
+        int32_t bad;
+        uint32_t tmax;
     } ga;
     __shared__ uint32_t tops[2][NW];
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -808,13 +810,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         if constexpr (OUT) tops[1][wv] = wave_max_of(qx);
         lds_barrier();
         const ChunkGates *cg = reinterpret_cast<const ChunkGates *>(record(c));
-        int bad = kC;
-        uint32_t tmax = 0;
         if constexpr (DELTA) {
             const f16x8 *from = reinterpret_cast<const f16x8 *>(cg + 1) + lane;
 #pragma unroll
             for (int i = 0; i < NP; ++i) tx[i] = from[(wv + NW * i) % 12 * 64];
-            bad = cg->bad, tmax = cg->tmax;
         }
         uint32_t mk = 0, mq = 0;
 #pragma unroll
@@ -837,6 +836,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
             reinterpret_cast<uint32_t *>(&ga)[min(static_cast<int>(threadIdx.x) + 64 * NW * i, kGateWords - 1)] = gx[i];
         lds_barrier();
         if (c + 1 < chunks) fetch(c + 1);
+        const int bad = DELTA ? __builtin_amdgcn_readfirstlane(ga.bad) : kC;
 
         again();
         // P times 2^-22 of the scales (|q.k| < 2^35 scaled), a block of 16 rows x 32 columns to a wave:
@@ -900,6 +900,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
                 }
             }
         }
+        // 3 steps' operands ahead (32 sequences: 537 -> 530 us); the update of S the same way is slower (541)
+        if constexpr (OUT && DELTA && sizeof(T) == 2) reads_ahead<4 * KB, 2, 4, 3>();
         again();
         // R (Delta) or U (decay), and whether it is finite; O's part from the state
         float z = 0.0f;
@@ -946,7 +948,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         float fu = 1.0f;
         if constexpr (DELTA) {
             const Pow2 sr = scale_for(column_max(tile_max(ks)));
-            const Pow2 st = scale_for(tmax);
+            const Pow2 st = scale_for(ga.tmax);
             fu = st.down * sr.down;
             f16x8 rp[2][2];
 #pragma unroll
