@@ -323,7 +323,10 @@ stepq_status stepq_pool_import_pivots(stepq_pool *pool, const int32_t *slot_ids,
  * attention over a shared prefix.  The same conventions as above; these calls
  * need no pool.  Workspaces are caller-owned device memory, 256-byte aligned,
  * of at least the size the *_workspace call gives (host only, no device work);
- * a workspace may be used again as soon as the stream has passed the call.
+ * a workspace may be used again as soon as the stream has passed the call.  One
+ * call takes fewer than 2^23 (64-token chunk, head) pairs of prompts, fewer than
+ * 2^24 (request, head) states, and at most 2^23 (request, head) rows of
+ * attention.
  */
 
 /* The recurrence of one (sequence, value head), state S in R^{d_k x d_v}. */

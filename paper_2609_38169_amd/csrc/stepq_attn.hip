@@ -528,8 +528,8 @@ stepq_status check(const stepq_attn_desc *d)
     if (!std::isfinite(d->scale)) return bad("scale must be finite");
     if (d->prefix_len >= (int64_t(1) << 30) || static_cast<int64_t>(d->max_pages) * d->page_size >= (int64_t(1) << 30))
         return set_error(STEPQ_E_UNSUPPORTED, "2^30 tokens or more in the prefix or a request's pages");
-    if (static_cast<int64_t>(d->batch) * d->n_q_heads > (int64_t(1) << 24))
-        return set_error(STEPQ_E_UNSUPPORTED, "more than 2^24 (request, head) rows in one call: split the batch");
+    if (static_cast<int64_t>(d->batch) * d->n_q_heads > (int64_t(1) << 23))      // a launch has less than 2^32 threads
+        return set_error(STEPQ_E_UNSUPPORTED, "more than 2^23 (request, head) rows in one call: split the batch");
     if (static_cast<double>(d->n_pages) * d->n_kv_heads * d->page_size >= 2147483648.0)
         return set_error(STEPQ_E_UNSUPPORTED, "2^31 rows or more in a cache");
     return STEPQ_OK;

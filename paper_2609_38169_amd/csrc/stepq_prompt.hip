@@ -672,7 +672,8 @@ __device__ __forceinline__ uint32_t tile_max(const f32x4 (&x)[4])
 // whatever S is, so that: a launch forms B of every segment by walking it from
 // a zero state, and for the Delta rule A by walking it from the identity with
 // all values zero; one applies them in order (prompt_join kernels), leaving the
-// state after each segment in B's place; and then all segments are walked at once.
+// state after each segment in B's place (the last one has no B: there, the state
+// before the first); and then all segments are walked at once.
 constexpr int kSegmentHead = 64;         // floats; [0] = gamma
 
 // Second launch: a workgroup of NW waves walks the chunks of one (sequence, head)
@@ -726,7 +727,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
     for (int rt = 0; rt < DKP / 16; ++rt) S[rt] = f32x4{};
     if constexpr (OUT) {
-        const float *from = part == 0 ? initial_state(a.p, s, h) : rec - a.p.Hv * a.seg_floats + kSegmentHead;
+        // the first of several segments has its state from the last one's record: state_out may be state_in
+        const int64_t back = part == 0 && a.seg ? (total + a.seg - 1) / a.seg - 1 : -1;
+        const float *from = part == 0 && back <= 0 ? initial_state(a.p, s, h)
+                                                   : rec + back * a.p.Hv * static_cast<int64_t>(a.seg_floats) + kSegmentHead;
         if (from)
             each_state_row<DKP>(from + col0 + mycol, a.p.dk, a.p.dv, g, n,
                                 [&](const float *at, int rt, int r) { S[rt][r] = *at; });
@@ -1060,13 +1064,14 @@ __global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
     const int h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv, e = blockIdx.x % blocks * 256 + threadIdx.x;
     const int2 be = seq_bounds(a.p, s);
     const int total = (be.y - be.x + kC - 1) / kC, parts = (total + a.seg - 1) / a.seg;
-    if (e >= quads) return;
+    if (e >= quads || parts < 2) return;
     const float *from = initial_state(a.p, s, h);
     f32x4 S = {};
     if (from)
 #pragma unroll
         for (int i = 0; i < 4; ++i) S[i] = from[4 * e + i];
     float *rec = a.segs + (static_cast<size_t>(first_slot(a.p, s, kC * a.seg)) * a.p.Hv + h) * a.seg_floats;
+    reinterpret_cast<f32x4 *>(rec + (parts - 1) * (a.p.Hv * a.seg_floats) + kSegmentHead)[e] = S;
     for (int j = 0; j + 1 < parts; ++j, rec += a.p.Hv * a.seg_floats) {
         f32x4 *B = reinterpret_cast<f32x4 *>(rec + kSegmentHead) + e;
         S = *B + S * rec[0];
@@ -1088,6 +1093,8 @@ __global__ __launch_bounds__(256) void prompt_join_delta_kernel(ChunkArgs a)
     const int2 be = seq_bounds(a.p, s);
     const int total = (be.y - be.x + kC - 1) / kC, parts = (total + a.seg - 1) / a.seg;
     if (parts < 2) return;
+    const size_t step = a.p.Hv * a.seg_floats;
+    float *rec = a.segs + (static_cast<size_t>(first_slot(a.p, s, kC * a.seg)) * a.p.Hv + h) * a.seg_floats;
     const float *from = initial_state(a.p, s, h);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -1096,11 +1103,10 @@ __global__ __launch_bounds__(256) void prompt_join_delta_kernel(ChunkArgs a)
         for (int r = 0; r < 4; ++r) {
             const int i = row0 + 16 * rt + r;
             x[r] = from && i < a.p.dk ? from[i * a.p.dv + col] : 0.0f;
+            if (i < a.p.dk) rec[(parts - 1) * step + kSegmentHead + i * a.p.dv + col] = x[r];
         }
         *reinterpret_cast<f32x4 *>(&st[0][n * LD + row0 + 16 * rt]) = x;
     }
-    const size_t step = a.p.Hv * a.seg_floats;
-    float *rec = a.segs + (static_cast<size_t>(first_slot(a.p, s, kC * a.seg)) * a.p.Hv + h) * a.seg_floats;
     f32x4 x[RT][KT], y[RT];
     const auto fetch = [&](const float *at) {
         const f32x4 *A = reinterpret_cast<const f32x4 *>(at + kSegmentHead + a.p.dk * a.p.dv) + (16 * RT * wv + n) * (DKP / 4) + g;
@@ -1196,8 +1202,9 @@ stepq_status check(const stepq_prompt_desc *d)
     // the kernels' offsets within a wave's rows are 32-bit
     if (std::max({d->q_stride, d->k_stride, d->v_stride, d->o_stride, qk, vo}) > (int64_t(1) << 26))
         return set_error(STEPQ_E_UNSUPPORTED, "tokens more than 2^26 elements apart");
-    if (slots(d) * d->n_v_heads >= (int64_t(1) << 31))
-        return set_error(STEPQ_E_UNSUPPORTED, "2^31 (chunk, head) pairs or more in one call: split the batch");
+    // (a launch has less than 2^32 threads)
+    if (slots(d) * d->n_v_heads >= (int64_t(1) << 23))
+        return set_error(STEPQ_E_UNSUPPORTED, "2^23 (chunk, head) pairs or more in one call: split the batch");
     return STEPQ_OK;
 }
 

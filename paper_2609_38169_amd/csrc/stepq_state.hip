@@ -144,8 +144,8 @@ extern "C" stepq_status stepq_state_step(const stepq_state_desc *d, float *state
     if (d->rule != STEPQ_RULE_DECAY && d->rule != STEPQ_RULE_DELTA) return bad("unknown rule");
     if (d->n_states < 0 || batch < 0) return bad("negative count");
     if (batch > d->n_states) return bad("more requests than states");
-    if (static_cast<int64_t>(batch) * d->n_v_heads > (int64_t(1) << 24))
-        return set_error(STEPQ_E_UNSUPPORTED, "more than 2^24 (request, head) tiles in one call: split the batch");
+    if (static_cast<int64_t>(batch) * d->n_v_heads >= (int64_t(1) << 24))        // a launch has less than 2^32 threads
+        return set_error(STEPQ_E_UNSUPPORTED, "2^24 or more (request, head) tiles in one call: split the batch");
     if (batch == 0) return STEPQ_OK;
     if (!state || !ids || !q || !k || !v || !alpha || !o) return bad("NULL state, ids, activation or output pointer");
     if (!aligned(state, 16) || !aligned(o, 16)) return bad("state and o must be 16-byte aligned");
