@@ -239,6 +239,16 @@ def test_offsets_over_32_bits():
     assert ((o.cpu().double() - ro).abs() <= 2.0 ** -8 * size + 2.0 ** -9 * ro.abs()).all()
 
 
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("B", [2, 40])
+def test_caches_without_a_page(act, B):
+    """No page at all, yet page ids and lengths that ask for some: every row is empty."""
+    x = list(inputs(B, 4, 2, 64, 40, [9] * B, 16, act))
+    x[1], x[2] = x[1][:0], x[2][:0]
+    o, lse = call(tuple(x))
+    assert not o.any() and (lse == -math.inf).all()
+
+
 def test_refusals():
     q, k, v, pre, prefix, table, lengths = (t.to(DEV) if isinstance(t, torch.Tensor) else t
                                             for t in inputs(2, 4, 2, 64, 40, [5, 6], 16, BF16))
