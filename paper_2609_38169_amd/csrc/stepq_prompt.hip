@@ -59,6 +59,7 @@ struct ChunkArgs {
     float *segs;             // per (segment, head): SegmentHead, B or the state after it [dk][dv], A [DKP][DKP] (Delta)
     size_t seg_floats;
     int32_t near;            // 64 tokens of q, k and v lie within 2^32 bytes
+    int32_t *order;          // [n_seq] sequences, longest first; NULL: they are walked in their own order
 };
 
 __device__ __forceinline__ int2 seq_bounds(const PromptArgs &a, int s)
@@ -468,6 +469,22 @@ __device__ __forceinline__ void put_gates(ChunkGates *r, int lane, double lg, fl
     if (lane == 0) r->bad = bad;
 }
 
+// A wave puts sequence s in its place among the sequences, longest first.
+__device__ __forceinline__ void put_order(const ChunkArgs &a, int s, int lane)
+{
+    const int2 be = seq_bounds(a.p, s);
+    const int len = be.y - be.x;
+    int before = 0;
+    for (int t = lane; t < a.p.n_seq; t += 64) {
+        const int2 other = seq_bounds(a.p, t);
+        const int d = other.y - other.x - len;
+        before += d > 0 || (d == 0 && t < s);
+    }
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) before += __shfl_xor(before, m);
+    if (lane == 0) a.order[before] = s;
+}
+
 // First launch, decay rule: a wave per (chunk, head).
 __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
 {
@@ -475,6 +492,7 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
     const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int x = static_cast<int>(id / a.p.Hv), h = static_cast<int>(id - static_cast<int64_t>(x) * a.p.Hv);
     if (x >= a.slots) return;
+    if (a.order && x < a.p.n_seq && h == 0) put_order(a, x, lane);       // there are at least as many slots
     const int s = owner(a.p, x, lane);
     const int2 be = seq_bounds(a.p, s);
     const int t0 = be.x + (x - first_slot(a.p, s)) * kC, n = min(kC, be.y - t0);
@@ -509,6 +527,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, n = lane & 15;
     const Share<DKP / 8, 256> sh(tid);
     const int x = blockIdx.x / a.p.Hv, h = blockIdx.x - x * a.p.Hv, hq = h / (a.p.Hv / a.p.Hqk);
+    if (a.order && x < a.p.n_seq && h == 0 && w == 0) put_order(a, x, lane);     // there are at least as many slots
     const int s = owner(a.p, x, lane);
     const int2 be = seq_bounds(a.p, s);
     const int64_t t0 = be.x + (x - first_slot(a.p, s)) * kC;
@@ -714,7 +733,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     const int hq = h / (a.p.Hv / a.p.Hqk);
     const bool values = OUT || !DELTA || cb < value_blocks;      // B; else A
     const int col0 = (values ? cb : cb - value_blocks) * W, mycol = wv * 16;
-    const int s = a.seg ? owner(a.p, item, lane, kC * a.seg) : item;
+    const int s = a.seg ? owner(a.p, item, lane, kC * a.seg)
+                        : a.order ? a.order[item] : item;
     const int2 be = seq_bounds(a.p, s);
     const int total = (be.y - be.x + kC - 1) / kC, part = a.seg ? item - first_slot(a.p, s, kC * a.seg) : 0;
     const int first = part * a.seg, chunks = a.seg ? min(total, first + a.seg) : total;
@@ -1227,7 +1247,7 @@ size_t record_bytes(const stepq_prompt_desc *d)
 struct Layout {              // of the workspace
     size_t record, chunks;   // bytes per (chunk, head), of all
     int32_t seg, seg_slots;
-    size_t seg_floats, bytes;
+    size_t seg_floats, order, bytes;   // order: its place, 0 without one
 };
 
 Layout layout_of(const stepq_prompt_desc *d)
@@ -1242,6 +1262,12 @@ Layout layout_of(const stepq_prompt_desc *d)
         l.seg_floats = kSegmentHead + (size_t(d->d_k) * d->d_v + (d->rule == STEPQ_RULE_DELTA ? dkp * dkp : 0) + 63) / 64 * 64;
     }
     l.bytes = l.chunks + static_cast<size_t>(l.seg_slots) * d->n_v_heads * l.seg_floats * sizeof(float);
+    // More walks than CUs are begun longest first, or the chip waits for long ones that were begun late.  Of very
+    // many sequences the last ones are a small part, and counting who is longer is not.
+    if (!l.seg && d->n_seq > 1 && d->n_seq <= 4096 && int64_t(d->n_seq) * d->n_v_heads > 256) {
+        l.order = l.bytes;
+        l.bytes += (static_cast<size_t>(d->n_seq) * sizeof(int32_t) + 255) / 256 * 256;
+    }
     return l;
 }
 
@@ -1287,6 +1313,7 @@ extern "C" stepq_status stepq_prompt(const stepq_prompt_desc *d, const int32_t *
     a.near = std::max({a.p.sq, a.p.sk, a.p.sv}) <= (int64_t(1) << 23);
     a.seg = l.seg, a.seg_slots = l.seg_slots, a.seg_floats = l.seg_floats;
     a.segs = reinterpret_cast<float *>(a.ws + l.chunks);
+    a.order = l.order ? reinterpret_cast<int32_t *>(a.ws + l.order) : nullptr;
     const int e = d->act_dtype == STEPQ_BF16 ? 8 : 4;   // elements in 16 bytes
     const bool vec = d->d_k % 8 == 0 && (a.p.sq | a.p.sk | a.p.sv) % e == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16);
     const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -116,6 +116,26 @@ def test_many_sequences(rule):
 
 
 @pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_many_sequences_of_several_heads(rule):
+    """Enough walks for an order of their own: equal lengths, empty sequences, one far longer."""
+    check([(37 * i) % 130 if i % 5 else 64 for i in range(140)] + [700, 0], 2, 1, 64, 64, BF16, F32, rule, start="own")
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+def test_many_malformed_bounds(rule):
+    """Bounds that go down or past the tokens, and more walks than an order needs: every sequence is settled."""
+    n = 300
+    q, k, v, alpha, beta = (x.to(DEV) for x in tokens(100, 1, 1, 64, 64, BF16, F32, 2))
+    o, out = torch.zeros((100, 1, 64), dtype=BF16, device=DEV), torch.full((n, 1, 64, 64), 7.0, device=DEV)
+    cu = torch.tensor([(61 * i) % 140 - 10 for i in range(n + 1)], dtype=torch.int32)
+    stepq.stepq_prompt(q, k, v, alpha, beta, o, out, rule, cu_seqlens=cu.to(DEV))
+    torch.cuda.synchronize()
+    at = cu.clamp(0, 100)
+    empty = (at[1:] <= at[:-1]).to(DEV)
+    assert empty.any() and not out[empty].any()
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
 def test_long(rule):
     check([5000, 2500], 1, 1, 64, 64, BF16, F32, rule, low=0.99)
 
