@@ -87,7 +87,10 @@ struct Running {
 // range of the prefix) and its waves take key tiles in turn.  Scores are formed
 // transposed, keys x queries, so that a query's weights lie in one lane group
 // and go into the second product as they are; values pass through LDS of the
-// wave's own to be read by columns.  Bound by the bytes of the caches.
+// wave's own to be read by columns.  Bound by the bytes of the caches: 64
+// requests x 8 key/value heads x 1024 tokens of 128 bfloat16 (268 MB) in 29-31 us,
+// of which the last-level cache serves a part; 512 x 2 x 256 of 256 (268 MB) in
+// 52 us, 5.2 TB/s.  4 requests over 512 + 64 tokens: 8 us, latency.
 template <typename T>
 struct Tile;
 template <>
@@ -297,11 +300,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnAr
 // ---------------------------------------------------------------------------
 // Many queries per key: the prefix of a large batch, a matrix product.  A
 // workgroup takes 256 query rows (32 to a wave, their queries in registers) and
-// a range of the prefix, 64 (D = 256: 32) keys at a time in LDS; the next ones are
-// on their way in registers meanwhile.  Scores transposed as above, in 32x32 blocks.  The
-// running maximum follows only when it is passed by 2^6, so that the outputs
-// are rescaled a few times in all.  The weights are rounded to bfloat16 once,
-// as the output is; their sum is taken before.
+// a range of the prefix, 64 (D = 256: 32) keys at a time, in two LDS buffers by
+// turns, so that a tile costs one barrier and waves may be a tile's phase apart;
+// the tile after the next is on its way in registers, with the page ids of the
+// one after that: nothing waits for a load of its own tile.  Rows in LDS are
+// padded, which makes every address a lane's base and a constant.  Scores
+// transposed as above, in 32x32 blocks.  The running maximum follows only when
+// it is passed by 2^6, so that the outputs are rescaled a few times in all.  The
+// weights are rounded to bfloat16 once, as the output is; their sum is taken
+// before.
+//   Bound by the matrix cores and the LDS reads that feed them (D = 256: the
+// queries and the output fill the registers, so a key block read from LDS serves
+// 32 queries only, and both take the same time at their best).  4096 rows a head
+// x 16384 tokens x 256, 2 heads: 137 GFLOP in 159 us, 0.86 PFLOP/s, 0.7 of a
+// large library product's rate; 512 rows x 4096 x 128, 8 heads (the queries of 64
+// requests): 19 us.
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
 {
@@ -486,7 +499,9 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
     }
 }
 
-// The parts of each row joined: a wave per row.
+// The parts of each row joined: a wave per row.  Bound by the parts' bytes: 9 x
+// 8192 rows of 256 (75 MB) in 14 us.  Joining them in attn_rows_kernel instead,
+// which has few waves to wait with, is slower (512 requests in all: 208 -> 225 us).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
@@ -548,8 +563,13 @@ Split split_of(const stepq_attn_desc *d)
     const auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
     // enough workgroups for the chip's 256 CUs, ranges of at least 256 keys
     if (d->prefix_len) {
-        // beyond 64 rows a head, rereading the prefix for every 16 rows costs more than a 256-row tile leaves idle
-        s.product = d->act_dtype == STEPQ_BF16 && rows > 64;
+        // attn_rows_kernel reads the prefix again for every 16 rows, which the caches serve up to a point; beyond
+        // 150 MB in all the product costs less.  Whole calls, rows / product, us, D = 64, 1024 tokens, 2 heads: 17 MB
+        // 11 / 19, 134 MB 22 / 24; D = 128, 1024 tokens, 8 heads: 34 MB 12 / 22, 134 MB 28 / 31, 268 MB 46 / 43; 4096
+        // tokens: 134 MB 23 / 25, 268 MB 34 / 31; D = 256, 2048 tokens, 2 heads: 34 MB 19 / 34, 134 MB 38 / 42, 268 MB
+        // 48 / 44; 512 requests over 16384 tokens: 17 GB
+        s.product = d->act_dtype == STEPQ_BF16 &&
+                    static_cast<double>(ceil_div(rows, 16)) * d->prefix_len * d->n_kv_heads * d->head_dim * 4 > 150e6;
         const int64_t blocks = d->n_kv_heads * ceil_div(rows, s.product ? 256 : 16), most = ceil_div(d->prefix_len, 256);
         int64_t parts = std::clamp<int64_t>(ceil_div(s.product ? 256 : 512, blocks), 1, most);
         // whole rounds of the 8 XCDs where that costs few parts

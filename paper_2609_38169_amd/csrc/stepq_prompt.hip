@@ -1,5 +1,6 @@
 // Prompts: packed sequences through the gated recurrences of stepq_rule.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "stepq_mma.h"
@@ -485,7 +486,8 @@ __device__ __forceinline__ void put_order(const ChunkArgs &a, int s, int lane)
     if (lane == 0) a.order[before] = s;
 }
 
-// First launch, decay rule: a wave per (chunk, head).
+// First launch, decay rule: a wave per (chunk, head).  Bound by the latency of
+// its scan: 512 chunks x 32 heads in 16 us.
 __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -508,6 +510,11 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
 // block's inverse by substitution, then the blocks left of it from
 //   T_wc = -T_ww sum_{c <= l < w} M_wl T_lc
 // in fp32 products, the blocks at equal distance from the diagonal together.
+// M is 4 % of a chunk's products; what counts is the chain of 16 substitution
+// steps and 3 rounds of blocks, so that 4 waves a SIMD (128 registers; the
+// inverse takes the keys' place in LDS) beat 3 with more registers: 32 sequences
+// 174 -> 139 us.  8 sequences of 1088 tokens x 32 heads: 51 us, 2.5 TB/s of keys
+// read and T' written.
 template <typename T, int DKP, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prompt_solve_kernel(ChunkArgs a)
 {
@@ -700,6 +707,19 @@ constexpr int kSegmentHead = 64;         // floats; [0] = gamma
 // (result layout: lane n column n).  Every product with the state, and every
 // one after it, keeps the columns in their lanes, so that the waves share only
 // what is read, and each column of an operand has a power of two of its own.
+//   Bound by the chain of a chunk: R needs S, U needs R, the next S needs U, and
+// 2 waves a SIMD (their state, R, O and the next chunk's tiles: 171 registers)
+// cover its waits only in part.  8 sequences of 1088 tokens x 32 heads, a
+// workgroup for every CU: 129 us, 7.4 us a chunk, in which the vector units issue
+// half of the time (conversions to planes above all) and the matrix cores work
+// 29 %; 2.1 TB/s.  Measured against it, for 32 sequences: 32 columns a wave
+// spill; 128 registers and two workgroups a CU spill too (826 us against 618
+// then); two workgroups of 64 columns form K, Q and P twice (492 -> 564);
+// opposite orders of P and K S in the two waves of a SIMD 570 -> 603; values
+// asked for a whole chunk ahead 488 -> 498; rounded products in one instruction
+// (v_fma_mixlo) instead of multiplies and packed conversions 504 -> 528.
+//   VEC: rows of 16-byte pieces that start at 16 bytes.  The other form reads
+// them at any alignment and cuts the last one; taken for all, 570 -> 628 us.
 template <typename T, int DKP, int NW, bool DELTA, bool VEC, bool OUT>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void prompt_chunks_kernel(ChunkArgs a)
 {
@@ -1077,7 +1097,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     }
 }
 
-// The states after the segments of a sequence, in order, decay rule: 4 elements a thread.
+// The states after the segments of a sequence, in order, decay rule: 4 elements
+// a thread.  Bound by memory: the records of 24 segments x 32 heads of 128 x 128
+// read and written, 100 MB in 21 us, 4.7 TB/s.
 __global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
 {
     const int quads = a.p.dk * a.p.dv / 4, blocks = (quads + 255) / 256;
@@ -1102,6 +1124,8 @@ __global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
 // The same for the Delta rule, S <- A S + B in fp32 products: a workgroup 16
 // columns of the state, a wave a quarter of its rows.  The state goes around
 // through LDS; A does not depend on it and is asked for one segment ahead.
+// Bound by the chain: 8 segments x 32 heads of 128 x 128 in 33 us (97 us with a
+// workgroup for all columns of a head).
 template <int DKP>
 __global__ __launch_bounds__(256) void prompt_join_delta_kernel(ChunkArgs a)
 {
@@ -1229,14 +1253,35 @@ stepq_status check(const stepq_prompt_desc *d)
 }
 
 // Chunks per segment; 0: sequences are walked whole.  Lengths are not known
-// here: the average decides.
+// here: the average decides, and of several sequences the longest is taken to be
+// half as long again.  Segments pay where whole sequences leave CUs idle: they
+// cost a walk of their own for B (Delta rule: and one for A), and a step of the
+// join each, of which more than about the root of the chunks' number are not
+// worth it.  Whole against segments, heads of 128 x 128, us:
+//   Delta, 32 heads: 16 chunks 111 / 91 (8 segments), 32 chunks 209 / 123, 128
+//     chunks 815 / 336; 8 chunks 62 / 62; 8 heads, 64 chunks 391 / 115 (16); 96
+//     heads, 64 chunks 445 / 413 (2), 16 chunks 121 / 137; 128 heads, 64 chunks
+//     466 / 511 (2); 5 ragged fp32 sequences of 6 heads, 12 chunks each on the
+//     average, 200 / 93 (6);
+//   decay, 32 heads: 8 chunks 50 / 39 (8), 32 chunks 167 / 64, 128 chunks 647 /
+//     168, 512 chunks 2572 / 600, and 539 with 24; 4 chunks 29 / 36 (4); 64 heads,
+//     16 chunks 91 / 63 (4); 128 heads, 64 chunks 330 / 278 (4), 16 chunks
+//     90 / 107; 160 heads, 32 chunks 172 / 190 (3).
 int32_t segment_chunks(const stepq_prompt_desc *d)
 {
     const int64_t pairs = int64_t(d->n_seq) * d->n_v_heads, each = d->n_seq ? slots(d) / d->n_seq : 0;
+    const int64_t longest = d->n_seq > 1 ? each * 3 / 2 : each, root = std::lround(std::sqrt(static_cast<double>(each)));
     const bool delta = d->rule == STEPQ_RULE_DELTA;
-    if (pairs < 1 || pairs >= 160) return 0;
-    const int64_t parts = std::min((delta ? 256 : 768) / pairs, each / (delta ? 8 : 4));
-    return parts < (delta ? 4 : 2) ? 0 : static_cast<int32_t>((each + parts - 1) / parts);
+    if (pairs < 1 || pairs >= (delta ? 100 : 160)) return 0;
+    int64_t parts;
+    if (delta) {
+        parts = std::min(256 / pairs, 2 * root);
+        if (parts < 2 || longest * parts < 6 * parts + 52) return 0;
+    } else {
+        parts = std::min({(each >= 256 ? 768 : pairs <= 64 ? 256 : 512) / pairs, 4 * root, each});
+        if (parts < 2 || longest < (pairs <= 64 ? 8 : 32)) return 0;
+    }
+    return static_cast<int32_t>((each + parts - 1) / parts);
 }
 
 size_t record_bytes(const stepq_prompt_desc *d)
