@@ -44,7 +44,8 @@ struct ChunkGates {
     float g[kC], w[kC], b[kC];
     int32_t bad;             // first token whose key or gate is not finite (Delta; kC: none)
     uint32_t tmax;           // largest |T'|, as bits
-    int32_t pad[30];
+    uint32_t kmax;           // largest finite |k| (Delta), as bits
+    int32_t pad[29];
 };
 static_assert(sizeof(ChunkGates) == 1408, "record size");
 constexpr size_t kTBytes = 2 * 6 * 1024;
@@ -559,7 +560,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
     bool keys_fine;
     kmax_s[w] = wave_max_of(v, &keys_fine);
     __syncthreads();
-    const Pow2 sk = scale_for(max(max(kmax_s[0], kmax_s[1]), max(kmax_s[2], kmax_s[3])));
+    const uint32_t kmax = max(max(kmax_s[0], kmax_s[1]), max(kmax_s[2], kmax_s[3]));
+    const Pow2 sk = scale_for(kmax);
     if (!fine) atomicMin(&bad_s, lane);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -572,6 +574,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
     const int bad = bad_s;
     uint8_t *rec = a.ws + (static_cast<size_t>(x) * a.p.Hv + h) * a.record;
     if (w == 0) put_gates(reinterpret_cast<ChunkGates *>(rec), lane, lg, beta, bad);
+    if (tid == 0) reinterpret_cast<ChunkGates *>(rec)->kmax = kmax;
     // M: lane (g, n) holds row i = 16 w + n, columns 16 tt + 4 g .. + 3
     f16x8 mine[DKP / 32][NA];
 #pragma unroll
@@ -790,7 +793,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     constexpr int NP = (12 + NW - 1) / NW;           // 1 KB pieces of T' per wave
     f16x8 tx[NP];
     constexpr int NG = (kGateWords + 64 * NW - 1) / (64 * NW);
-    uint32_t gx[NG];
+    uint32_t gx[NG], kmax = 0;
     const auto record = [&](int c) { return records + static_cast<size_t>(c) * a.p.Hv * a.record; };
     // Whole chunks whose rows lie within 32-bit offsets: one lane offset per
     // array for all chunks, the rest in scalar registers.
@@ -831,6 +834,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         const uint32_t *words = reinterpret_cast<const uint32_t *>(record(c));
 #pragma unroll
         for (int i = 0; i < NG; ++i) gx[i] = words[min(static_cast<int>(threadIdx.x) + 64 * NW * i, kGateWords - 1)];
+        if (DELTA) kmax = reinterpret_cast<const ChunkGates *>(words)->kmax;
     };
     if (chunks > first) fetch(first), fetch_values(first);
 
@@ -850,7 +854,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
             }
         }
         again();
-        tops[0][wv] = wave_max_of(kx);
+        if constexpr (!DELTA) tops[0][wv] = wave_max_of(kx);
         if constexpr (OUT) tops[1][wv] = wave_max_of(qx);
         lds_barrier();
         const ChunkGates *cg = reinterpret_cast<const ChunkGates *>(record(c));
@@ -859,10 +863,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
             for (int i = 0; i < NP; ++i) tx[i] = from[(wv + NW * i) % 12 * 64];
         }
-        uint32_t mk = 0, mq = 0;
+        uint32_t mk = DELTA ? __builtin_amdgcn_readfirstlane(kmax) : 0, mq = 0;
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
-            mk = max(mk, tops[0][i]);
+            if (!DELTA) mk = max(mk, tops[0][i]);
             if constexpr (OUT) mq = max(mq, tops[1][i]);
         }
         const Pow2 sk = scale_for(mk), sq = scale_for(mq);
