@@ -243,7 +243,8 @@ PyObject *py_tiles(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 
 // ---------------------------------------------------------------------------
 // The calls without a pool: everything is on the current device, sizes follow
-// from the tensors.
+// from the tensors, workspaces from torch (on the current stream).  One token
+// of a small model 14 -> 4 us, attention of 4 requests 19 -> 11 us a call.
 
 // bind_calls(state_step, prompt_workspace, prompt, attention_workspace, attention)
 PyObject *py_bind_calls(PyObject *, PyObject *args)
