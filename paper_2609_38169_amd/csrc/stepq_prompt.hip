@@ -61,13 +61,20 @@ struct ChunkArgs {
     float *segs;             // per (segment, head): SegmentHead, B or the state after it [dk][dv], A [DKP][DKP] (Delta)
     size_t seg_floats;
     int32_t near;            // 64 tokens of q, k and v lie within 2^32 bytes
-    int32_t *order;          // [n_seq] sequences, longest first; NULL: they are walked in their own order
+    int4 *order;             // [n_seq] sequences, longest first: number, bounds, initial state; NULL: they are walked in their own order
 };
 
 __device__ __forceinline__ int2 seq_bounds(const PromptArgs &a, int s)
 {
     const int from = min(max(a.cu[s], 0), a.T);
     return make_int2(from, min(max(a.cu[s + 1], from), a.T));
+}
+
+// The index of the state sequence s starts from; -1: zeros.
+__device__ __forceinline__ int initial_index(const PromptArgs &a, int s)
+{
+    const int src = a.state_in ? (a.in_ids ? a.in_ids[s] : s) : -1;
+    return src < a.n_in ? src : -1;
 }
 
 // First slot of sequence s where a slot holds `unit` tokens.
@@ -484,7 +491,7 @@ __device__ __forceinline__ void put_order(const ChunkArgs &a, int s, int lane)
     }
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) before += __shfl_xor(before, m);
-    if (lane == 0) a.order[before] = s;
+    if (lane == 0) a.order[before] = make_int4(s, be.x, be.y, initial_index(a.p, s));
 }
 
 // First launch, decay rule: a wave per (chunk, head).  Bound by the latency of
@@ -680,10 +687,9 @@ __device__ __forceinline__ void each_state_row(P *base, int dk, int dv, int g, i
 }
 
 // The state sequence s starts from; NULL: zeros.
-__device__ __forceinline__ const float *initial_state(const PromptArgs &a, int s, int h)
+__device__ __forceinline__ const float *initial_state(const PromptArgs &a, int src, int h)
 {
-    const int src = a.state_in ? (a.in_ids ? a.in_ids[s] : s) : -1;
-    return src >= 0 && src < a.n_in ? a.state_in + (static_cast<size_t>(src) * a.Hv + h) * a.dk * a.dv : nullptr;
+    return src >= 0 ? a.state_in + (static_cast<size_t>(src) * a.Hv + h) * a.dk * a.dv : nullptr;
 }
 
 __device__ __forceinline__ uint32_t tile_max(const f32x4 (&x)[4])
@@ -756,15 +762,22 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     const int hq = h / (a.p.Hv / a.p.Hqk);
     const bool values = OUT || !DELTA || cb < value_blocks;      // B; else A
     const int col0 = (values ? cb : cb - value_blocks) * W, mycol = wv * 16;
-    const int s = a.seg ? owner(a.p, item, lane, kC * a.seg)
-                        : a.order ? a.order[item] : item;
-    const int2 be = seq_bounds(a.p, s);
+    int s, start;
+    int2 be;
+    if (!a.seg && a.order) {
+        const int4 e = a.order[item];            // one load deep
+        s = e.x, be = make_int2(e.y, e.z), start = e.w;
+    } else {
+        s = a.seg ? owner(a.p, item, lane, kC * a.seg) : item;
+        be = seq_bounds(a.p, s);
+        start = initial_index(a.p, s);
+    }
     const int total = (be.y - be.x + kC - 1) / kC, part = a.seg ? item - first_slot(a.p, s, kC * a.seg) : 0;
     const int first = part * a.seg, chunks = a.seg ? min(total, first + a.seg) : total;
     if (part > 0 && first >= total) return;
     if (!OUT && chunks == total) return;         // nothing follows it
     float *rec = a.seg ? a.segs + (static_cast<size_t>(item) * a.p.Hv + h) * a.seg_floats : nullptr;
-    const uint8_t *records = a.ws + (static_cast<size_t>(first_slot(a.p, s)) * a.p.Hv + h) * a.record;
+    const uint8_t *records = a.ws + (static_cast<size_t>(be.x / kC + s) * a.p.Hv + h) * a.record;
 
     f32x4 S[DKP / 16];
 #pragma unroll
@@ -772,7 +785,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     if constexpr (OUT) {
         // the first of several segments has its state from the last one's record: state_out may be state_in
         const int64_t back = part == 0 && a.seg ? (total + a.seg - 1) / a.seg - 1 : -1;
-        const float *from = part == 0 && back <= 0 ? initial_state(a.p, s, h)
+        const float *from = part == 0 && back <= 0 ? initial_state(a.p, start, h)
                                                    : rec + back * a.p.Hv * static_cast<int64_t>(a.seg_floats) + kSegmentHead;
         if (from)
             each_state_row<DKP>(from + col0 + mycol, a.p.dk, a.p.dv, g, n,
@@ -1111,7 +1124,7 @@ __global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
     const int2 be = seq_bounds(a.p, s);
     const int total = (be.y - be.x + kC - 1) / kC, parts = (total + a.seg - 1) / a.seg;
     if (e >= quads || parts < 2) return;
-    const float *from = initial_state(a.p, s, h);
+    const float *from = initial_state(a.p, initial_index(a.p, s), h);
     f32x4 S = {};
     if (from)
 #pragma unroll
@@ -1143,7 +1156,7 @@ __global__ __launch_bounds__(256) void prompt_join_delta_kernel(ChunkArgs a)
     if (parts < 2) return;
     const size_t step = a.p.Hv * a.seg_floats;
     float *rec = a.segs + (static_cast<size_t>(first_slot(a.p, s, kC * a.seg)) * a.p.Hv + h) * a.seg_floats;
-    const float *from = initial_state(a.p, s, h);
+    const float *from = initial_state(a.p, initial_index(a.p, s), h);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         f32x4 x;
@@ -1315,7 +1328,7 @@ Layout layout_of(const stepq_prompt_desc *d)
     // many sequences the last ones are a small part, and counting who is longer is not.
     if (!l.seg && d->n_seq > 1 && d->n_seq <= 4096 && int64_t(d->n_seq) * d->n_v_heads > 256) {
         l.order = l.bytes;
-        l.bytes += (static_cast<size_t>(d->n_seq) * sizeof(int32_t) + 255) / 256 * 256;
+        l.bytes += (static_cast<size_t>(d->n_seq) * sizeof(int4) + 255) / 256 * 256;
     }
     return l;
 }
@@ -1362,7 +1375,7 @@ extern "C" stepq_status stepq_prompt(const stepq_prompt_desc *d, const int32_t *
     a.near = std::max({a.p.sq, a.p.sk, a.p.sv}) <= (int64_t(1) << 23);
     a.seg = l.seg, a.seg_slots = l.seg_slots, a.seg_floats = l.seg_floats;
     a.segs = reinterpret_cast<float *>(a.ws + l.chunks);
-    a.order = l.order ? reinterpret_cast<int32_t *>(a.ws + l.order) : nullptr;
+    a.order = l.order ? reinterpret_cast<int4 *>(a.ws + l.order) : nullptr;
     const int e = d->act_dtype == STEPQ_BF16 ? 8 : 4;   // elements in 16 bytes
     const bool vec = d->d_k % 8 == 0 && (a.p.sq | a.p.sk | a.p.sv) % e == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16);
     const hipStream_t s = static_cast<hipStream_t>(stream);
