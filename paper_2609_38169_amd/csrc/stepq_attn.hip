@@ -499,35 +499,60 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
     }
 }
 
-// The parts of each row joined: a wave per row.  Bound by the parts' bytes: 9 x
-// 8192 rows of 256 (75 MB) in 14 us.  Joining them in attn_rows_kernel instead,
-// which has few waves to wait with, is slower (512 requests in all: 208 -> 225 us).
-template <typename T, int D>
+// The parts of each row joined: W waves per row take parts in turn, a few at a
+// time so that their loads overlap.  Few rows (up to 1024): 4 waves, as latency
+// counts; a request over 16384 tokens, 16 heads of 256 in 65 parts, in all: 37 us
+// with one load after the other in a wave, 20 so.  More: a wave each, bound by
+// the parts' bytes; 9 x 8192 rows of 256 (75 MB) in 14 us, 3 more with 4 waves.
+// (Joined in attn_rows_kernel instead, which has few waves to wait with, 512
+// requests take 225 us in all, not 208.)
+template <typename T, int D, int W>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x & 63;
-    const size_t total = static_cast<size_t>(a.batch) * a.Hq, row = static_cast<size_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (row >= total) return;
+    constexpr int E = D / 64, U = 4;
+    using Piece = __attribute__((ext_vector_type(E))) float;
+    __shared__ alignas(16) float sum[4][D];
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % W, lane = threadIdx.x & 63;
+    const size_t total = static_cast<size_t>(a.batch) * a.Hq, row = static_cast<size_t>(blockIdx.x) * (4 / W) + w / W;
+    if (W == 1 && row >= total) return;
     const int parts = a.prefix_parts + a.own_parts;
-    float top = -INFINITY;
-    for (int i = lane; i < parts; i += 64) top = fmaxf(top, a.ml[i * total + row].x);
+    const auto stats = [&](int c) { return c + lane < parts ? a.ml[(c + lane) * total + row] : make_float2(-INFINITY, 0.0f); };
+    const float2 first = stats(0);
+    float top = first.x;
+    for (int c = 64; c < parts; c += 64) top = fmaxf(top, stats(c).x);
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
     const float base = top == -INFINITY ? 0.0f : top;
-    float y[E] = {}, z = 0.0f;
-    for (int i = 0; i < parts; ++i) {
-        const float2 ml = a.ml[i * total + row];
+    Piece y = {};
+    float z = 0.0f;
+    for (int c = 0; c < parts; c += 64) {
+        const float2 ml = c == 0 ? first : stats(c);
         const float f = __builtin_amdgcn_exp2f(ml.x - base);
         z = fmaf(ml.y, f, z);
-        const float *at = a.acc + (i * total + row) * D + lane * E;
+        const int n = min(64, parts - c);
+        for (int p = wave; p < n; p += W * U) {
+            Piece x[U];
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = fmaf(f, at[e], y[e]);
+            for (int u = 0; u < U; ++u)
+                x[u] = reinterpret_cast<const Piece *>(a.acc + ((c + min(p + W * u, n - 1)) * total + row) * D)[lane];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + W * u < n) y += x[u] * __shfl(f, p + W * u);
+        }
     }
-    T *o = static_cast<T *>(a.o) + row * D + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = narrow<T>(z == 0.0f ? 0.0f : y[e] / z);
-    if (lane == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
+    for (int x = 32; x > 0; x >>= 1) z += __shfl_xor(z, x);
+    T *o = static_cast<T *>(a.o) + row * D;
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[lane * E + e] = narrow<T>(z == 0.0f ? 0.0f : y[e] / z);
+    } else {
+        *reinterpret_cast<Piece *>(&sum[w][lane * E]) = y;
+        __syncthreads();
+        const int d = threadIdx.x;
+        if (d < D) o[d] = narrow<T>(z == 0.0f ? 0.0f : (sum[0][d] + sum[1][d] + sum[2][d] + sum[3][d]) / z);
+    }
+    if (wave == 0 && lane == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
 }
 
 stepq_status check(const stepq_attn_desc *d)
@@ -559,9 +584,16 @@ struct Split {
 Split split_of(const stepq_attn_desc *d)
 {
     Split s{};
+    if (d->batch == 0) return s;
     const int64_t G = d->n_q_heads / d->n_kv_heads, rows = d->batch * G;
     const auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    // enough workgroups for the chip's 256 CUs, ranges of at least 256 keys
+    // attn_rows_kernel: two workgroups a CU, of ranges of 128 keys or more (a tile per wave), 256 where there would be
+    // more than 16, whose join costs more than the shorter ranges save: 4 requests over 512 + 64 tokens 10.9 us at 256, 9.6
+    // at 128; one over 4096 + 1024 11.8 and 13.1, over 16384 20 and 28; 64 is slower than 128 from 1024 tokens on
+    const auto ranges = [&](int64_t blocks, int64_t len) {
+        const int64_t want = std::clamp<int64_t>(ceil_div(512, blocks), 1, std::max<int64_t>(1, ceil_div(len, 128)));
+        return want <= 16 ? want : std::max<int64_t>(16, std::min(want, ceil_div(len, 256)));
+    };
     if (d->prefix_len) {
         // attn_rows_kernel reads the prefix again for every 16 rows, which the caches serve up to a point; beyond
         // 150 MB in all the product costs less.  Whole calls, rows / product, us, D = 64, 1024 tokens, 2 heads: 17 MB
@@ -571,16 +603,15 @@ Split split_of(const stepq_attn_desc *d)
         s.product = d->act_dtype == STEPQ_BF16 &&
                     static_cast<double>(ceil_div(rows, 16)) * d->prefix_len * d->n_kv_heads * d->head_dim * 4 > 150e6;
         const int64_t blocks = d->n_kv_heads * ceil_div(rows, s.product ? 256 : 16), most = ceil_div(d->prefix_len, 256);
-        int64_t parts = std::clamp<int64_t>(ceil_div(s.product ? 256 : 512, blocks), 1, most);
+        int64_t parts = s.product ? std::clamp<int64_t>(ceil_div(256, blocks), 1, most) : ranges(blocks, d->prefix_len);
         // whole rounds of the 8 XCDs where that costs few parts
         if (s.product)
             while (parts < most && d->n_kv_heads * parts % 8 != 0 && parts < 2 * ceil_div(256, blocks)) ++parts;
         s.prefix_parts = static_cast<int>(parts);
         if (!s.product) s.prefix_items = static_cast<int>(blocks * parts);
     }
-    const int64_t blocks = d->batch * static_cast<int64_t>(d->n_kv_heads) * ceil_div(G, 16);
-    const int64_t most = std::max<int64_t>(1, ceil_div(static_cast<int64_t>(d->max_pages) * d->page_size, 256));
-    s.own_parts = static_cast<int>(std::clamp<int64_t>(ceil_div(512, blocks), 1, most));
+    s.own_parts = static_cast<int>(ranges(d->batch * static_cast<int64_t>(d->n_kv_heads) * ceil_div(G, 16),
+                                          static_cast<int64_t>(d->max_pages) * d->page_size));
     return s;
 }
 
@@ -600,7 +631,9 @@ void launch(AttnArgs a, const Split &s, hipStream_t st)
             attn_prefix_kernel<D><<<dim3(static_cast<unsigned>(grid)), 512, 0, st>>>(a);
         }
     attn_rows_kernel<T, D><<<dim3(static_cast<unsigned>(a.prefix_items + own)), 256, 0, st>>>(a);
-    attn_join_kernel<T, D><<<dim3(static_cast<unsigned>((static_cast<int64_t>(a.batch) * a.Hq + 3) / 4)), 256, 0, st>>>(a);
+    const unsigned rows = static_cast<unsigned>(a.batch) * a.Hq;
+    if (rows <= 1024) attn_join_kernel<T, D, 4><<<dim3(rows), 256, 0, st>>>(a);
+    else attn_join_kernel<T, D, 1><<<dim3((rows + 3) / 4), 256, 0, st>>>(a);
 }
 
 template <typename T>
