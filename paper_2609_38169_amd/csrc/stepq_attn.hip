@@ -88,9 +88,10 @@ struct Running {
 // transposed, keys x queries, so that a query's weights lie in one lane group
 // and go into the second product as they are; values pass through LDS of the
 // wave's own to be read by columns.  Bound by the bytes of the caches: 64
-// requests x 8 key/value heads x 1024 tokens of 128 bfloat16 (268 MB) in 29-31 us,
-// of which the last-level cache serves a part; 512 x 2 x 256 of 256 (268 MB) in
-// 52 us, 5.2 TB/s.  4 requests over 512 + 64 tokens: 8 us, latency.
+// requests x 8 key/value heads x 1-1024 tokens of 128 bfloat16 (134 MB) in 28.5 us,
+// 4.7 TB/s.  512 x 2 x 1-256 tokens of 256 (134 MB) take 51 us, 2.6 TB/s: a wave
+// has one tile or two there, and its registers (400) leave 4 waves a CU to wait
+// with; at 256 registers they spill.  4 requests over 512 + 64 tokens: 6.6 us, latency.
 template <typename T>
 struct Tile;
 template <>
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnAr
 // queries and the output fill the registers, so a key block read from LDS serves
 // 32 queries only, and both take the same time at their best).  4096 rows a head
 // x 16384 tokens x 256, 2 heads: 137 GFLOP in 159 us, 0.86 PFLOP/s, 0.7 of a
-// large library product's rate; 512 rows x 4096 x 128, 8 heads (the queries of 64
+// large library product's rate; 256 rows x 4096 x 128, 8 heads (the queries of 64
 // requests): 19 us.
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)

@@ -1141,16 +1141,20 @@ __global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
 // The same for the Delta rule, S <- A S + B in fp32 products: a workgroup 16
 // columns of the state, a wave a quarter of its rows.  The state goes around
 // through LDS; A does not depend on it and is asked for one segment ahead.
-// Bound by the chain: 8 segments x 32 heads of 128 x 128 in 33 us (97 us with a
-// workgroup for all columns of a head).
+// Bound by the chain of segments: 8 of them x 32 heads of 128 x 128 in 27 us (97
+// us with a workgroup for all columns of a head; 32 with a head's column blocks
+// on 8 XCDs, each of which read A for itself).
 template <int DKP>
 __global__ __launch_bounds__(256) void prompt_join_delta_kernel(ChunkArgs a)
 {
     constexpr int KT = DKP / 16, RT = KT / 4, LD = DKP + 4;
     __shared__ alignas(16) float st[2][16 * LD];      // [column][row]
     const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
-    const int blocks = a.p.dv / 16, h = blockIdx.x / blocks % a.p.Hv, s = blockIdx.x / blocks / a.p.Hv;
-    const int col = blockIdx.x % blocks * 16 + n, row0 = 16 * RT * wv + 4 * g;     // + 16 rt + r
+    // the column blocks of a head go to one XCD (every 8th workgroup), which then reads its A once
+    const int blocks = a.p.dv / 16, pair = blockIdx.x / (8 * blocks) * 8 + blockIdx.x % 8;
+    if (pair >= a.p.n_seq * a.p.Hv) return;
+    const int h = pair % a.p.Hv, s = pair / a.p.Hv;
+    const int col = blockIdx.x / 8 % blocks * 16 + n, row0 = 16 * RT * wv + 4 * g;     // + 16 rt + r
     const int2 be = seq_bounds(a.p, s);
     const int total = (be.y - be.x + kC - 1) / kC, parts = (total + a.seg - 1) / a.seg;
     if (parts < 2) return;
@@ -1219,7 +1223,7 @@ void launch_rule(const ChunkArgs &a, hipStream_t s)
         const unsigned blocks = 1 + (DELTA ? (DKP + a.p.dv - 1) / a.p.dv : 0);
         if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC, false><<<dim3(walks * blocks), 512, 0, s>>>(a);
         else prompt_chunks_kernel<T, DKP, 4, DELTA, VEC, false><<<dim3(walks * blocks), 256, 0, s>>>(a);
-        if constexpr (DELTA) prompt_join_delta_kernel<DKP><<<dim3(pairs * (a.p.dv / 16)), 256, 0, s>>>(a);
+        if constexpr (DELTA) prompt_join_delta_kernel<DKP><<<dim3((pairs + 7) / 8 * 8 * (a.p.dv / 16)), 256, 0, s>>>(a);
         else prompt_join_decay_kernel<<<dim3(pairs * ((a.p.dk * a.p.dv / 4 + 255) / 256)), 256, 0, s>>>(a);
     }
     if (a.p.dv == 128) prompt_chunks_kernel<T, DKP, 8, DELTA, VEC, true><<<dim3(walks), 512, 0, s>>>(a);
