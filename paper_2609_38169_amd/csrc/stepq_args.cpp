@@ -354,21 +354,22 @@ PyObject *py_prompt(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded([&]() -> long {
         if (n_args != 11 || !g.prompt) return -1;
-        const at::Tensor *q = tensor_of(a[0], 3), *v = tensor_of(a[2], 3), *cu = tensor_of(a[8], 1);
+        const at::Tensor *q = tensor_of(a[0], 3), *v = tensor_of(a[2], 3), *cu = a[8] == Py_None ? nullptr : tensor_of(a[8], 1);
         Plain p{};
         int64_t rule;
-        if (!q || !v || !cu || cu->size(0) < 1 || !take_device(*q, &p) || !take_long(a[7], &rule)) return -1;
-        const int64_t T = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2), n = cu->size(0) - 1;
+        if (!q || !v || (a[8] != Py_None && (!cu || cu->size(0) < 1)) || !take_device(*q, &p) || !take_long(a[7], &rule)) return -1;
+        const int64_t T = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2);
+        const int64_t n = cu ? cu->size(0) - 1 : 1;
         const at::ScalarType dt = q->scalar_type();
         stepq_prompt_desc d{};
-        void *qp, *kp, *vp, *op, *ap, *bp, *cp, *out, *in = nullptr, *ids = nullptr, *st;
+        void *qp, *kp, *vp, *op, *ap, *bp, *cp = nullptr, *out, *in = nullptr, *ids = nullptr, *st;
         int gate;
         int64_t m = 0;
         if (n > INT32_MAX || !take_tokens(a[0], p, dt, {T, Hqk, dk}, &qp, &d.q_stride) ||
             !take_tokens(a[1], p, dt, {T, Hqk, dk}, &kp, &d.k_stride) ||
             !take_tokens(a[2], p, dt, {T, Hv, dv}, &vp, &d.v_stride) ||
             !take_tokens(a[5], p, dt, {T, Hv, dv}, &op, &d.o_stride) ||
-            !take_gates(a[3], a[4], p, {T, Hv}, &ap, &bp, &gate) || !take(a[8], p, at::kInt, {n + 1}, &cp) ||
+            !take_gates(a[3], a[4], p, {T, Hv}, &ap, &bp, &gate) || (cu && !take(a[8], p, at::kInt, {n + 1}, &cp)) ||
             !take(a[6], p, at::kFloat, {n, Hv, dk, dv}, &out))
             return -1;
         if (a[9] != Py_None) {

@@ -9,7 +9,7 @@ namespace stepq {
 namespace {
 
 struct PromptArgs {
-    const int32_t *cu;
+    const int32_t *cu;       // NULL: one sequence of all tokens
     const void *q, *k, *v;
     Gate alpha, beta;        // beta.p NULL: 1
     void *o;
@@ -66,6 +66,7 @@ struct ChunkArgs {
 
 __device__ __forceinline__ int2 seq_bounds(const PromptArgs &a, int s)
 {
+    if (!a.cu) return make_int2(0, a.T);
     const int from = min(max(a.cu[s], 0), a.T);
     return make_int2(from, min(max(a.cu[s + 1], from), a.T));
 }
@@ -80,7 +81,7 @@ __device__ __forceinline__ int initial_index(const PromptArgs &a, int s)
 // First slot of sequence s where a slot holds `unit` tokens.
 __device__ __forceinline__ int first_slot(const PromptArgs &a, int s, int unit = kC)
 {
-    return min(max(a.cu[s], 0), a.T) / unit + s;
+    return a.cu ? min(max(a.cu[s], 0), a.T) / unit + s : 0;
 }
 
 // The sequence that owns a chunk slot: the last one whose first slot is at most
@@ -1358,7 +1359,8 @@ extern "C" stepq_status stepq_prompt(const stepq_prompt_desc *d, const int32_t *
 {
     if (const stepq_status st = check(d)) return st;
     if (d->n_seq == 0) return STEPQ_OK;
-    if (!cu_seqlens || !state_out) return bad("NULL cu_seqlens or state_out");
+    if (!cu_seqlens && d->n_seq > 1) return bad("NULL cu_seqlens with more than one sequence");
+    if (!state_out) return bad("state_out is NULL");
     if (d->n_tokens && (!q || !k || !v || !alpha || !o)) return bad("NULL activation or output pointer");
     if (!state_in && in_ids) return bad("in_ids without state_in");
     if (state_in && !in_ids && d->n_states_in < d->n_seq) return bad("fewer states in state_in than sequences");

@@ -591,12 +591,12 @@ def stepq_prompt(q, k, v, alpha, beta, o, state_out, rule=STEPQ_RULE_DELTA, cu_s
     vp, vs = _tokens(v, "v", dt, (T, Hv, dv), dev)
     op, os_ = _tokens(o, "o", dt, (T, Hv, dv), dev)
     ap, bp, gate = _gates(alpha, beta, (T, Hv), dev)
-    if cu_seqlens is None:
-        cu_seqlens = torch.tensor([0, T], dtype=torch.int32, device=dev)
-    if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
-        raise ValueError("cu_seqlens must be a 1-D tensor of n + 1 entries")
-    n = cu_seqlens.shape[0] - 1
-    cu = _dev(cu_seqlens, "cu_seqlens", torch.int32, (n + 1,), dev)
+    n, cu = 1, None
+    if cu_seqlens is not None:
+        if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+            raise ValueError("cu_seqlens must be a 1-D tensor of n + 1 entries")
+        n = cu_seqlens.shape[0] - 1
+        cu = _dev(cu_seqlens, "cu_seqlens", torch.int32, (n + 1,), dev)
     out = _dev(state_out, "state_out", torch.float32, (n, Hv, dk, dv), dev)
     sp, ip, m = None, None, 0
     if state_in is not None:
