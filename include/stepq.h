@@ -365,7 +365,10 @@ typedef struct {
  * alpha lies in [0, 1]: 0 forgets everything before the token, an alpha < 0
  * gives NaN.  state_out may be state_in itself (in place) when in_ids is NULL,
  * and must not overlap it otherwise.
- * Sums, decays and states are fp32 or wider; o is rounded once, to act_dtype. */
+ * Sums, decays and states are fp32 or wider, products are formed from operands
+ * of 24 bits (what falls below 2^-22 of a product is left out) with fp32's
+ * exponents: a token's o does not depend on the size of others in its chunk.  o
+ * is rounded once, to act_dtype. */
 stepq_status stepq_prompt_workspace(const stepq_prompt_desc *desc, size_t *bytes);
 stepq_status stepq_prompt(const stepq_prompt_desc *desc, const int32_t *cu_seqlens, const void *q, const void *k,
                           const void *v, const void *alpha, const void *beta, void *o, const float *state_in,

@@ -9,8 +9,6 @@
 namespace stepq {
 namespace {
 
-using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
-using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 using f32x16 = __attribute__((ext_vector_type(16))) float;
 
 struct AttnArgs {

@@ -1,13 +1,13 @@
 // Matrix-core building blocks shared by the prompt and attention kernels:
-// binary16 planes of fp32 values, 16x16x32 products of them, transposing reads.
+// bfloat16 planes of fp32 values, 16x16x32 products of them, transposing reads.
 #pragma once
 
 #include "stepq_seq.h"
 
 namespace stepq {
 
-using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
-using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
 using f32x2 = __attribute__((ext_vector_type(2))) float;
 using f32x4 = __attribute__((ext_vector_type(4))) float;
 using s16x4 = __attribute__((ext_vector_type(4))) short;
@@ -23,64 +23,42 @@ using u32x2 = __attribute__((ext_vector_type(2))) uint32_t;
 // results of two blocks (rows 0-15 and 16-31, column n in lane n) then are
 // operand B of the next product without a move between lanes.
 
-// A power of two that brings values of magnitude up to m below 2^14, near it
-// (binary16 then keeps 11 bits of everything down to 2^-28 of m), and its inverse.
-struct Pow2 {
-    float up, down;
-};
-__device__ __forceinline__ Pow2 scale_for(uint32_t m_bits)
-{
-    const uint32_t e = max(m_bits >> 23, 14u);
-    return Pow2{__uint_as_float((267u - e) << 23), __uint_as_float((e - 13u) << 23)};
-}
-
-// N binary16 planes of 8 floats times a power of two: the value rounded to 11
-// bits, then what that leaves, rounded to 11 more (22 bits; the difference is exact).
-template <int N>
-__device__ __forceinline__ void split(const float (&x)[8], float up, f16x8 (&p)[N])
+// Three bfloat16 planes of 8 floats, whose sum is the value itself: its upper
+// half (8 bits, cut), what that leaves rounded to 8 bits, and the rest (at most
+// 8 bits).  bfloat16 has fp32's exponents, so that a value keeps its bits whatever
+// stands beside it in its row, column or tile.
+__device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&p)[3])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const f16x2 hi = __builtin_convertvector((f32x2{x[2 * i] * up, x[2 * i + 1] * up}), f16x2);
+        const uint32_t a = __float_as_uint(x[2 * i]), b = __float_as_uint(x[2 * i + 1]);
+        const bf16x2 hi = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(b, a, 0x07060302u));
+        const f32x2 r = {x[2 * i] - __uint_as_float(a & 0xffff0000u), x[2 * i + 1] - __uint_as_float(b & 0xffff0000u)};
+        const bf16x2 mid = __builtin_convertvector(r, bf16x2);
+        const bf16x2 lo = __builtin_convertvector((f32x2{r[0] - static_cast<float>(mid[0]), r[1] - static_cast<float>(mid[1])}), bf16x2);
         p[0][2 * i] = hi[0], p[0][2 * i + 1] = hi[1];
-        if constexpr (N > 1) {
-            const f32x2 r = {fmaf(x[2 * i], up, -static_cast<float>(hi[0])), fmaf(x[2 * i + 1], up, -static_cast<float>(hi[1]))};
-            const f16x2 lo = __builtin_convertvector(r, f16x2);
-            p[1][2 * i] = lo[0], p[1][2 * i + 1] = lo[1];
-        }
+        p[1][2 * i] = mid[0], p[1][2 * i + 1] = mid[1];
+        p[2][2 * i] = lo[0], p[2][2 * i + 1] = lo[1];
     }
 }
-template <int N>
-__device__ __forceinline__ void split(const f32x4 &a, const f32x4 &b, float up, f16x8 (&p)[N])
+__device__ __forceinline__ void split(const f32x4 &a, const f32x4 &b, bf16x8 (&p)[3])
 {
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    split(x, up, p);
+    split(x, p);
 }
 
-// c += a b over planes, without the terms of order LIM and up (each order is
-// 2^-11 of the one before it).
-template <int LIM, int NA, int NB>
-__device__ __forceinline__ void mma(f32x4 &c, const f16x8 (&a)[NA], const f16x8 (&b)[NB])
+// c += a b over planes, the smallest terms first, without those below 2^-22 of
+// the product (a middle by a low plane, a low by a low).
+template <int NA, int NB>
+__device__ __forceinline__ void mma(f32x4 &c, const bf16x8 (&a)[NA], const bf16x8 (&b)[NB])
 {
 #pragma unroll
-    for (int o = LIM - 1; o >= 0; --o)
+    for (int o = 2; o >= 0; --o)
 #pragma unroll
         for (int i = 0; i < NA; ++i)
-            if (o - i >= 0 && o - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i], b[o - i], c, 0, 0, 0);
+            if (o - i >= 0 && o - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[o - i], c, 0, 0, 0);
 }
 
-template <int CTRL>
-__device__ __forceinline__ uint32_t max_dpp(uint32_t x)
-{
-    return max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, 0xf, 0xf, false)));
-}
-// The largest of the wave's values (as unsigned: the order of non-negative floats).
-__device__ __forceinline__ uint32_t wave_max(uint32_t x)
-{
-    x = max_dpp<0x121>(x), x = max_dpp<0x122>(x), x = max_dpp<0x124>(x), x = max_dpp<0x128>(x);   // row_ror 1, 2, 4, 8
-    const auto at = [&](int l) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), l)); };
-    return max(max(at(0), at(16)), max(at(32), at(48)));
-}
 // The largest over the lanes n, n + 16, n + 32, n + 48: over a column of results.
 __device__ __forceinline__ uint32_t column_max(uint32_t x)
 {

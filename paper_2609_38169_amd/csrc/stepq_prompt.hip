@@ -29,27 +29,26 @@ struct PromptArgs {
 //   O = G (Q S) + P U,  P = D (Q K^T)
 //   S <- G_last S + K^T (w U),  w_j = G_last / G_j
 // (the decay rule has U = beta V).
-// Operands on the matrix cores are binary16 planes of a value times a power of
-// two, two planes (22 bits) each but for bfloat16 keys and queries, which are
-// exact in one.  O gets the same as the states: with one plane (11 bits) its
-// error before the rounding to bfloat16 reached 2^-12 of a head's largest entry.
+// Operands on the matrix cores are bfloat16 planes of the values, three (24 bits,
+// the value itself) each but for bfloat16 keys and queries, which are one.  Their
+// exponents are fp32's: tokens of very different size share a chunk, and with
+// two binary16 planes under a power of two for a tile or a column (22 bits; 32
+// sequences 485 us, not 540) a token 2^28 times the others left nothing of those before it.
 // T' and the gates' products depend on no state: a first launch forms them
 // for every chunk at once; the second walks each sequence's chunks in order.
 constexpr int kC = 64;
 
 // Per (chunk, head) of the workspace: the gates' products, then for the Delta
-// rule the two planes of T', lane by lane as operand A wants them.
+// rule T', lane by lane as operand A wants it.
 struct ChunkGates {
     double lg[kC];           // log2 G_i: differences of them stay exact where G itself is 0 or tiny
     float g[kC], w[kC], b[kC];
     int32_t bad;             // first token whose key or gate is not finite (Delta; kC: none)
-    uint32_t tmax;           // largest |T'|, as bits
-    uint32_t kmax;           // largest finite |k| (Delta), as bits
-    int32_t pad[29];
+    int32_t pad[31];
 };
 static_assert(sizeof(ChunkGates) == 1408, "record size");
-constexpr size_t kTBytes = 2 * 6 * 1024;
-constexpr int kGateWords = 5 * kC + 2;   // lg, g, w, b, bad, tmax
+constexpr size_t kTBytes = 6 * 2048;
+constexpr int kGateWords = 5 * kC + 1;   // lg, g, w, b, bad
 
 struct ChunkArgs {
     PromptArgs p;
@@ -110,7 +109,7 @@ struct Act<bf16_t> {
 };
 template <>
 struct Act<float> {
-    static constexpr int planes = 2;
+    static constexpr int planes = 3;
     f32x4 x[2];
 };
 
@@ -234,7 +233,6 @@ struct Out4<float> {
 };
 template <>
 struct Out4<bf16_t> {
-    using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
     uint32_t x[2];
     __device__ __forceinline__ void set(const f32x4 &v)
     {
@@ -281,21 +279,7 @@ __device__ __forceinline__ uint32_t max_of(const Act<float> (&v)[N])
         for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(fabsf(v[i].x[e / 4][e % 4])));
     return m;
 }
-// the same without what is not finite
 constexpr uint32_t kInfBits = 0x7f800000u;
-template <typename T>
-__device__ __forceinline__ uint32_t finite_max8(uint32_t m, const Act<T> &v)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float a;
-        if constexpr (sizeof(T) == 2) a = i % 2 ? upper_bf16(v.x[i / 2]) : lower_bf16(v.x[i / 2]);
-        else a = v.x[i / 4][i % 4];
-        const uint32_t u = __float_as_uint(fabsf(a));
-        m = u < kInfBits ? max(m, u) : m;
-    }
-    return m;
-}
 template <typename T>
 __device__ __forceinline__ bool all_finite(const Act<T> &v)
 {
@@ -309,22 +293,7 @@ __device__ __forceinline__ bool all_finite(const Act<T> &v)
     }
     return ok;
 }
-// of a thread's N units, over its wave; *fine: all are finite
-template <int N, typename T>
-__device__ __forceinline__ uint32_t wave_max_of(const Act<T> (&v)[N], bool *fine = nullptr)
-{
-    uint32_t w = wave_max(max_of(v));
-    if (fine) *fine = w < kInfBits;
-    if (w >= kInfBits) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) m = finite_max8(m, v[i]);
-        w = wave_max(m);
-    }
-    return w;
-}
-
-// A tile of keys or queries: 64 rows of DKP elements in binary16 planes.  Their
+// A tile of keys or queries: 64 rows of DKP elements in bfloat16 planes.  Their
 // summation slots are the elements in order (operands are 16-byte reads), so
 // the state, their partner, keeps element 32 kb + 8 g + 4 h + r of a column in
 // row 4 g + r of its block 2 kb + h.
@@ -338,32 +307,30 @@ struct RowTile {
     static constexpr int NA = Act<T>::planes, RB = DKP * 2;
     alignas(16) uint8_t b[NA][kC * RB];
 
-    __device__ __forceinline__ void put(int row, int c8, const Act<T> &v, float up)
+    __device__ __forceinline__ void put(int row, int c8, const Act<T> &v)
     {
         uint8_t *at = &b[0][row * RB + ((c8 ^ swizzle<RB>(row)) * 16)];
-        float x[8];
+        if constexpr (NA == 1) {
+            *reinterpret_cast<u32x4 *>(at) = v.x;
+        } else {
+            bf16x8 p[NA];
+            split(v.x[0], v.x[1], p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (NA == 1) x[i] = i % 2 ? upper_bf16(v.x[i / 2]) : lower_bf16(v.x[i / 2]);
-            else x[i] = v.x[i / 4][i % 4];
+            for (int n = 0; n < NA; ++n) *reinterpret_cast<bf16x8 *>(at + n * kC * RB) = p[n];
         }
-        f16x8 p[NA];
-        split(x, up, p);
-#pragma unroll
-        for (int n = 0; n < NA; ++n) *reinterpret_cast<f16x8 *>(at + n * kC * RB) = p[n];
     }
 
     // operand: row 16 rt + n, elements 32 kb .. 32 kb + 31
-    __device__ __forceinline__ void rows(int rt, int kb, int g, int n, f16x8 (&a)[NA]) const
+    __device__ __forceinline__ void rows(int rt, int kb, int g, int n, bf16x8 (&a)[NA]) const
     {
         const int row = 16 * rt + n;
 #pragma unroll
         for (int i = 0; i < NA; ++i)
-            a[i] = *reinterpret_cast<const f16x8 *>(&b[i][row * RB + (((4 * kb + g) ^ swizzle<RB>(n)) * 16)]);
+            a[i] = *reinterpret_cast<const bf16x8 *>(&b[i][row * RB + (((4 * kb + g) ^ swizzle<RB>(n)) * 16)]);
     }
 
     // operand A of the transposed tile: tokens 32 kb .. 32 kb + 31 of state row state_row(dt, n)
-    __device__ __forceinline__ void columns(int dt, int kb, int g, int n, f16x8 (&a)[NA]) const
+    __device__ __forceinline__ void columns(int dt, int kb, int g, int n, bf16x8 (&a)[NA]) const
     {
         const int f = swizzle<RB>(4 * g + (n >> 2));
 #pragma unroll
@@ -375,45 +342,28 @@ struct RowTile {
                 const u32x2 x = read_columns(&b[i][row * RB + ((slot ^ f) * 16) + 8 * (dt & 1)]);
                 w[2 * h] = x[0], w[2 * h + 1] = x[1];
             }
-            a[i] = __builtin_bit_cast(f16x8, w);
+            a[i] = __builtin_bit_cast(bf16x8, w);
         }
     }
 };
 
-// A tile of values: 64 rows of W columns, bfloat16 or fp32 as given.
-template <typename T, int W>
+// A tile of bfloat16 values: 64 rows of W columns.
+template <int W>
 struct ValueTile {
-    static constexpr int RB = W * static_cast<int>(sizeof(T));
+    static constexpr int RB = 2 * W;
     alignas(16) uint8_t b[kC * RB];
 
-    __device__ __forceinline__ void put(int row, int c8, const Act<T> &v)
+    __device__ __forceinline__ void put(int row, int c8, const Act<bf16_t> &v)
     {
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<u32x4 *>(&b[row * RB + ((c8 ^ swizzle<RB>(row)) * 16)]) = v.x;
-        } else {
-            // 16 columns at a time exchanged between the rows that one read takes together
-            const int col = (8 * c8) ^ (16 * ((row >> 2) & (W / 16 - 1)));
-            *reinterpret_cast<f32x4 *>(&b[row * RB + col * 4]) = v.x[0];
-            *reinterpret_cast<f32x4 *>(&b[row * RB + col * 4 + 16]) = v.x[1];
-        }
+        *reinterpret_cast<u32x4 *>(&b[row * RB + ((c8 ^ swizzle<RB>(row)) * 16)]) = v.x;
     }
 
     // rows 16 tt + 4 g .. + 3 of column col + n (col a multiple of 16)
     __device__ __forceinline__ f32x4 four(int tt, int col, int g, int n) const
     {
-        if constexpr (sizeof(T) == 2) {
-            const int row = 16 * tt + 4 * g + (n >> 2), slot = col / 8 + ((n & 3) >> 1);
-            const u32x2 w = read_columns(&b[row * RB + ((slot ^ swizzle<RB>(row)) * 16) + 8 * (n & 1)]);
-            return f32x4{lower_bf16(w[0]), upper_bf16(w[0]), lower_bf16(w[1]), upper_bf16(w[1])};
-        } else {
-            f32x4 r;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = 16 * tt + 4 * g + j;
-                r[j] = *reinterpret_cast<const float *>(&b[row * RB + ((col ^ (16 * ((row >> 2) & (W / 16 - 1)))) + n) * 4]);
-            }
-            return r;
-        }
+        const int row = 16 * tt + 4 * g + (n >> 2), slot = col / 8 + ((n & 3) >> 1);
+        const u32x2 w = read_columns(&b[row * RB + ((slot ^ swizzle<RB>(row)) * 16) + 8 * (n & 1)]);
+        return f32x4{lower_bf16(w[0]), upper_bf16(w[0]), lower_bf16(w[1]), upper_bf16(w[1])};
     }
 };
 
@@ -421,25 +371,20 @@ struct ValueTile {
 __device__ __forceinline__ constexpr int triangle_row(int b) { return b < 2 ? b : b < 4 ? 2 : 3; }
 __device__ __forceinline__ constexpr int triangle_block(int b) { return b < 2 ? 0 : b & 1; }
 
-template <int N>
 struct TriangleTile {
-    alignas(16) uint8_t b[N][6 * 1024];
-    __device__ __forceinline__ void put(int block, int lane, const f16x8 (&p)[N])
+    alignas(16) uint8_t b[3][6 * 1024];
+    __device__ __forceinline__ void put(int block, int lane, const f32x4 &lo, const f32x4 &hi)
     {
+        bf16x8 p[3];
+        split(lo, hi, p);
 #pragma unroll
-        for (int i = 0; i < N; ++i) *reinterpret_cast<f16x8 *>(&b[i][block * 1024 + lane * 16]) = p[i];
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<bf16x8 *>(&b[i][block * 1024 + lane * 16]) = p[i];
     }
-    __device__ __forceinline__ void put(int block, int lane, const f32x4 &lo, const f32x4 &hi, float up)
-    {
-        f16x8 p[N];
-        split(lo, hi, up, p);
-        put(block, lane, p);
-    }
-    __device__ __forceinline__ void rows(int rb, int kb, int lane, f16x8 (&a)[N]) const
+    __device__ __forceinline__ void rows(int rb, int kb, int lane, bf16x8 (&a)[3]) const
     {
         const int block = rb < 2 ? rb : 2 * rb - 2 + kb;
 #pragma unroll
-        for (int i = 0; i < N; ++i) a[i] = *reinterpret_cast<const f16x8 *>(&b[i][block * 1024 + lane * 16]);
+        for (int i = 0; i < 3; ++i) a[i] = *reinterpret_cast<const bf16x8 *>(&b[i][block * 1024 + lane * 16]);
     }
 };
 
@@ -525,7 +470,7 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
 // 174 -> 139 us.  8 sequences of 1088 tokens x 32 heads: 51 us, 2.5 TB/s of keys
 // read and T' written.
 template <typename T, int DKP, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prompt_solve_kernel(ChunkArgs a)
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void prompt_solve_kernel(ChunkArgs a)
 {
     constexpr int NA = Act<T>::planes, U = DKP / 32, LD = 68;
     // the keys are not needed once M is formed: the inverse takes their place
@@ -539,7 +484,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
     __shared__ double lgs[kC];
     __shared__ float bs[kC];
     __shared__ int bad_s;
-    __shared__ uint32_t tmax_s, kmax_s[4];
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, n = lane & 15;
     const Share<DKP / 8, 256> sh(tid);
     const int x = blockIdx.x / a.p.Hv, h = blockIdx.x - x * a.p.Hv, hq = h / (a.p.Hv / a.p.Hqk);
@@ -549,7 +493,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
     const int64_t t0 = be.x + (x - first_slot(a.p, s)) * kC;
     const int len = min(kC, be.y - static_cast<int>(t0));
     if (len <= 0) return;
-    if (tid == 0) bad_s = kC, tmax_s = 0;
+    if (tid == 0) bad_s = kC;
     Act<T> v[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -565,26 +509,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
         if constexpr (!VEC) v[i] = settle(v[i], 8 * sh.c8, a.p.dk);
         v[i] = zero_unless(sh.valid(i, a.p.dk, len), v[i]);
     }
-    bool keys_fine;
-    kmax_s[w] = wave_max_of(v, &keys_fine);
+    const bool keys_fine = max_of(v) < kInfBits;
     __syncthreads();
-    const uint32_t kmax = max(max(kmax_s[0], kmax_s[1]), max(kmax_s[2], kmax_s[3]));
-    const Pow2 sk = scale_for(kmax);
     if (!fine) atomicMin(&bad_s, lane);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int row = sh.row + sh.step * i;
         if (!keys_fine && !all_finite(v[i])) atomicMin(&bad_s, row);
-        K.put(row, sh.c8, v[i], sk.up);
+        K.put(row, sh.c8, v[i]);
     }
     if (w == 0) lgs[lane] = lg, bs[lane] = beta;
     __syncthreads();
     const int bad = bad_s;
     uint8_t *rec = a.ws + (static_cast<size_t>(x) * a.p.Hv + h) * a.record;
     if (w == 0) put_gates(reinterpret_cast<ChunkGates *>(rec), lane, lg, beta, bad);
-    if (tid == 0) reinterpret_cast<ChunkGates *>(rec)->kmax = kmax;
     // M: lane (g, n) holds row i = 16 w + n, columns 16 tt + 4 g .. + 3
-    f16x8 mine[DKP / 32][NA];
+    bf16x8 mine[DKP / 32][NA];
 #pragma unroll
     for (int kb = 0; kb < DKP / 32; ++kb) K.rows(w, kb, g, n, mine[kb]);
     const int row_i = 16 * w + n;
@@ -594,14 +534,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
         f32x4 c = {};
 #pragma unroll
         for (int kb = 0; kb < DKP / 32; ++kb) {
-            f16x8 k[NA];
+            bf16x8 k[NA];
             K.rows(tt, kb, g, n, k);
-            mma<2>(c, k, mine[kb]);
+            mma(c, k, mine[kb]);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int j = 16 * tt + 4 * g + r;
-            c[r] = j < row_i && row_i < bad ? bi * decay(lgs[j], lgi) * (c[r] * sk.down * sk.down) : 0.0f;
+            c[r] = j < row_i && row_i < bad ? bi * decay(lgs[j], lgi) * c[r] : 0.0f;
         }
         *reinterpret_cast<f32x4 *>(&M[row_i][16 * tt + 4 * g]) = c;
     }
@@ -642,7 +582,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
     }
     __syncthreads();
     // beta into the columns, then block by block to the record
-    uint32_t top = 0;
     for (int tt = 0; tt <= w; ++tt) {
         f32x4 *at = reinterpret_cast<f32x4 *>(&X[row_i][16 * tt + 4 * g]);
         f32x4 y = *at;
@@ -650,24 +589,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DKP == 64 ? 4 : 3) void prom
         for (int r = 0; r < 4; ++r) {
             const int j = 16 * tt + 4 * g + r;
             y[r] = j < bad ? y[r] * bs[j] : 0.0f;
-            top = max(top, __float_as_uint(fabsf(y[r])));
         }
         *at = y;
     }
-    top = wave_max(top);
-    if (lane == 0) atomicMax(&tmax_s, top);
     __syncthreads();
-    const uint32_t tmax = tmax_s;
-    if (tid == 0) reinterpret_cast<ChunkGates *>(rec)->tmax = tmax;
     for (int b = w; b < 6; b += 4) {
         const int rb = triangle_row(b), kb = triangle_block(b);
         const f32x4 lo = *reinterpret_cast<const f32x4 *>(&X[16 * rb + n][32 * kb + 4 * g]);
         const f32x4 hi = 2 * kb + 1 <= rb ? *reinterpret_cast<const f32x4 *>(&X[16 * rb + n][32 * kb + 16 + 4 * g]) : f32x4{};
-        f16x8 pl[2];
-        split(lo, hi, scale_for(tmax).up, pl);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<f16x8 *>(rec + sizeof(ChunkGates) + i * 6144 + b * 1024 + lane * 16) = pl[i];
+        f32x4 *to = reinterpret_cast<f32x4 *>(rec + sizeof(ChunkGates) + b * 2048) + 2 * lane;
+        to[0] = lo, to[1] = hi;
     }
 }
 
@@ -693,16 +624,6 @@ __device__ __forceinline__ const float *initial_state(const PromptArgs &a, int s
     return src >= 0 ? a.state_in + (static_cast<size_t>(src) * a.Hv + h) * a.dk * a.dv : nullptr;
 }
 
-__device__ __forceinline__ uint32_t tile_max(const f32x4 (&x)[4])
-{
-    float m = 0.0f;
-#pragma unroll
-    for (int rb = 0; rb < 4; ++rb)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[rb][r]));
-    return __float_as_uint(m);
-}
-
 // Long sequences with too few heads to fill the chip are cut into segments of
 // whole chunks.  A segment takes a state S to A S + B (decay rule: A = gamma I),
 // whatever S is, so that: a launch forms B of every segment by walking it from
@@ -716,7 +637,7 @@ constexpr int kSegmentHead = 64;         // floats; [0] = gamma
 // or of a segment of it (OUT false: for B and A, without outputs) for 16 NW value columns, a wave holds 16 columns of the state in registers
 // (result layout: lane n column n).  Every product with the state, and every
 // one after it, keeps the columns in their lanes, so that the waves share only
-// what is read, and each column of an operand has a power of two of its own.
+// what is read.
 //   Bound by the chain of a chunk: R needs S, U needs R, the next S needs U, and
 // 2 waves a SIMD (their state, R, O and the next chunk's tiles: 171 registers)
 // cover its waits only in part.  8 sequences of 1088 tokens x 32 heads, a
@@ -739,16 +660,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     constexpr int UQ = ShareQ::units, UV = ShareV::units;
     __shared__ RowTile<T, DKP> K;
     __shared__ std::conditional_t<OUT, RowTile<T, DKP>, char> Q;
-    __shared__ ValueTile<T, W> V;
-    __shared__ std::conditional_t<OUT, TriangleTile<2>, char> P;
-    __shared__ std::conditional_t<DELTA, TriangleTile<2>, char> Tt;
+    __shared__ std::conditional_t<sizeof(T) == 2, ValueTile<W>, char> V;
+    __shared__ std::conditional_t<OUT, TriangleTile, char> P;
+    __shared__ std::conditional_t<DELTA, TriangleTile, char> Tt;
     __shared__ struct alignas(16) {
         double lg[kC];
         float g[kC], w[kC], b[kC];
         int32_t bad;
-        uint32_t tmax;
     } ga;
-    __shared__ uint32_t tops[2][NW];
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
     // Addresses in LDS follow from the lane: formed again in each phase, they do not hold registers from chunk to chunk.
@@ -803,18 +722,21 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     // part in registers for as short as its latency allows: keys and queries
     // from the second barrier on, values and gates from the state's update on;
     // T' from the chunk's own first barrier to its third.
-    Act<T> kx[UQ], qx[OUT ? UQ : 1], vx[UV] = {};
-    constexpr int NP = (12 + NW - 1) / NW;           // 1 KB pieces of T' per wave
-    f16x8 tx[NP];
+    Act<T> kx[UQ], qx[OUT ? UQ : 1];
+    Act<bf16_t> vx[sizeof(T) == 2 ? UV : 1] = {};
+    f32x4 vf[sizeof(T) == 4 ? 4 : 1] = {};           // fp32 values: rows 16 rb + 4 g .. + 3 of the lane's column
+    constexpr int NT = (6 + NW - 1) / NW;            // blocks of T' per wave
+    f32x4 tx[NT][2];
     constexpr int NG = (kGateWords + 64 * NW - 1) / (64 * NW);
-    uint32_t gx[NG], kmax = 0;
+    uint32_t gx[NG];
     const auto record = [&](int c) { return records + static_cast<size_t>(c) * a.p.Hv * a.record; };
     // Whole chunks whose rows lie within 32-bit offsets: one lane offset per
     // array for all chunks, the rest in scalar registers.
     const bool near = VEC && a.near && a.p.dk == DKP;
     const uint32_t at_k = (sh.row * static_cast<uint32_t>(a.p.sk) + 8 * sh.c8) * static_cast<uint32_t>(sizeof(T));
     const uint32_t at_q = (sh.row * static_cast<uint32_t>(a.p.sq) + 8 * sh.c8) * static_cast<uint32_t>(sizeof(T));
-    const uint32_t at_v = (sv.row * static_cast<uint32_t>(a.p.sv) + 8 * sv.c8) * static_cast<uint32_t>(sizeof(T));
+    const uint32_t at_v = sizeof(T) == 2 ? (sv.row * static_cast<uint32_t>(a.p.sv) + 8 * sv.c8) * 2u
+                                         : (4 * g * static_cast<uint32_t>(a.p.sv) + n) * 4u;
     const auto fetch = [&](int c) {
         const int64_t t0 = be.x + c * kC;
         const int len = min(kC, be.y - static_cast<int>(t0));
@@ -833,22 +755,33 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
                 qx[i] = sh.template load<VEC>(static_cast<const T *>(a.p.q) + t0 * a.p.sq + hq * a.p.dk, a.p.sq, i, a.p.dk, len);
         }
     };
-    // values past the last token repeat it: their rows of U are 0 (beta is 0 there)
+    // bfloat16 values past the last token repeat it, fp32 ones are 0: their rows of U are 0 (beta is 0 there)
     const auto fetch_values = [&](int c) {
         const int64_t t0 = be.x + c * kC;
         const int len = min(kC, be.y - static_cast<int>(t0));
-        if (values && near && len == kC) {
+        const T *from = static_cast<const T *>(a.p.v) + t0 * a.p.sv + h * a.p.dv + col0;
+        if constexpr (sizeof(T) == 2) {
+            if (values && near && len == kC) {
 #pragma unroll
-            for (int i = 0; i < UV; ++i)
-                vx[i] = load_at(static_cast<const T *>(a.p.v) + (t0 + i * sv.step) * a.p.sv + h * a.p.dv + col0, at_v);
-        } else if (values)
+                for (int i = 0; i < UV; ++i) vx[i] = load_at(from + i * sv.step * a.p.sv, at_v);
+            } else if (values)
 #pragma unroll
-        for (int i = 0; i < UV; ++i)
-            vx[i] = sv.template load<VEC>(static_cast<const T *>(a.p.v) + t0 * a.p.sv + h * a.p.dv + col0, a.p.sv, i, W, len);
+            for (int i = 0; i < UV; ++i) vx[i] = sv.template load<VEC>(from, a.p.sv, i, W, len);
+        } else if (values) {
+            const auto load = [&](int m) {
+                const T *row = from + mycol;
+#pragma unroll
+                for (int rb = 0; rb < 4; ++rb, row += 12 * a.p.sv)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r, row += a.p.sv)
+                        vf[rb][r] = 16 * rb + 4 * g + r < m
+                                        ? *reinterpret_cast<const T *>(reinterpret_cast<const uint8_t *>(row) + at_v) : 0.0f;
+            };
+            len == kC ? load(kC) : load(len);
+        }
         const uint32_t *words = reinterpret_cast<const uint32_t *>(record(c));
 #pragma unroll
         for (int i = 0; i < NG; ++i) gx[i] = words[min(static_cast<int>(threadIdx.x) + 64 * NW * i, kGateWords - 1)];
-        if (DELTA) kmax = reinterpret_cast<const ChunkGates *>(words)->kmax;
     };
     if (chunks > first) fetch(first), fetch_values(first);
 
@@ -868,31 +801,27 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
             }
         }
         again();
-        if constexpr (!DELTA) tops[0][wv] = wave_max_of(kx);
-        if constexpr (OUT) tops[1][wv] = wave_max_of(qx);
         lds_barrier();
         const ChunkGates *cg = reinterpret_cast<const ChunkGates *>(record(c));
         if constexpr (DELTA) {
-            const f16x8 *from = reinterpret_cast<const f16x8 *>(cg + 1) + lane;
+            const f32x4 *from = reinterpret_cast<const f32x4 *>(cg + 1) + 2 * lane;
 #pragma unroll
-            for (int i = 0; i < NP; ++i) tx[i] = from[(wv + NW * i) % 12 * 64];
+            for (int i = 0; i < NT; ++i) {
+                const int b = min(wv + NW * i, 5) * 128;
+                tx[i][0] = from[b], tx[i][1] = from[b + 1];
+            }
         }
-        uint32_t mk = DELTA ? __builtin_amdgcn_readfirstlane(kmax) : 0, mq = 0;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            if (!DELTA) mk = max(mk, tops[0][i]);
-            if constexpr (OUT) mq = max(mq, tops[1][i]);
-        }
-        const Pow2 sk = scale_for(mk), sq = scale_for(mq);
         const auto at = sh.again();
 #pragma unroll
         for (int i = 0; i < UQ; ++i) {
-            K.put(at.row + at.step * i, at.c8, kx[i], sk.up);
-            if constexpr (OUT) Q.put(at.row + at.step * i, at.c8, qx[i], sq.up);
+            K.put(at.row + at.step * i, at.c8, kx[i]);
+            if constexpr (OUT) Q.put(at.row + at.step * i, at.c8, qx[i]);
         }
-        const auto av = sv.again();
+        if constexpr (sizeof(T) == 2) {
+            const auto av = sv.again();
 #pragma unroll
-        for (int i = 0; i < UV; ++i) V.put(av.row + av.step * i, av.c8, vx[i]);
+            for (int i = 0; i < UV; ++i) V.put(av.row + av.step * i, av.c8, vx[i]);
+        }
 #pragma unroll
         for (int i = 0; i < NG; ++i)
             reinterpret_cast<uint32_t *>(&ga)[min(static_cast<int>(threadIdx.x) + 64 * NW * i, kGateWords - 1)] = gx[i];
@@ -901,13 +830,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         const int bad = DELTA ? __builtin_amdgcn_readfirstlane(ga.bad) : kC;
 
         again();
-        // P times 2^-22 of the scales (|q.k| < 2^35 scaled), a block of 16 rows x 32 columns to a wave:
-        // lane (g, n) forms row i = 16 rb + n, columns 16 tt + 4 g .. + 3
+        // P, a block of 16 rows x 32 columns to a wave: lane (g, n) forms row i = 16 rb + n, columns 16 tt + 4 g .. + 3
         if constexpr (OUT)
 #pragma unroll
         for (int b = wv; b < 6; b += NW) {
             const int rb = triangle_row(b), pb = triangle_block(b);
-            f16x8 q[KB][NA];
+            bf16x8 q[KB][NA];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) Q.rows(rb, kb, g, n, q[kb]);
             const double lgi = ga.lg[16 * rb + n];
@@ -919,9 +847,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
                     f32x4 x = {};
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) {
-                        f16x8 k[NA];
+                        bf16x8 k[NA];
                         K.rows(tt, kb, g, n, k);
-                        mma<2>(x, k, q[kb]);
+                        mma(x, k, q[kb]);
                     }
                     float d[4];
 #pragma unroll
@@ -930,56 +858,50 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
                     for (int r = 0; r < 4; ++r) y[hh][r] = ((tt < rb) | (4 * g + r <= n)) ? d[r] : 0.0f;
                 }
             }
-            P.put(b, lane, y[0], y[1], 0x1p-22f);
+            P.put(b, lane, y[0], y[1]);
         }
         again();
         // K S and Q S
         f32x4 ks[4], o[4];
-        float sm = 0.0f;
-        if (OUT || DELTA)
-#pragma unroll
-        for (int rt = 0; rt < DKP / 16; ++rt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sm = fmaxf(sm, fabsf(S[rt][r]));
-        const Pow2 ss = scale_for(column_max(__float_as_uint(sm)));
 #pragma unroll
         for (int rb = 0; rb < 4; ++rb) ks[rb] = o[rb] = f32x4{};
 #pragma unroll
         for (int kb = 0; kb < (OUT || DELTA ? KB : 0); ++kb) {
-            f16x8 sp[2];
-            split(S[2 * kb], S[2 * kb + 1], ss.up, sp);
+            bf16x8 sp[3];
+            split(S[2 * kb], S[2 * kb + 1], sp);
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb) {
                 if constexpr (OUT) {
-                    f16x8 q[NA];
+                    bf16x8 q[NA];
                     Q.rows(rb, kb, g, n, q);
-                    mma<2>(o[rb], q, sp);
+                    mma(o[rb], q, sp);
                 }
                 if constexpr (DELTA) {
-                    f16x8 k[NA];
+                    bf16x8 k[NA];
                     K.rows(rb, kb, g, n, k);
-                    mma<2>(ks[rb], k, sp);
+                    mma(ks[rb], k, sp);
                 }
             }
         }
         // 3 steps' operands ahead (32 sequences: 537 -> 530 us); the update of S the same way is slower (541)
-        if constexpr (OUT && DELTA && sizeof(T) == 2) reads_ahead<4 * KB, 2, 4, 3>();
+        if constexpr (OUT && DELTA && sizeof(T) == 2) reads_ahead<4 * KB, 2, 6, 3>();
         again();
         // R (Delta) or U (decay), and whether it is finite; O's part from the state
         float z = 0.0f;
-        const float fk = -(sk.down * ss.down), fq = sq.down * ss.down;
 #pragma unroll
         for (int rb = 0; rb < 4; ++rb) {
             const f32x4 gg = *reinterpret_cast<const f32x4 *>(&ga.g[16 * rb + 4 * g]);
             f32x4 bb = {};
             if (!DELTA) bb = *reinterpret_cast<const f32x4 *>(&ga.b[16 * rb + 4 * g]);
-            const f32x4 v = V.four(rb, mycol, g, n);
+            f32x4 v;
+            if constexpr (sizeof(T) == 2) v = V.four(rb, mycol, g, n);
+            else v = vf[rb];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (DELTA) ks[rb][r] = fmaf(gg[r] * fk, ks[rb][r], v[r]);
+                if (DELTA) ks[rb][r] = fmaf(-gg[r], ks[rb][r], v[r]);
                 else ks[rb][r] = v[r] * bb[r];
                 z = fmaf(ks[rb][r], 0.0f, z);
-                if (OUT) o[rb][r] *= gg[r] * fq;
+                if (OUT) o[rb][r] *= gg[r];
             }
         }
         // tokens from `from` on are lost in their column: what is not finite there may not reach the others
@@ -1002,51 +924,40 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         }
         if constexpr (DELTA)
 #pragma unroll
-            for (int i = 0; i < NP; ++i)
-                *reinterpret_cast<f16x8 *>(&Tt.b[0][0] + (wv + NW * i) % 12 * 1024 + lane * 16) = tx[i];
+            for (int i = 0; i < NT; ++i)
+                if (wv + NW * i < 6) Tt.put(wv + NW * i, lane, tx[i][0], tx[i][1]);
         lds_barrier();
         again();
-        // U = T' R: in ks, times fu
-        float fu = 1.0f;
+        // U = T' R
         if constexpr (DELTA) {
-            const Pow2 sr = scale_for(column_max(tile_max(ks)));
-            const Pow2 st = scale_for(ga.tmax);
-            fu = st.down * sr.down;
-            f16x8 rp[2][2];
+            bf16x8 rp[2][3];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], sr.up, rp[kb]);
+            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], rp[kb]);
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb) {
                 ks[rb] = f32x4{};
 #pragma unroll
                 for (int kb = 0; kb <= rb / 2; ++kb) {
-                    f16x8 t[2];
+                    bf16x8 t[3];
                     Tt.rows(rb, kb, lane, t);
-                    mma<2>(ks[rb], t, rp[kb]);
+                    mma(ks[rb], t, rp[kb]);
                 }
             }
         }
-        const Pow2 su = scale_for(column_max(tile_max(ks)));
-        fu *= su.down;
         again();
         // O += P U
         if constexpr (OUT) {
-            f16x8 up[2][2];
+            bf16x8 up[2][3];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], su.up, up[kb]);
-            const float f = (sk.down * sq.down * 0x1p22f) * fu;
+            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], up[kb]);
 #pragma unroll
-            for (int rb = 0; rb < 4; ++rb) {
-                f32x4 y = {};
+            for (int rb = 0; rb < 4; ++rb)
 #pragma unroll
                 for (int kb = 0; kb <= rb / 2; ++kb) {
-                    f16x8 p[2];
+                    bf16x8 p[3];
                     P.rows(rb, kb, lane, p);
-                    mma<2>(y, p, up[kb]);
+                    mma(o[rb], p, up[kb]);
                 }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[rb][r] = fmaf(y[r], f, o[rb][r]);
-            }
         }
         if (OUT && lost)
 #pragma unroll
@@ -1074,26 +985,24 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         again();
         // S <- G_last S + K^T (w U)
         {
-            const float glast = ga.g[kC - 1], f = sk.down * fu;
+            const float glast = ga.g[kC - 1];
             if (!OUT) gamma *= glast;
-            f16x8 up[2][2];
+            bf16x8 up[2][3];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
                 const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&ga.w[32 * kb + 4 * g]);
                 const f32x4 w1 = *reinterpret_cast<const f32x4 *>(&ga.w[32 * kb + 16 + 4 * g]);
-                split(ks[2 * kb] * w0, ks[2 * kb + 1] * w1, su.up, up[kb]);
+                split(ks[2 * kb] * w0, ks[2 * kb + 1] * w1, up[kb]);
             }
 #pragma unroll
             for (int rt = 0; rt < DKP / 16; ++rt) {
-                f32x4 y = {};
+                S[rt] *= glast;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
-                    f16x8 k[NA];
+                    bf16x8 k[NA];
                     K.columns(rt, kb, g, n, k);
-                    mma<2>(y, k, up[kb]);
+                    mma(S[rt], k, up[kb]);
                 }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[rt][r] = fmaf(S[rt][r], glast, y[r] * f);
             }
         }
         if (lost && from < kC)
