@@ -363,8 +363,8 @@ typedef struct {
  *   one; an id outside [0, n_states_in): zeros), NULL: from state_in[i];
  *   state_out [n_seq][Hv][d_k][d_v] fp32: what stepq_pool_load packs.
  * alpha lies in [0, 1]: 0 forgets everything before the token, an alpha < 0
- * gives NaN.  state_out may be state_in itself (in place) when in_ids is NULL,
- * and must not overlap it otherwise.
+ * gives NaN from its token on.  state_out may be state_in itself (in place)
+ * when in_ids is NULL, and must not overlap it otherwise.
  * Sums, decays and states are fp32 or wider, products are formed from operands
  * of 24 bits (what falls below 2^-22 of a product is left out) with fp32's
  * exponents: a token's o does not depend on the size of others in its chunk.  o

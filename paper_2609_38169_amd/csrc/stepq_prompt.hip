@@ -43,7 +43,7 @@ constexpr int kC = 64;
 struct ChunkGates {
     double lg[kC];           // log2 G_i: differences of them stay exact where G itself is 0 or tiny
     float g[kC], w[kC], b[kC];
-    int32_t bad;             // first token whose key or gate is not finite (Delta; kC: none)
+    int32_t bad;             // first token whose key or gate is not finite, or whose alpha is below 0 (Delta; kC: none)
     int32_t pad[31];
 };
 static_assert(sizeof(ChunkGates) == 1408, "record size");
@@ -404,7 +404,7 @@ __device__ __forceinline__ double scan_gates(const PromptArgs &a, int t0, int n,
         const float al = a.alpha.at(at);
         *beta = a.beta.p ? a.beta.at(at) : 1.0f;
         lg = log2_gate(al);
-        *fine = fabsf(al) < INFINITY && fabsf(*beta) < INFINITY;
+        *fine = al >= 0.0f && al < INFINITY && fabsf(*beta) < INFINITY;      // no logarithm below 0
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {

@@ -135,3 +135,23 @@ def test_largest_finite_values(act, rule):
         stepq.stepq_prompt(*(t.to(DEV) for t in y), o, out, rule, cu_seqlens=torch.tensor([0, 64], dtype=torch.int32, device=DEV))
         outs.append((o, out))
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+@pytest.mark.parametrize("rule", [DECAY, DELTA])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("j", [5, 40, 77])
+def test_a_gate_below_zero(j, act, rule):
+    """NaN from its token on in its head, and nothing else."""
+    T = 130
+    outs = []
+    for a in (None, -0.5, -1e-30):
+        x = tokens(T, 2, 1, 64, 64, act, F32, 12)
+        if a is not None:
+            x[3][j, 1] = a
+        o, out = torch.empty((T, 2, 64), dtype=act, device=DEV), torch.empty((1, 2, 64, 64), device=DEV)
+        stepq.stepq_prompt(*(t.to(DEV) for t in x), o, out, rule, cu_seqlens=torch.tensor([0, T], dtype=torch.int32, device=DEV))
+        outs.append((o, out))
+    (o, out), *rest = outs
+    for po, pout in rest:
+        assert torch.equal(po[:j], o[:j]) and torch.equal(po[:, 0], o[:, 0]) and torch.equal(pout[0, 0], out[0, 0])
+        assert torch.isnan(po[j:, 1]).all() and torch.isnan(pout[0, 1]).all()
