@@ -368,7 +368,9 @@ typedef struct {
  * Sums, decays and states are fp32 or wider, products are formed from operands
  * of 24 bits (what falls below 2^-22 of a product is left out) with fp32's
  * exponents: a token's o does not depend on the size of others in its chunk.  o
- * is rounded once, to act_dtype. */
+ * is rounded once, to act_dtype.  Under the Delta rule beta |k|^2 <= 2 keeps the
+ * state bounded; beyond, it grows from token to token, and where the products of
+ * a chunk of 64 tokens pass fp32, its tokens are NaN from there on. */
 stepq_status stepq_prompt_workspace(const stepq_prompt_desc *desc, size_t *bytes);
 stepq_status stepq_prompt(const stepq_prompt_desc *desc, const int32_t *cu_seqlens, const void *q, const void *k,
                           const void *v, const void *alpha, const void *beta, void *o, const float *state_in,

@@ -29,6 +29,7 @@ using u32x2 = __attribute__((ext_vector_type(2))) uint32_t;
 // stands beside it in its row, column or tile.
 __device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&p)[3])
 {
+#pragma clang fp contract(off)              // of the value as rounded, whatever product it came from
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t a = __float_as_uint(x[2 * i]), b = __float_as_uint(x[2 * i + 1]);

@@ -43,7 +43,7 @@ constexpr int kC = 64;
 struct ChunkGates {
     double lg[kC];           // log2 G_i: differences of them stay exact where G itself is 0 or tiny
     float g[kC], w[kC], b[kC];
-    int32_t bad;             // first token whose key or gate is not finite, or whose alpha is below 0 (Delta; kC: none)
+    int32_t bad;             // Delta: first token whose key, gate or row of T' is not finite, or whose alpha is below 0 (kC: none)
     int32_t pad[31];
 };
 static_assert(sizeof(ChunkGates) == 1408, "record size");
@@ -414,14 +414,13 @@ __device__ __forceinline__ double scan_gates(const PromptArgs &a, int t0, int n,
     return lg;
 }
 
-__device__ __forceinline__ void put_gates(ChunkGates *r, int lane, double lg, float beta, int bad)
+__device__ __forceinline__ void put_gates(ChunkGates *r, int lane, double lg, float beta)
 {
     const double last = __shfl(lg, 63);
     r->lg[lane] = lg;
     r->g[lane] = decay(0.0, lg);
     r->w[lane] = decay(lg, last);
     r->b[lane] = beta;
-    if (lane == 0) r->bad = bad;
 }
 
 // A wave puts sequence s in its place among the sequences, longest first.
@@ -456,7 +455,7 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
     float beta;
     bool fine;
     const double lg = scan_gates(a.p, t0, n, h, lane, &beta, &fine);
-    put_gates(reinterpret_cast<ChunkGates *>(a.ws + id * a.record), lane, lg, beta, kC);
+    put_gates(reinterpret_cast<ChunkGates *>(a.ws + id * a.record), lane, lg, beta);
 }
 
 // First launch, Delta rule: a workgroup per (chunk, head) forms T'.  Wave w owns
@@ -469,6 +468,9 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
 // inverse takes the keys' place in LDS) beat 3 with more registers: 32 sequences
 // 174 -> 139 us.  8 sequences of 1088 tokens x 32 heads: 51 us, 2.5 TB/s of keys
 // read and T' written.
+//   With beta |k|^2 beyond 2 the recurrence grows, and rows of T' may pass fp32:
+// their tokens and those after them are lost, and 0 stands in their place, so
+// that no product takes them to a row before.
 template <typename T, int DKP, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void prompt_solve_kernel(ChunkArgs a)
 {
@@ -522,7 +524,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void p
     __syncthreads();
     const int bad = bad_s;
     uint8_t *rec = a.ws + (static_cast<size_t>(x) * a.p.Hv + h) * a.record;
-    if (w == 0) put_gates(reinterpret_cast<ChunkGates *>(rec), lane, lg, beta, bad);
+    if (w == 0) put_gates(reinterpret_cast<ChunkGates *>(rec), lane, lg, beta);
     // M: lane (g, n) holds row i = 16 w + n, columns 16 tt + 4 g .. + 3
     bf16x8 mine[DKP / 32][NA];
 #pragma unroll
@@ -530,6 +532,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void p
     const int row_i = 16 * w + n;
     const double lgi = lgs[row_i];
     const float bi = bs[row_i];
+    const auto finite_or_lost = [&](float y, int row) {
+        if (fabsf(y) < INFINITY) return y;
+        atomicMin(&bad_s, row);
+        return 0.0f;
+    };
     for (int tt = 0; tt <= w; ++tt) {
         f32x4 c = {};
 #pragma unroll
@@ -541,7 +548,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void p
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int j = 16 * tt + 4 * g + r;
-            c[r] = j < row_i && row_i < bad ? bi * decay(lgs[j], lgi) * c[r] : 0.0f;
+            c[r] = j < row_i && row_i < bad ? finite_or_lost(bi * decay(lgs[j], lgi) * c[r], row_i) : 0.0f;
         }
         *reinterpret_cast<f32x4 *>(&M[row_i][16 * tt + 4 * g]) = c;
     }
@@ -572,12 +579,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void p
                 for (int r = 0; r < 4; ++r)
                     y = __builtin_amdgcn_mfma_f32_16x16x4f32(m[r], X[16 * l + 4 * g + r][16 * c + n], y, 0, 0, 0);
             }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = finite_or_lost(y[r], 16 * w + 4 * g + r);
             const f32x4 tw = *reinterpret_cast<const f32x4 *>(&X[16 * w + n][16 * w + 4 * g]);
             f32x4 z = {};
 #pragma unroll
             for (int r = 0; r < 4; ++r) z = __builtin_amdgcn_mfma_f32_16x16x4f32(tw[r], y[r], z, 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) X[16 * w + 4 * g + r][16 * c + n] = -z[r];
+            for (int r = 0; r < 4; ++r) X[16 * w + 4 * g + r][16 * c + n] = -finite_or_lost(z[r], 16 * w + 4 * g + r);
         }
     }
     __syncthreads();
@@ -588,11 +597,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void p
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int j = 16 * tt + 4 * g + r;
-            y[r] = j < bad ? y[r] * bs[j] : 0.0f;
+            y[r] = j < bad ? finite_or_lost(y[r] * bs[j], row_i) : 0.0f;
         }
         *at = y;
     }
     __syncthreads();
+    if (tid == 0) reinterpret_cast<ChunkGates *>(rec)->bad = bad_s;
     for (int b = w; b < 6; b += 4) {
         const int rb = triangle_row(b), kb = triangle_block(b);
         const f32x4 lo = *reinterpret_cast<const f32x4 *>(&X[16 * rb + n][32 * kb + 4 * g]);
@@ -886,8 +896,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         // 3 steps' operands ahead (32 sequences: 537 -> 530 us); the update of S the same way is slower (541)
         if constexpr (OUT && DELTA && sizeof(T) == 2) reads_ahead<4 * KB, 2, 6, 3>();
         again();
-        // R (Delta) or U (decay), and whether it is finite; O's part from the state
-        float z = 0.0f;
+        // R (Delta) or U (decay); O's part from the state
 #pragma unroll
         for (int rb = 0; rb < 4; ++rb) {
             const f32x4 gg = *reinterpret_cast<const f32x4 *>(&ga.g[16 * rb + 4 * g]);
@@ -900,16 +909,28 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
             for (int r = 0; r < 4; ++r) {
                 if (DELTA) ks[rb][r] = fmaf(-gg[r], ks[rb][r], v[r]);
                 else ks[rb][r] = v[r] * bb[r];
-                z = fmaf(ks[rb][r], 0.0f, z);
                 if (OUT) o[rb][r] *= gg[r];
             }
         }
-        // tokens from `from` on are lost in their column: what is not finite there may not reach the others
-        // through products with zeros, so it is taken out and put in its place at the end
-        const bool lost = bad < kC || __any(z != 0.0f);
-        int from = kC;
-        if (lost) {
-            from = bad;
+        // Tokens from `from` on are lost in their column: what is not finite there may not reach the others
+        // through products with zeros, so it is taken out of an operand and put in its place at the end.  A
+        // product of the operand with zeros tells (the final state needs no care: it has all tokens).
+        bool lost = false;
+        int from = bad;
+        const auto operand = [&](bf16x8 (&p)[2][3], bool cut) {
+            const auto form = [&] {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], p[kb]);
+            };
+            form();
+            if constexpr (OUT) {
+                f32x4 z = {};
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16x8{}, p[kb][0], z, 0, 0, 0);
+                cut |= __any(z[0] != 0.0f);
+            }
+            if (!cut) return;
+            lost = true;
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
 #pragma unroll
@@ -921,7 +942,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     if (16 * rb + 4 * g + r >= from) ks[rb][r] = 0.0f;
-        }
+            form();
+        };
         if constexpr (DELTA)
 #pragma unroll
             for (int i = 0; i < NT; ++i)
@@ -931,8 +953,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         // U = T' R
         if constexpr (DELTA) {
             bf16x8 rp[2][3];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], rp[kb]);
+            operand(rp, bad < kC);
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb) {
                 ks[rb] = f32x4{};
@@ -948,8 +969,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
         // O += P U
         if constexpr (OUT) {
             bf16x8 up[2][3];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) split(ks[2 * kb], ks[2 * kb + 1], up[kb]);
+            operand(up, false);              // U may pass fp32 where R did not
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
 #pragma unroll

@@ -155,3 +155,33 @@ def test_a_gate_below_zero(j, act, rule):
     for po, pout in rest:
         assert torch.equal(po[:j], o[:j]) and torch.equal(po[:, 0], o[:, 0]) and torch.equal(pout[0, 0], out[0, 0])
         assert torch.isnan(po[j:, 1]).all() and torch.isnan(pout[0, 1]).all()
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("how", ["random keys of norm 16", "equal keys of norm 8", "two keys of norm 2^70"])
+def test_growth_past_fp32(how, act):
+    """A state that passes fp32 inside a chunk does not reach the tokens before: those whose terms (of T's rows as of
+    the outputs) are below 2^110 are what they are."""
+    T = 64
+    x = tokens(T, 2, 1, 64, 64, act, F32, 13)
+    if how.startswith("two"):
+        x[1][40:42] *= 2.0 ** 70
+    else:
+        x[1].mul_(16.0 if how.startswith("random") else 8.0)
+        if how.startswith("equal"):
+            x[1][:] = x[1][:1]
+    S = torch.zeros(2, 64, 64)
+    o, out = torch.empty((T, 2, 64), dtype=act, device=DEV), torch.empty((1, 2, 64, 64), device=DEV)
+    stepq.stepq_prompt(*(t.to(DEV) for t in x), o, out, DELTA, cu_seqlens=torch.tensor([0, T], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    ro, _ = recurrence(*x, S, DELTA)
+    mo, _ = magnitude(*x, S, DELTA)
+    # T's rows, |M| |T| within them: what a token's u would be of values of size 1 everywhere
+    rows, _ = magnitude(torch.ones_like(x[0]), x[1], torch.ones_like(x[2]), x[3], x[4], S, DELTA)
+    safe = ((mo.amax((1, 2)) < 2.0 ** 110) & (rows.amax((1, 2)) < 2.0 ** 110)).tolist()
+    n = safe.index(False) if False in safe else T
+    assert 12 <= n < T                          # it does pass, and not at once
+    off = (o[:n].cpu().double() - ro[:n]).abs()
+    worst = (off / (3e-5 * mo[:n] + (0 if act == F32 else 2.0 ** -8) * ro[:n].abs())).amax((1, 2))
+    assert (worst <= 1).all(), (n, worst)
+    assert torch.isnan(o[T - 1]).all() and torch.isnan(out).all()
