@@ -354,8 +354,9 @@ typedef struct {
 /* Prompts: every token of n_seq packed sequences through the recurrence, from
  * an initial state to the final one, in chunks on the matrix cores.  Sequence
  * i is tokens cu_seqlens[i] .. cu_seqlens[i+1] (device, int32 [n_seq+1], from
- * 0 up and never down; empty sequences keep their initial state); cu_seqlens
- * NULL with n_seq = 1: one sequence of all tokens.
+ * 0 up and never down; empty sequences keep their initial state; what lies before
+ * the first is not touched); cu_seqlens NULL with n_seq = 1: one sequence of all
+ * tokens.
  *   q, k [n_tokens][Hqk][d_k], v, o [n_tokens][Hv][d_v] in act_dtype (token
  *   strides above), alpha, beta [n_tokens][Hv] in gate_dtype, beta NULL: 1;
  *   state_in [n_states_in][Hv][d_k][d_v] fp32, NULL: zeros; in_ids [n_seq]

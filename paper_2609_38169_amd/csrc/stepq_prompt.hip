@@ -450,8 +450,8 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
     if (a.order && x < a.p.n_seq && h == 0) put_order(a, x, lane);       // there are at least as many slots
     const int s = owner(a.p, x, lane);
     const int2 be = seq_bounds(a.p, s);
-    const int t0 = be.x + (x - first_slot(a.p, s)) * kC, n = min(kC, be.y - t0);
-    if (n <= 0) return;
+    const int c = x - first_slot(a.p, s), t0 = be.x + c * kC, n = min(kC, be.y - t0);
+    if (c < 0 || n <= 0) return;
     float beta;
     bool fine;
     const double lg = scan_gates(a.p, t0, n, h, lane, &beta, &fine);
@@ -492,9 +492,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : DKP == 64 ? 3 : 2) void p
     if (a.order && x < a.p.n_seq && h == 0 && w == 0) put_order(a, x, lane);     // there are at least as many slots
     const int s = owner(a.p, x, lane);
     const int2 be = seq_bounds(a.p, s);
-    const int64_t t0 = be.x + (x - first_slot(a.p, s)) * kC;
+    const int chunk = x - first_slot(a.p, s);
+    const int64_t t0 = be.x + chunk * kC;
     const int len = min(kC, be.y - static_cast<int>(t0));
-    if (len <= 0) return;
+    if (chunk < 0 || len <= 0) return;
     if (tid == 0) bad_s = kC;
     Act<T> v[U];
 #pragma unroll
@@ -704,7 +705,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
     }
     const int total = (be.y - be.x + kC - 1) / kC, part = a.seg ? item - first_slot(a.p, s, kC * a.seg) : 0;
     const int first = part * a.seg, chunks = a.seg ? min(total, first + a.seg) : total;
-    if (part > 0 && first >= total) return;
+    if (part < 0 || (part > 0 && first >= total)) return;        // tokens before the first sequence, or a slot that none has
     if (!OUT && chunks == total) return;         // nothing follows it
     float *rec = a.seg ? a.segs + (static_cast<size_t>(item) * a.p.Hv + h) * a.seg_floats : nullptr;
     const uint8_t *records = a.ws + (static_cast<size_t>(be.x / kC + s) * a.p.Hv + h) * a.record;
