@@ -601,13 +601,16 @@ Split split_of(const stepq_attn_desc *d)
         return want <= 16 ? want : std::max<int64_t>(16, std::min(want, ceil_div(len, 256)));
     };
     if (d->prefix_len) {
-        // attn_rows_kernel reads the prefix again for every 16 rows, which the caches serve up to a point; beyond
-        // 150 MB in all the product costs less.  Whole calls, rows / product, us, D = 64, 1024 tokens, 2 heads: 17 MB
-        // 11 / 19, 134 MB 22 / 24; D = 128, 1024 tokens, 8 heads: 34 MB 12 / 22, 134 MB 28 / 31, 268 MB 46 / 43; 4096
-        // tokens: 134 MB 23 / 25, 268 MB 34 / 31; D = 256, 2048 tokens, 2 heads: 34 MB 19 / 34, 134 MB 38 / 42, 268 MB
-        // 48 / 44; 512 requests over 16384 tokens: 17 GB
-        s.product = d->act_dtype == STEPQ_BF16 &&
-                    static_cast<double>(ceil_div(rows, 16)) * d->prefix_len * d->n_kv_heads * d->head_dim * 4 > 150e6;
+        // attn_rows_kernel reads the prefix once for every 16 rows; the product reads it once for 256 and computes
+        // 256 however few there are.  It pays where more than 130 MB are read again, and from 33 rows on at D = 256
+        // (whose rows take most registers in the other kernel), 65 otherwise.  Whole calls, rows / product, us:
+        //   D = 256, 2 heads, 134 MB of prefix: 4 rows 47 / 62, 32 65 / 63, 48 93 / 65, 128 121 / 72, 512 385 / 129;
+        //     8 heads, 67 MB: 32 37 / 41, 48 45 / 42 (134 MB again), 64 51 / 43; 17 MB: 128 42 / 43 (119 MB), 256 57 / 54
+        //   D = 128, 8 heads, 268 MB: 4 52 / 108, 32 58 / 114, 64 95 / 115, 128 169 / 120; 17 MB: 128 25 / 29, 256 35 /
+        //     32; 1 head, 134 MB: 48 74 / 70, 64 92 / 70, 128 167 / 73
+        //   D = 64, 2 heads, 134 MB: 4 37 / 90, 48 71 / 82, 64 86 / 82, 128 106 / 83; 17 MB: 128 22 / 29, 256 32 / 31
+        const double again = static_cast<double>(ceil_div(rows, 16) - 1) * d->prefix_len * d->n_kv_heads * d->head_dim * 4;
+        s.product = d->act_dtype == STEPQ_BF16 && again > 130e6 && rows > (d->head_dim == 256 ? 32 : 64);
         const int64_t blocks = d->n_kv_heads * ceil_div(rows, s.product ? 256 : 16), most = ceil_div(d->prefix_len, 256);
         int64_t parts = s.product ? std::clamp<int64_t>(ceil_div(256, blocks), 1, most) : ranges(blocks, d->prefix_len);
         // whole rounds of the 8 XCDs where that costs few parts
