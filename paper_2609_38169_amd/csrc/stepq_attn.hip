@@ -67,6 +67,15 @@ __device__ __forceinline__ float swap_add32(float x)
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
+// The scale goes into the exponent, one fma from a score: rounded before the maximum is taken off, scores of 4096
+// and more would lose what tells them apart.  That needs it positive (the maximum is taken before): its sign goes
+// into the queries, and 0 makes them 0.
+__device__ __forceinline__ float scale_of(const AttnArgs &a) { return a.scale == 0.0f ? 1.0f : fabsf(a.scale); }
+__device__ __forceinline__ u32x4 with_sign(u32x4 q, float scale, uint32_t signs)
+{
+    return scale > 0.0f ? q : scale == 0.0f ? u32x4{} : q ^ signs;
+}
+
 // A running softmax: maximum and sum of what was seen; next() returns the
 // factor on everything so far when scores of maximum m join.
 struct Running {
@@ -147,7 +156,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnAr
     Piece q[QF];
 #pragma unroll
     for (int i = 0; i < QF; ++i)
-        q[i] = reinterpret_cast<const Piece *>(static_cast<const T *>(a.q) + qrow * D)[4 * i + g];
+        q[i] = __builtin_bit_cast(Piece, with_sign(reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.q) + qrow * D)[4 * i + g],
+                                                   a.scale, BF ? 0x80008000u : 0x80000000u));
+    const float scale = scale_of(a);
 
     const uint8_t *K = static_cast<const uint8_t *>(a.k), *V = static_cast<const uint8_t *>(a.v);
     Running run;
@@ -197,17 +208,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnAr
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const bool none = __shfl(at, 16 * rt + 4 * g + r) < 0;
-                s[rt][r] = none ? -INFINITY : s[rt][r] * a.scale;
+                if (none) s[rt][r] = -INFINITY;
                 top = fmaxf(top, s[rt][r]);
             }
         }
         if (more) at = next_at, fetch_keys();
-        const float f = run.next(swap_max32(swap_max16(top)));
+        const float f = run.next(swap_max32(swap_max16(top)) * scale);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                s[rt][r] = __builtin_amdgcn_exp2f(s[rt][r] - run.base);
+                s[rt][r] = __builtin_amdgcn_exp2f(fmaf(s[rt][r], scale, -run.base));
                 run.l += s[rt][r];
             }
 #pragma unroll
@@ -351,16 +362,11 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
         q[kb] = reinterpret_cast<const bf16x8 *>(static_cast<const bf16_t *>(a.q) + qrow * D)[2 * kb + h];
-    // the scale goes into the exponent, which needs it positive (the maximum is taken before): its sign goes
-    // into the queries, and 0 makes them 0
-    const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
-    if (!(a.scale > 0.0f)) {
+    const float scale = scale_of(a);
+    if (!(a.scale > 0.0f))
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            const u32x4 w = __builtin_bit_cast(u32x4, q[kb]);
-            q[kb] = __builtin_bit_cast(bf16x8, a.scale == 0.0f ? u32x4{} : w ^ 0x80008000u);
-        }
-    }
+        for (int kb = 0; kb < KB; ++kb)
+            q[kb] = __builtin_bit_cast(bf16x8, with_sign(__builtin_bit_cast(u32x4, q[kb]), a.scale, 0x80008000u));
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(q[kb]));   // there before the loop: nothing in it waits for them
     const uint8_t *K = static_cast<const uint8_t *>(a.k), *V = static_cast<const uint8_t *>(a.v);
