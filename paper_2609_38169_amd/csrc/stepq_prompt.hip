@@ -1210,15 +1210,17 @@ stepq_status check(const stepq_prompt_desc *d)
 // cost a walk of their own for B (Delta rule: and one for A), and a step of the
 // join each, of which more than about the root of the chunks' number are not
 // worth it.  Whole against segments, heads of 128 x 128, us:
-//   Delta, 32 heads: 16 chunks 111 / 91 (8 segments), 32 chunks 209 / 123, 128
-//     chunks 815 / 336; 8 chunks 62 / 62; 8 heads, 64 chunks 391 / 115 (16); 96
-//     heads, 64 chunks 445 / 413 (2), 16 chunks 121 / 137; 128 heads, 64 chunks
-//     466 / 511 (2); 5 ragged fp32 sequences of 6 heads, 12 chunks each on the
-//     average, 200 / 93 (6);
-//   decay, 32 heads: 8 chunks 50 / 39 (8), 32 chunks 167 / 64, 128 chunks 647 /
-//     168, 512 chunks 2572 / 600, and 539 with 24; 4 chunks 29 / 36 (4); 64 heads,
-//     16 chunks 91 / 63 (4); 128 heads, 64 chunks 330 / 278 (4), 16 chunks
-//     90 / 107; 160 heads, 32 chunks 172 / 190 (3).
+//   Delta, 32 heads: 6 chunks 54 / 55 (6 segments), 8 chunks 67 / 58 (6), 16
+//     chunks 121 / 87 (8), 32 chunks 228 / 120, 128 chunks 882 / 319; 64 heads, 8
+//     chunks 69 / 74 (4), 16 chunks 125 / 117 (4); 8 heads, 64 chunks 431 / 118
+//     (16); 96 heads, 64 chunks 495 / 449 (2), 16 chunks 135 / 149; 128 heads, 16
+//     chunks 139 / 157 (2), 32 chunks 265 / 270 (2); 5 ragged fp32 sequences of 6
+//     heads, 12 chunks each on the average, 167 / 88 (12);
+//   decay, 32 heads: 8 chunks 50 / 38 (8), 32 chunks 174 / 62, 128 chunks 671 /
+//     155, 256 chunks 1366 / 281 (8; 16: 304, 24: 329), 512 chunks 2717 / 548 (8;
+//     24: 606); 4 chunks 29 / 35 (4); 8 heads, 512 chunks 2674 / 159 (32); 64 heads,
+//     16 chunks 92 / 63 (4), 256 chunks 1380 / 532 (4; 12: 600); 128 heads, 64
+//     chunks 368 / 287 (4), 16 chunks 94 / 106; 152 heads, 32 chunks 181 / 187 (3).
 int32_t segment_chunks(const stepq_prompt_desc *d)
 {
     const int64_t pairs = int64_t(d->n_seq) * d->n_v_heads, each = d->n_seq ? slots(d) / d->n_seq : 0;
@@ -1228,9 +1230,9 @@ int32_t segment_chunks(const stepq_prompt_desc *d)
     int64_t parts;
     if (delta) {
         parts = std::min(256 / pairs, 2 * root);
-        if (parts < 2 || longest * parts < 6 * parts + 52) return 0;
+        if (parts < 2 || (longest + 4) * parts < 72) return 0;
     } else {
-        parts = std::min({(each >= 256 ? 768 : pairs <= 64 ? 256 : 512) / pairs, 4 * root, each});
+        parts = std::min({(pairs <= 64 ? 256 : 512) / pairs, 4 * root, each});
         if (parts < 2 || longest < (pairs <= 64 ? 8 : 32)) return 0;
     }
     return static_cast<int32_t>((each + parts - 1) / parts);
