@@ -269,6 +269,8 @@ bool take_long(PyObject *o, int64_t *out)
     return false;
 }
 
+bool take_rule(PyObject *o, int64_t *out) { return take_long(o, out) && *out == static_cast<int32_t>(*out); }
+
 const at::Tensor *tensor_of(PyObject *o, int64_t dims)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
@@ -326,7 +328,7 @@ PyObject *py_state_step(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const at::Tensor *S = tensor_of(a[0], 4), *q = tensor_of(a[2], 3), *v = tensor_of(a[4], 3);
         Plain p{};
         int64_t rule;
-        if (!S || !q || !v || !take_device(*q, &p) || !take_long(a[8], &rule)) return -1;
+        if (!S || !q || !v || !take_device(*q, &p) || !take_rule(a[8], &rule)) return -1;
         const int64_t B = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2), n = S->size(0);
         const at::ScalarType dt = q->scalar_type();
         void *sp, *ip, *qp, *kp, *vp, *ap, *bp, *op, *st;
@@ -357,7 +359,7 @@ PyObject *py_prompt(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const at::Tensor *q = tensor_of(a[0], 3), *v = tensor_of(a[2], 3), *cu = a[8] == Py_None ? nullptr : tensor_of(a[8], 1);
         Plain p{};
         int64_t rule;
-        if (!q || !v || (a[8] != Py_None && (!cu || cu->size(0) < 1)) || !take_device(*q, &p) || !take_long(a[7], &rule)) return -1;
+        if (!q || !v || (a[8] != Py_None && (!cu || cu->size(0) < 1)) || !take_device(*q, &p) || !take_rule(a[7], &rule)) return -1;
         const int64_t T = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2);
         const int64_t n = cu ? cu->size(0) - 1 : 1;
         const at::ScalarType dt = q->scalar_type();

@@ -557,8 +557,16 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _whole(x, name, bits):
+    """A whole number that a descriptor's field of `bits` holds (what it means is the library's to check)."""
+    n = int(x)
+    if n != x or not -2 ** (bits - 1) <= n < 2 ** (bits - 1):
+        raise ValueError(f"{name} must be a whole number of {bits} bits, not {x}")
+    return n
+
+
 def _prompt_desc(T, n_seq, Hv, Hqk, dk, dv, act, gate, rule, n_in, strides):
-    return stepq_prompt_desc(T, n_seq, Hv, Hqk, dk, dv, act, gate, int(rule), n_in, *strides)
+    return stepq_prompt_desc(T, n_seq, Hv, Hqk, dk, dv, act, gate, _whole(rule, "rule", 32), n_in, *strides)
 
 
 def stepq_prompt_workspace(n_tokens, n_seq, n_v_heads, n_qk_heads, d_k, d_v, rule, act_dtype=torch.bfloat16) -> int:
@@ -630,7 +638,7 @@ def stepq_state_step(state, ids, q, k, v, alpha, beta, o, rule=STEPQ_RULE_DELTA,
     if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3 or not isinstance(state, torch.Tensor) or state.dim() != 4:
         raise ValueError("q and v must be [B][heads][d], state [n][Hv][d_k][d_v]")
     (B, Hqk, dk), (Hv, dv) = q.shape, v.shape[1:]
-    d = stepq_state_desc(state.shape[0], Hv, Hqk, dk, dv, code, 0, int(rule))
+    d = stepq_state_desc(state.shape[0], Hv, Hqk, dk, dv, code, 0, _whole(rule, "rule", 32))
     ap, bp, d.gate_dtype = _gates(alpha, beta, (B, Hv), dev)
     _check(lib().stepq_state_step(
         ctypes.byref(d), _dev(state, "state", torch.float32, (state.shape[0], Hv, dk, dv), dev),
@@ -667,7 +675,7 @@ def stepq_prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_t
     n_pages, Hkv, page = k_cache.shape[:3]
     if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be [B][pages]")
-    prefix_len = int(prefix_len)
+    prefix_len = _whole(prefix_len, "prefix_len", 64)
     if prefix_len < 0 or page < 1:
         raise ValueError("prefix_len must be >= 0 and pages hold at least one token")
     P = -(-prefix_len // page)
