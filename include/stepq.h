@@ -413,8 +413,11 @@ typedef struct {
 /* Softmax attention of one query token of each of `batch` requests over the
  * tokens of a prefix they all share, then their own:
  *   o = sum_t p_t v_t,  p = softmax over t of scale q.k_t,  lse = log sum_t exp(scale q.k_t).
- * The prefix is read once for the whole batch, its products being matrix
- * products over all requests' queries; each request's own tokens are read once.
+ * The prefix is read once for every 16 query rows of a key/value head (a row is
+ * a request's head), or, where that would read much of it again, once for every
+ * 256, its products being matrix products then (bfloat16); a request's own tokens
+ * are read once for every 16 of its heads that share them.  Scores, weights and
+ * sums are the same in both: fp32, bfloat16 weights in 16 bits.
  *   k_cache, v_cache [n_pages][Hkv][page_size][D];
  *   prefix_pages [ceil(prefix_len / page_size)] int32: the prefix's pages;
  *   page_table [batch][max_pages] int32, lengths [batch] int32: request b's own

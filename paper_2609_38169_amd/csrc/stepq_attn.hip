@@ -96,7 +96,7 @@ struct Running {
 // and go into the second product as they are; values pass through LDS of the
 // wave's own to be read by columns.  Bound by the bytes of the caches: 64
 // requests x 8 key/value heads x 1-1024 tokens of 128 bfloat16 (134 MB) in 28.5 us,
-// 4.7 TB/s.  512 x 2 x 1-256 tokens of 256 (134 MB) take 51 us, 2.6 TB/s: a wave
+// 4.7 TB/s.  512 x 2 x 1-256 tokens of 256 (134 MB) take 50 us, 2.7 TB/s: a wave
 // has one tile or two there, and its registers (400) leave 4 waves a CU to wait
 // with; at 256 registers they spill.  4 requests over 512 + 64 tokens: 6.6 us, latency.
 template <typename T>
@@ -319,14 +319,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_rows_kernel(AttnAr
 // it is passed by 2^6, so that the outputs are rescaled a few times in all.  The
 // weights go into the second product in two bfloat16 planes (16 bits), as in
 // attn_rows_kernel: a request gets the same precision in any batch.  In one plane
-// (8 bits) 512 requests over 16384 tokens of 256 took 212 us in all, not 261, and
+// (8 bits) 512 requests over 16384 tokens of 256 took 212 us in all, not 262, and
 // the error of o was 2.2e-3, not the 1.7e-3 of its own rounding.
 //   Bound by the matrix cores and the LDS reads that feed them (D = 256: the
 // queries and the output fill the registers, so a key block read from LDS serves
 // 32 queries only, and both take the same time at their best).  4096 rows a head
-// x 16384 tokens x 256, 2 heads: 137 GFLOP in 159 us, 0.86 PFLOP/s, 0.7 of a
-// large library product's rate; 256 rows x 4096 x 128, 8 heads (the queries of 64
-// requests): 19 us.
+// x 16384 tokens x 256, 2 heads: 137 GFLOP in 193 us, 0.71 PFLOP/s, 0.57 of a
+// large library product's rate (a half more with the weights' second plane, which
+// the matrix cores compute too); 256 rows x 4096 x 128, 8 heads (the queries of 64
+// requests): 21 us.
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
 {
@@ -516,6 +517,9 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
 // counts; a request over 16384 tokens, 16 heads of 256 in 65 parts, in all: 37 us
 // with one load after the other in a wave, 20 so.  More: a wave each, bound by
 // the parts' bytes; 9 x 8192 rows of 256 (75 MB) in 14 us, 3 more with 4 waves.
+// Whole calls, one wave / 4, us, 64 dimensions over 1024 tokens: 32 rows 8.6 / 7.3,
+// 1024 13.5 / 12.1, 2048 17.9 / 17.1, 8192 48 / 50; 256 over 4096: 128 19.3 / 17.5,
+// 1024 51.5 / 50.7, 2048 50.5 / 53.2, 16384 178 / 185.
 // (Joined in attn_rows_kernel instead, which has few waves to wait with, 512
 // requests take 225 us in all, not 208.)
 template <typename T, int D, int W>

@@ -33,7 +33,8 @@ struct PromptArgs {
 // the value itself) each but for bfloat16 keys and queries, which are one.  Their
 // exponents are fp32's: tokens of very different size share a chunk, and with
 // two binary16 planes under a power of two for a tile or a column (22 bits; 32
-// sequences 485 us, not 540) a token 2^28 times the others left nothing of those before it.
+// sequences 485 us, not 533; 24 fp32 ones 78, not 98) a token 2^28 times the others
+// left nothing of those before it.
 // T' and the gates' products depend on no state: a first launch forms them
 // for every chunk at once; the second walks each sequence's chunks in order.
 constexpr int kC = 64;
@@ -466,8 +467,9 @@ __global__ __launch_bounds__(256) void prompt_gates_kernel(ChunkArgs a)
 // M is 4 % of a chunk's products; what counts is the chain of 16 substitution
 // steps and 3 rounds of blocks, so that 4 waves a SIMD (128 registers; the
 // inverse takes the keys' place in LDS) beat 3 with more registers: 32 sequences
-// 174 -> 139 us.  8 sequences of 1088 tokens x 32 heads: 51 us, 2.5 TB/s of keys
-// read and T' written.
+// 174 -> 139 us.  8 sequences of 1088 tokens x 32 heads: 53 us, 2.4 TB/s of keys
+// read and T' written.  T' goes to the workspace in fp32, 4 bytes an entry where
+// its three planes are 6.
 //   With beta |k|^2 beyond 2 the recurrence grows, and rows of T' may pass fp32:
 // their tokens and those after them are lost, and 0 stands in their place, so
 // that no product takes them to a row before.
@@ -645,21 +647,23 @@ __device__ __forceinline__ const float *initial_state(const PromptArgs &a, int s
 constexpr int kSegmentHead = 64;         // floats; [0] = gamma
 
 // Second launch: a workgroup of NW waves walks the chunks of one (sequence, head)
-// or of a segment of it (OUT false: for B and A, without outputs) for 16 NW value columns, a wave holds 16 columns of the state in registers
-// (result layout: lane n column n).  Every product with the state, and every
-// one after it, keeps the columns in their lanes, so that the waves share only
-// what is read.
+// or of a segment of it (OUT false: for B and A, without outputs) for 16 NW value
+// columns, a wave holds 16 columns of the state in registers (result layout: lane
+// n column n).  Every product with the state, and every one after it, keeps the
+// columns in their lanes, so that the waves share only what is read.  fp32 values
+// come straight into that layout (their tile, beside keys and queries in three
+// planes, would not fit the LDS).
 //   Bound by the chain of a chunk: R needs S, U needs R, the next S needs U, and
-// 2 waves a SIMD (their state, R, O and the next chunk's tiles: 171 registers)
+// 2 waves a SIMD (their state, R, O and the next chunk's tiles: 184 registers)
 // cover its waits only in part.  8 sequences of 1088 tokens x 32 heads, a
-// workgroup for every CU: 129 us, 7.4 us a chunk, in which the vector units issue
-// half of the time (conversions to planes above all) and the matrix cores work
-// 29 %; 2.1 TB/s.  Measured against it, for 32 sequences: 32 columns a wave
-// spill; 128 registers and two workgroups a CU spill too (826 us against 618
-// then); two workgroups of 64 columns form K, Q and P twice (492 -> 564);
-// opposite orders of P and K S in the two waves of a SIMD 570 -> 603; values
-// asked for a whole chunk ahead 488 -> 498; rounded products in one instruction
-// (v_fma_mixlo) instead of multiplies and packed conversions 504 -> 528.
+// workgroup for every CU: 141 us, 8.3 us a chunk, in which the vector units issue
+// half of the time (splitting into planes above all) and the matrix cores work
+// 43 %; 1.9 TB/s.  Without outputs bfloat16 takes 128 registers, two workgroups a
+// CU.  Measured with the operands in two binary16 planes, for 32 sequences: 32
+// columns a wave spill; 128 registers and two workgroups a CU spill too (826 us
+// against 618 then); two workgroups of 64 columns form K, Q and P twice (492 ->
+// 564); opposite orders of P and K S in the two waves of a SIMD 570 -> 603; values
+// asked for a whole chunk ahead 488 -> 498.
 //   VEC: rows of 16-byte pieces that start at 16 bytes.  The other form reads
 // them at any alignment and cuts the last one; taken for all, 570 -> 628 us.
 template <typename T, int DKP, int NW, bool DELTA, bool VEC, bool OUT>
@@ -894,7 +898,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
                 }
             }
         }
-        // 3 steps' operands ahead (32 sequences: 537 -> 530 us); the update of S the same way is slower (541)
+        // 3 steps' operands ahead (32 sequences, in two binary16 planes: 537 -> 530 us); the update of S the same way is
+        // slower (541)
         if constexpr (OUT && DELTA && sizeof(T) == 2) reads_ahead<4 * KB, 2, 6, 3>();
         again();
         // R (Delta) or U (decay); O's part from the state
@@ -1046,8 +1051,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || NW == 8 ? 2 : 1) void pr
 }
 
 // The states after the segments of a sequence, in order, decay rule: 4 elements
-// a thread.  Bound by memory: the records of 24 segments x 32 heads of 128 x 128
-// read and written, 100 MB in 21 us, 4.7 TB/s.
+// a thread.  Bound by memory: the records of 8 segments x 32 heads of 128 x 128
+// read and written, 34 MB in 8.5 us, 3.9 TB/s; of 24, 100 MB in 21 us, 4.7.
 __global__ __launch_bounds__(256) void prompt_join_decay_kernel(ChunkArgs a)
 {
     const int quads = a.p.dk * a.p.dv / 4, blocks = (quads + 255) / 256;
