@@ -371,7 +371,10 @@ typedef struct {
  * exponents: a token's o does not depend on the size of others in its chunk.  o
  * is rounded once, to act_dtype.  Under the Delta rule beta |k|^2 <= 2 keeps the
  * state bounded; beyond, it grows from token to token, and where the products of
- * a chunk of 64 tokens pass fp32, its tokens are NaN from there on. */
+ * a chunk of 64 tokens pass fp32, its tokens are NaN from there on.  A key or gate
+ * that is not finite makes its head's o not finite from its token on, a value its
+ * column's, a query its token's; the final state with all but the last, and
+ * nothing else.  o overlaps no input. */
 stepq_status stepq_prompt_workspace(const stepq_prompt_desc *desc, size_t *bytes);
 stepq_status stepq_prompt(const stepq_prompt_desc *desc, const int32_t *cu_seqlens, const void *q, const void *k,
                           const void *v, const void *alpha, const void *beta, void *o, const float *state_in,
@@ -388,10 +391,11 @@ typedef struct {
 
 /* One token of `batch` requests on full-precision states, in place: the single-
  * token form of stepq_prompt, and stepq_decode_step without the quantization.
- *   state [n_states][Hv][d_k][d_v] fp32; ids [batch] int32, distinct; a request
- *   whose id is outside [0, n_states) is an empty row of the batch: its o is
- *   zero and no state changes.  q, k [batch][Hqk][d_k], v [batch][Hv][d_v],
- *   alpha, beta [batch][Hv] (beta NULL: 1), o [batch][Hv][d_v] fp32.
+ *   state [n_states][Hv][d_k][d_v] fp32; ids [batch] int32, distinct, batch at
+ *   most n_states; a request whose id is outside [0, n_states) is an empty row of
+ *   the batch: its o is zero and no state changes.  q, k [batch][Hqk][d_k], v
+ *   [batch][Hv][d_v], alpha, beta [batch][Hv] (beta NULL: 1), o [batch][Hv][d_v]
+ *   fp32.
  * fp32 arithmetic. */
 stepq_status stepq_state_step(const stepq_state_desc *desc, float *state, const int32_t *ids, int32_t batch,
                               const void *q, const void *k, const void *v, const void *alpha, const void *beta, float *o,
@@ -426,7 +430,9 @@ typedef struct {
  * Entries past a request's length, and cache rows past it, are not read or do
  * not matter, whatever they hold.  Tokens of a page id outside [0, n_pages) are
  * left out.  A row without any key, or with all scores -inf, gets o = 0 and
- * lse = -inf. */
+ * lse = -inf.  A value that is not finite makes its column of o not finite for the
+ * requests that read it (NaN perhaps where the sum is infinite), and nothing else.
+ * o overlaps no input. */
 stepq_status stepq_prefix_attention_workspace(const stepq_attn_desc *desc, size_t *bytes);
 stepq_status stepq_prefix_attention(const stepq_attn_desc *desc, const void *q, const void *k_cache,
                                     const void *v_cache, const int32_t *prefix_pages, const int32_t *page_table,

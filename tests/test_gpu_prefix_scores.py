@@ -48,3 +48,28 @@ def test_scores_with_a_common_part(act, B, hq, hkv, D, P, offset, scale):
         off = (o.double() - ro).abs()
         assert (off <= 3e-5 * size).all(), float((off / size).max())
     assert ((lse.double() - rl).abs() <= 5 * 2.0 ** -24 * rl.abs()).all()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("act,B,hq,hkv,D,P", [(F32, 3, 4, 2, 64, 90), (BF16, 3, 4, 2, 128, 90), (BF16, 256, 16, 2, 64, 2333)])
+def test_values_that_are_not_finite(act, B, hq, hkv, D, P, bad):
+    """One of the prefix and one of a request's own: their columns of the rows that read them, and nothing else."""
+    from test_gpu_prefix_product import inputs
+    x = inputs(B, hq, hkv, D, P, own=5)
+    x[:3] = [t.to(act) for t in x[:3]]
+    x[6][:] = 3
+    got = []
+    for spoil in (False, True):
+        if spoil:
+            x[2][x[3][1].long(), 0, 3, 5] = bad
+            x[2][x[5][1, 0].long(), hkv - 1, 2, 9] = bad
+        o, lse = torch.empty((B, hq, D), dtype=act, device=DEV), torch.empty((B, hq), device=DEV)
+        stepq.stepq_prefix_attention(*x, o, lse)
+        got.append((o, lse))
+    torch.cuda.synchronize()
+    G = hq // hkv
+    hit = torch.zeros((B, hq, D), dtype=torch.bool, device=DEV)
+    hit[:, :G, 5] = True
+    hit[1, hq - G:, 9] = True
+    (clean, lse), (o, lse2) = got
+    assert not torch.isfinite(o[hit]).any() and torch.equal(o[~hit], clean[~hit]) and torch.equal(lse, lse2)
