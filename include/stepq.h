@@ -439,6 +439,130 @@ stepq_status stepq_prefix_attention(const stepq_attn_desc *desc, const void *q, 
                                     const int32_t *lengths, void *o, float *lse, void *workspace,
                                     size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Quantized key/value caches: attention layers between recurrent ones, their
+ * caches in 8- or 4-bit codes.  Tokens are quantized as they are written, and read
+ * back, attended to, or selected by pages.  The conventions of the calls above.
+ *
+ * A cache is n_pages x n_kv_heads records in caller-owned device memory, 128-byte
+ * aligned; the record of (page, head) is, with P tokens a page and D dimensions:
+ *  - P rows of key codes, then P rows of value codes, D bits / 8 bytes each;
+ *  - P rows of key scales, then P rows of value scales, bfloat16: one for a row of
+ *    8-bit codes, one for every 64 dimensions of 4-bit codes;
+ *  - zero or more bytes up to a multiple of 128.
+ * A row of 8-bit codes is one two's-complement byte for each dimension.  A row of
+ * 4-bit codes is D/4 little-endian words of 16 bits: bits 4j .. 4j + 3 of word w
+ * are dimension (D/4) j + w, two's complement.
+ * Of a group with the largest magnitude a (top = 127 or 7):
+ *   scale s: the smallest bfloat16 with top s >= a;  code: x / s rounded to the
+ *   nearest whole number, ties to even;  the value held: code x s.
+ * a < 2^-100: s = 0 and the group is zeros.  A value that is not finite: s is NaN
+ * and so is the whole group when it is read.  (A magnitude past 3.3e38 may be read
+ * as an infinite one, where rounding takes it past the type's largest.)
+ *
+ * Requests find their tokens through page_table [n][max_pages] int32, whose entry
+ * (i, j) is the page of request i's tokens j P .. j P + P - 1.  A page id outside
+ * [0, n_pages) is no page: nothing is written there or read from there.
+ */
+typedef struct {
+    int32_t n_pages;          /* >= 0 */
+    int32_t n_kv_heads;       /* Hkv >= 1 */
+    int32_t page_size;        /* P: tokens per page, 1 .. 2^20 */
+    int32_t head_dim;         /* D: 64, 128 or 256 */
+    int32_t bits;             /* 8 or 4 */
+} stepq_cache_desc;
+
+/* Bytes of the whole cache and (record_bytes not NULL) of one record. */
+stepq_status stepq_cache_bytes(const stepq_cache_desc *desc, size_t *cache_bytes, size_t *record_bytes);
+
+typedef struct {
+    int64_t n_tokens;         /* T: tokens of all sequences together, < 2^31 */
+    int32_t n_seq;            /* sequences */
+    int32_t max_pages;        /* columns of page_table */
+    int32_t act_dtype;        /* stepq_dtype of k and v */
+    /* elements from one token to the next (k and v may be slices of one
+     * projection's output), at most 2^26; 0: tokens back to back */
+    int64_t k_stride, v_stride;
+} stepq_cache_tokens;
+
+/* Keys and values k, v [T][Hkv][D] of packed sequences' tokens into the cache
+ * (write), or out of it (read: values rounded once to act_dtype).  Sequence i is
+ * tokens cu_seqlens[i] .. cu_seqlens[i+1] (device, int32 [n_seq+1], from 0 up and
+ * never down), at the positions from starts[i] on of its pages; cu_seqlens NULL:
+ * token i is sequence i's only one (T = n_seq).
+ * A token without a place (starts[i] < 0, as of an empty row of a batch; a position
+ * past its max_pages pages; no page there) is not written, and zeros when read.  A
+ * token in no sequence (before cu_seqlens[0], or behind the last one) is left as it
+ * is.  No two tokens of a write may have the same place; other rows of their pages
+ * keep their bits.  k and v of a read must not overlap each other. */
+stepq_status stepq_cache_write(const stepq_cache_desc *desc, const stepq_cache_tokens *tokens, void *cache,
+                               const int32_t *page_table, const int32_t *starts, const int32_t *cu_seqlens,
+                               const void *k, const void *v, void *stream);
+stepq_status stepq_cache_read(const stepq_cache_desc *desc, const stepq_cache_tokens *tokens, const void *cache,
+                              const int32_t *page_table, const int32_t *starts, const int32_t *cu_seqlens, void *k,
+                              void *v, void *stream);
+
+typedef struct {
+    int32_t batch;
+    int32_t n_q_heads;        /* Hq, Hq % Hkv == 0; query head h reads key/value head h / (Hq/Hkv) */
+    int32_t max_pages;        /* columns of page_table */
+    int32_t act_dtype;        /* stepq_dtype of q and o */
+    int32_t n_select;         /* columns of selected; 0: all of each request's tokens */
+    float scale;              /* scores are scale q.k */
+} stepq_cache_attn_desc;
+
+/* Softmax attention of one query token of each of `batch` requests over its
+ * tokens, split over their length and joined:
+ *   o = sum_t p_t v_t,  p = softmax over t of scale q.k_t,  lse = log sum_t exp(scale q.k_t)
+ * with the values that the cache holds.
+ *   q, o [batch][Hq][D] in act_dtype; lse [batch][Hq] fp32 or NULL; lengths [batch]
+ *   int32: request b's tokens are the first lengths[b] of its pages (0 .. max_pages
+ *   * page_size);
+ *   selected [batch][Hkv][n_select] int32 (n_select > 0): for each key/value head the
+ *   positions in page_table of the pages that are read, distinct, in any order; what
+ *   lies outside [0, max_pages) is none, tokens past the length are left out.
+ * What no request's tokens use may hold anything.  A row without a key, or with all
+ * scores -inf, gets o = 0 and lse = -inf.  A key that is not finite makes its heads'
+ * o NaN, a value its group of dimensions.  Scores, weights and sums are fp32, weights
+ * in 16 bits (bfloat16) or 24 (fp32).  o overlaps no input. */
+stepq_status stepq_cache_attention_workspace(const stepq_cache_desc *desc, const stepq_cache_attn_desc *attn,
+                                             size_t *bytes);
+stepq_status stepq_cache_attention(const stepq_cache_desc *desc, const stepq_cache_attn_desc *attn, const void *cache,
+                                   const void *q, const int32_t *page_table, const int32_t *lengths,
+                                   const int32_t *selected, void *o, float *lse, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
+/* Bounds of the keys in each page, bounds [n_pages][Hkv][2][D] bfloat16: below
+ * (rounded down) and above (up) every key that the page holds; NaN in a dimension
+ * where one is.  Brings those pages up to date that hold tokens starts[b] ..
+ * lengths[b] - 1 of request b (none: starts[b] < 0, or not below the length): a
+ * prompt's pages after it is written, the last page after each new token.  A page's
+ * tokens from the length on do not count; other pages' bounds stay as they are. */
+stepq_status stepq_cache_bounds(const stepq_cache_desc *desc, const void *cache, int32_t batch, int32_t max_pages,
+                                const int32_t *page_table, const int32_t *starts, const int32_t *lengths, void *bounds,
+                                void *stream);
+
+typedef struct {
+    int32_t batch, n_q_heads, max_pages, act_dtype;   /* as in stepq_cache_attn_desc */
+    int32_t n_select;         /* pages selected for each request and key/value head, >= 1 */
+    int32_t n_first, n_last;  /* pages of each request's beginning and end that always are; n_first + n_last <= n_select */
+} stepq_cache_select_desc;
+
+/* The pages that attention reads where a request has more than n_select:
+ * selected [batch][Hkv][n_select] int32, positions in page_table, ascending, then -1.
+ * The n_first first and n_last last pages, and those between them of the highest
+ *   score = sum_d hi_d sum_h max(q_hd, 0) + lo_d sum_h min(q_hd, 0)
+ * over the query heads h of the key/value head, with the page's bounds: no key of the
+ * page has a larger sum of q_h.k.  (For a negative scale of the attention, -q is
+ * scored.)  Sums are formed in 64 bits and rounded once, to fp32; a score that is NaN
+ * counts as the highest, a page that there is not as the lowest, and of equal scores
+ * the lowest position is taken. */
+stepq_status stepq_cache_select_workspace(const stepq_cache_desc *desc, const stepq_cache_select_desc *select,
+                                          size_t *bytes);
+stepq_status stepq_cache_select(const stepq_cache_desc *desc, const stepq_cache_select_desc *select, const void *bounds,
+                                const void *q, const int32_t *page_table, const int32_t *lengths, int32_t *selected,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
 /* Last failure message of the calling thread ("" if none). */
 const char *stepq_last_error(void);
 

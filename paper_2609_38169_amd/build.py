@@ -22,7 +22,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libstepq.so")
 HIP_SOURCES = ["stepq_host.hip", "stepq_kernels.hip", "stepq_refit.hip", "stepq_rowmax.hip", "stepq_tiles.hip",
-               "stepq_prompt.hip", "stepq_state.hip", "stepq_attn.hip"]
+               "stepq_prompt.hip", "stepq_state.hip", "stepq_attn.hip", "stepq_cache.hip", "stepq_cache_attn.hip",
+               "stepq_cache_select.hip"]
 CXX_SOURCES = ["stepq_setup.cpp", "stepq_plan.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -36,7 +36,9 @@ EXPORTED = (
     "stepq_setup_lifetime_weights", "stepq_setup_allocate", "stepq_setup_select_pivots",
     "stepq_setup_mean_log_retention", "stepq_setup_lifetime_costs", "stepq_setup_pivot_risk",
     "stepq_prompt_workspace", "stepq_prompt", "stepq_state_step", "stepq_prefix_attention_workspace",
-    "stepq_prefix_attention",
+    "stepq_prefix_attention", "stepq_cache_bytes", "stepq_cache_write", "stepq_cache_read",
+    "stepq_cache_attention_workspace", "stepq_cache_attention", "stepq_cache_bounds", "stepq_cache_select_workspace",
+    "stepq_cache_select",
 )
 
 
@@ -71,6 +73,25 @@ class stepq_attn_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "n_pages", "page_size")] + [
         ("prefix_len", ctypes.c_int64), ("max_pages", ctypes.c_int32), ("act_dtype", ctypes.c_int32),
         ("scale", ctypes.c_float)]
+
+
+class stepq_cache_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "page_size", "head_dim", "bits")]
+
+
+class stepq_cache_tokens(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("n_seq", "max_pages", "act_dtype")] + [
+        (n, ctypes.c_int64) for n in ("k_stride", "v_stride")]
+
+
+class stepq_cache_attn_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "max_pages", "act_dtype", "n_select")] + [
+        ("scale", ctypes.c_float)]
+
+
+class stepq_cache_select_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "max_pages", "act_dtype", "n_select", "n_first",
+                                              "n_last")]
 
 
 _lib = None
@@ -121,6 +142,14 @@ def lib():
             "stepq_state_step": ([P, P, P, i32] + [P] * 7, st),
             "stepq_prefix_attention_workspace": ([P, P], st),
             "stepq_prefix_attention": ([P] * 10 + [ctypes.c_size_t, P], st),
+            "stepq_cache_bytes": ([P] * 3, st),
+            "stepq_cache_write": ([P] * 9, st),
+            "stepq_cache_read": ([P] * 9, st),
+            "stepq_cache_attention_workspace": ([P] * 3, st),
+            "stepq_cache_attention": ([P] * 10 + [ctypes.c_size_t, P], st),
+            "stepq_cache_bounds": ([P, P, i32, i32] + [P] * 5, st),
+            "stepq_cache_select_workspace": ([P] * 3, st),
+            "stepq_cache_select": ([P] * 8 + [ctypes.c_size_t, P], st),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -508,12 +537,12 @@ def _act_dtype(t, name):
     return t.dtype, STEPQ_F32 if t.dtype == torch.float32 else STEPQ_BF16
 
 
-def _tokens(t, name, dtype, shape, device):
+def _tokens(t, name, dtype, shape, device, other="q"):
     """A tensor of tokens whose heads are contiguous: its pointer and the elements from one token to the next."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, q is on {device}")
+        raise ValueError(f"{name} is on {t.device}, {other} is on {device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if tuple(t.shape) != tuple(shape):
@@ -697,6 +726,203 @@ def stepq_prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_t
     ws = _workspace(size.value, workspace, dev, stream)
     _check(lib().stepq_prefix_attention(ctypes.byref(d), *args, _ptr(ws), 0 if ws is None else ws.numel(),
                                         _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# quantized key/value caches
+def _cache_desc(n_pages, n_kv_heads, page_size, head_dim, bits):
+    return stepq_cache_desc(*(_whole(x, n, 32) for x, n in zip(
+        (n_pages, n_kv_heads, page_size, head_dim, bits), ("n_pages", "n_kv_heads", "page_size", "head_dim", "bits"))))
+
+
+def stepq_cache_bytes(n_pages, n_kv_heads, page_size, head_dim, bits):
+    """Bytes of a cache, and of the record of one (page, head)."""
+    n, r = ctypes.c_size_t(), ctypes.c_size_t()
+    d = _cache_desc(n_pages, n_kv_heads, page_size, head_dim, bits)
+    _check(lib().stepq_cache_bytes(ctypes.byref(d), ctypes.byref(n), ctypes.byref(r)))
+    return n.value, r.value
+
+
+class Cache:
+    """Keys and values of an attention layer in 8- or 4-bit codes, in pages of
+    page_size tokens.  Its memory is a torch uint8 tensor on the current
+    device, `memory` if it is given.  Rows that no token was written to hold anything."""
+
+    def __init__(self, n_pages, n_kv_heads, page_size, head_dim, bits, device=None, memory=None):
+        self.bytes, self.record_bytes = stepq_cache_bytes(n_pages, n_kv_heads, page_size, head_dim, bits)
+        self.desc = _cache_desc(n_pages, n_kv_heads, page_size, head_dim, bits)
+        self.n_pages, self.Hkv, self.page_size = self.desc.n_pages, self.desc.n_kv_heads, self.desc.page_size
+        self.D, self.bits = self.desc.head_dim, self.desc.bits
+        if memory is None:
+            dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+            memory = torch.empty(self.bytes, dtype=torch.uint8, device=dev)
+        elif not isinstance(memory, torch.Tensor) or memory.dtype != torch.uint8 or not memory.is_contiguous():
+            raise TypeError("memory must be a contiguous torch.uint8 tensor")
+        elif device is not None and torch.device(device) != memory.device:
+            raise ValueError(f"memory is on {memory.device}, not on {device}")
+        if memory.numel() < self.bytes or (self.bytes and memory.data_ptr() % 128):
+            raise ValueError(f"memory must hold {self.bytes} bytes, 128-byte aligned")
+        self.memory, self.device = memory, memory.device
+
+    def write(self, k, v, page_table, starts, cu_seqlens=None, stream=None):
+        stepq_cache_write(self, k, v, page_table, starts, cu_seqlens, stream)
+
+    def read(self, page_table, starts, k, v, cu_seqlens=None, stream=None):
+        stepq_cache_read(self, page_table, starts, k, v, cu_seqlens, stream)
+
+    def attend(self, q, page_table, lengths, o, lse=None, selected=None, scale=None, workspace=None, stream=None):
+        stepq_cache_attention(self, q, page_table, lengths, o, lse, selected, scale, workspace, stream)
+
+    def bounds(self, page_table, starts, lengths, bounds, stream=None):
+        stepq_cache_bounds(self, page_table, starts, lengths, bounds, stream)
+
+    def select(self, q, bounds, page_table, lengths, selected, n_first=1, n_last=1, workspace=None, stream=None):
+        stepq_cache_select(self, q, bounds, page_table, lengths, selected, n_first, n_last, workspace, stream)
+
+
+def _cache_device(cache):
+    if not isinstance(cache, Cache):
+        raise TypeError("cache must be a stepq.Cache")
+    if cache.device.type != "cuda" or cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return cache.device
+
+
+def _paged(page_table, dev):
+    """A page table's pointer, requests and columns."""
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be [requests][pages]")
+    B, M = page_table.shape
+    return _dev(page_table, "page_table", torch.int32, (B, M), dev), _whole(B, "requests", 32), _whole(M, "pages", 32)
+
+
+def _cache_rows(cache, fn, k, v, page_table, starts, cu_seqlens, stream):
+    dev = _cache_device(cache)
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k and v must be [tokens][heads][d]")
+    dt, code = _act_dtype(k, "k")
+    shape = (k.shape[0], cache.Hkv, cache.D)
+    kp, ks = _tokens(k, "k", dt, shape, dev, "the cache")
+    vp, vs = _tokens(v, "v", dt, shape, dev, "the cache")
+    tp, n, M = _paged(page_table, dev)
+    sp = _dev(starts, "starts", torch.int32, (n,), dev)
+    cu = None
+    if cu_seqlens is not None:
+        cu = _dev(cu_seqlens, "cu_seqlens", torch.int32, (n + 1,), dev)
+    elif shape[0] != n:
+        raise ValueError("without cu_seqlens each sequence of page_table has one token")
+    d = stepq_cache_tokens(shape[0], n, M, code, ks, vs)
+    _check(fn(ctypes.byref(cache.desc), ctypes.byref(d), ctypes.c_void_p(cache.memory.data_ptr()), tp, sp, cu, kp, vp,
+              _stream(stream)))
+
+
+def stepq_cache_write(cache: Cache, k, v, page_table, starts, cu_seqlens=None, stream=None):
+    """Quantize tokens into their pages: k, v [T][Hkv][D] (float32 or bfloat16;
+    slices of a wider token are taken as they are), page_table [n][M] int32,
+    starts [n] int32 the position of each sequence's first token (< 0: none of
+    it is written), cu_seqlens [n+1] int32 (None: one token each)."""
+    _cache_rows(cache, lib().stepq_cache_write, k, v, page_table, starts, cu_seqlens, stream)
+
+
+def stepq_cache_read(cache: Cache, page_table, starts, k, v, cu_seqlens=None, stream=None):
+    """The values that the cache holds into k, v (arguments as in stepq_cache_write)."""
+    _cache_rows(cache, lib().stepq_cache_read, k, v, page_table, starts, cu_seqlens, stream)
+
+
+def _selected(selected, cache, B, dev):
+    if not isinstance(selected, torch.Tensor) or selected.dim() != 3 or selected.shape[2] < 1:
+        raise ValueError("selected must be [requests][key/value heads][pages], one page or more")
+    S = _whole(selected.shape[2], "selected pages", 32)
+    return _dev(selected, "selected", torch.int32, (B, cache.Hkv, S), dev), S
+
+
+def _attn_desc(cache, batch, n_q_heads, max_pages, n_select, scale, code):
+    return stepq_cache_attn_desc(batch, n_q_heads, max_pages, code, n_select,
+                                 float(cache.D ** -0.5 if scale is None else scale))
+
+
+def stepq_cache_attention_workspace(cache: Cache, batch, n_q_heads, max_pages, n_select=0,
+                                    act_dtype=torch.bfloat16) -> int:
+    """Bytes of workspace a stepq_cache_attention call of these sizes takes."""
+    d = _attn_desc(cache, batch, n_q_heads, max_pages, n_select, None,
+                   STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16)
+    n = ctypes.c_size_t()
+    _check(lib().stepq_cache_attention_workspace(ctypes.byref(cache.desc), ctypes.byref(d), ctypes.byref(n)))
+    return n.value
+
+
+def stepq_cache_attention(cache: Cache, q, page_table, lengths, o, lse=None, selected=None, scale=None, workspace=None,
+                          stream=None):
+    """Softmax attention of one token of each request over its tokens in the
+    cache: q, o [B][Hq][D] (float32 or bfloat16), page_table [B][M] int32,
+    lengths [B] int32, lse [B][Hq] float32 (None: not wanted), selected
+    [B][Hkv][S] int32 the positions in page_table of the pages that are read
+    (None: all); scale defaults to D ** -0.5."""
+    dev = _cache_device(cache)
+    dt, code = _act_dtype(q, "q")
+    if q.dim() != 3:
+        raise ValueError("q must be [requests][heads][d]")
+    Hq = q.shape[1]
+    tp, n, M = _paged(page_table, dev)
+    qp = _dev(q, "q", dt, (n, Hq, cache.D), dev)
+    lp = _dev(lengths, "lengths", torch.int32, (n,), dev)
+    op = _dev(o, "o", dt, (n, Hq, cache.D), dev)
+    ep = None if lse is None else _dev(lse, "lse", torch.float32, (n, Hq), dev)
+    sp, S = (None, 0) if selected is None else _selected(selected, cache, n, dev)
+    d = _attn_desc(cache, n, _whole(Hq, "heads", 32), M, S, scale, code)
+    size = ctypes.c_size_t()
+    _check(lib().stepq_cache_attention_workspace(ctypes.byref(cache.desc), ctypes.byref(d), ctypes.byref(size)))
+    ws = _workspace(size.value, workspace, dev, stream)
+    _check(lib().stepq_cache_attention(ctypes.byref(cache.desc), ctypes.byref(d),
+                                       ctypes.c_void_p(cache.memory.data_ptr()), qp, tp, lp, sp, op, ep, _ptr(ws),
+                                       0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def stepq_cache_bounds(cache: Cache, page_table, starts, lengths, bounds, stream=None):
+    """Bring the bounds of the pages up to date that hold tokens starts[b] ..
+    lengths[b] - 1 of each request: page_table [B][M], starts, lengths [B]
+    int32, bounds [n_pages][Hkv][2][D] bfloat16 (below, above)."""
+    dev = _cache_device(cache)
+    tp, n, M = _paged(page_table, dev)
+    _check(lib().stepq_cache_bounds(
+        ctypes.byref(cache.desc), ctypes.c_void_p(cache.memory.data_ptr()), n, M, tp,
+        _dev(starts, "starts", torch.int32, (n,), dev), _dev(lengths, "lengths", torch.int32, (n,), dev),
+        _dev(bounds, "bounds", torch.bfloat16, (cache.n_pages, cache.Hkv, 2, cache.D), dev), _stream(stream)))
+
+
+def stepq_cache_select_workspace(cache: Cache, batch, n_q_heads, max_pages, n_select, n_first=1, n_last=1,
+                                 act_dtype=torch.bfloat16) -> int:
+    """Bytes of workspace a stepq_cache_select call of these sizes takes."""
+    d = stepq_cache_select_desc(batch, n_q_heads, max_pages, STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16,
+                                n_select, n_first, n_last)
+    n = ctypes.c_size_t()
+    _check(lib().stepq_cache_select_workspace(ctypes.byref(cache.desc), ctypes.byref(d), ctypes.byref(n)))
+    return n.value
+
+
+def stepq_cache_select(cache: Cache, q, bounds, page_table, lengths, selected, n_first=1, n_last=1, workspace=None,
+                       stream=None):
+    """The pages that each request's query may need most, for each key/value
+    head: selected [B][Hkv][S] int32 receives positions in page_table,
+    ascending, then -1; the n_first first and n_last last pages among them
+    (the other arguments as in stepq_cache_bounds and stepq_cache_attention)."""
+    dev = _cache_device(cache)
+    dt, code = _act_dtype(q, "q")
+    if q.dim() != 3:
+        raise ValueError("q must be [requests][heads][d]")
+    Hq = q.shape[1]
+    tp, n, M = _paged(page_table, dev)
+    qp = _dev(q, "q", dt, (n, Hq, cache.D), dev)
+    bp = _dev(bounds, "bounds", torch.bfloat16, (cache.n_pages, cache.Hkv, 2, cache.D), dev)
+    lp = _dev(lengths, "lengths", torch.int32, (n,), dev)
+    sp, S = _selected(selected, cache, n, dev)
+    d = stepq_cache_select_desc(n, _whole(Hq, "heads", 32), M, code, S, _whole(n_first, "n_first", 32),
+                                _whole(n_last, "n_last", 32))
+    size = ctypes.c_size_t()
+    _check(lib().stepq_cache_select_workspace(ctypes.byref(cache.desc), ctypes.byref(d), ctypes.byref(size)))
+    ws = _workspace(size.value, workspace, dev, stream)
+    _check(lib().stepq_cache_select(ctypes.byref(cache.desc), ctypes.byref(d), bp, qp, tp, lp, sp, _ptr(ws),
+                                    0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def stepq_last_error() -> str:
