@@ -37,6 +37,13 @@ struct Entry {
     decltype(&stepq_prompt) prompt;
     decltype(&stepq_prefix_attention_workspace) attention_workspace;
     decltype(&stepq_prefix_attention) attention;
+    decltype(&stepq_cache_write) cache_write;
+    decltype(&stepq_cache_read) cache_read;
+    decltype(&stepq_cache_attention_workspace) cache_attention_workspace;
+    decltype(&stepq_cache_attention) cache_attention;
+    decltype(&stepq_cache_bounds) cache_bounds;
+    decltype(&stepq_cache_select_workspace) cache_select_workspace;
+    decltype(&stepq_cache_select) cache_select;
 } g{};
 
 struct Plain {
@@ -269,7 +276,8 @@ bool take_long(PyObject *o, int64_t *out)
     return false;
 }
 
-bool take_rule(PyObject *o, int64_t *out) { return take_long(o, out) && *out == static_cast<int32_t>(*out); }
+// a whole number of 32 bits
+bool take_int(PyObject *o, int64_t *out) { return take_long(o, out) && *out == static_cast<int32_t>(*out); }
 
 const at::Tensor *tensor_of(PyObject *o, int64_t dims)
 {
@@ -328,7 +336,7 @@ PyObject *py_state_step(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const at::Tensor *S = tensor_of(a[0], 4), *q = tensor_of(a[2], 3), *v = tensor_of(a[4], 3);
         Plain p{};
         int64_t rule;
-        if (!S || !q || !v || !take_device(*q, &p) || !take_rule(a[8], &rule)) return -1;
+        if (!S || !q || !v || !take_device(*q, &p) || !take_int(a[8], &rule)) return -1;
         const int64_t B = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2), n = S->size(0);
         const at::ScalarType dt = q->scalar_type();
         void *sp, *ip, *qp, *kp, *vp, *ap, *bp, *op, *st;
@@ -359,7 +367,7 @@ PyObject *py_prompt(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const at::Tensor *q = tensor_of(a[0], 3), *v = tensor_of(a[2], 3), *cu = a[8] == Py_None ? nullptr : tensor_of(a[8], 1);
         Plain p{};
         int64_t rule;
-        if (!q || !v || (a[8] != Py_None && (!cu || cu->size(0) < 1)) || !take_device(*q, &p) || !take_rule(a[7], &rule)) return -1;
+        if (!q || !v || (a[8] != Py_None && (!cu || cu->size(0) < 1)) || !take_device(*q, &p) || !take_int(a[7], &rule)) return -1;
         const int64_t T = q->size(0), Hqk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2);
         const int64_t n = cu ? cu->size(0) - 1 : 1;
         const at::ScalarType dt = q->scalar_type();
@@ -449,6 +457,198 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
+// ---------------------------------------------------------------------------
+// Calls on quantized caches, as above; the cache is on the current device.  Writing and reading back one token of 4
+// requests takes CALLS_STORE us, attention of 4 requests CALLS_ATTN.
+
+struct CachePlain {
+    stepq_cache_desc desc;
+    int device;
+    void *memory;
+};
+
+void free_cache(PyObject *cap) { delete static_cast<CachePlain *>(PyCapsule_GetPointer(cap, "stepq.cache")); }
+
+// cache(n_pages, n_kv_heads, page_size, head_dim, bits, device, memory): what the checks compare with
+PyObject *py_cache(PyObject *, PyObject *args)
+{
+    int n, h, p, d, b, device;
+    unsigned long long memory;
+    if (!PyArg_ParseTuple(args, "iiiiiiK", &n, &h, &p, &d, &b, &device, &memory)) return nullptr;
+    auto *c = new CachePlain{{n, h, p, d, b}, device, reinterpret_cast<void *>(memory)};
+    return PyCapsule_New(c, "stepq.cache", free_cache);
+}
+
+// bind_caches(write, read, attention_workspace, attention, bounds, select_workspace, select)
+PyObject *py_bind_caches(PyObject *, PyObject *args)
+{
+    unsigned long long f[7];
+    if (!PyArg_ParseTuple(args, "KKKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6])) return nullptr;
+    auto set = [&f](auto &fn, int i) { fn = reinterpret_cast<std::remove_reference_t<decltype(fn)>>(f[i]); };
+    set(g.cache_write, 0);
+    set(g.cache_read, 1);
+    set(g.cache_attention_workspace, 2);
+    set(g.cache_attention, 3);
+    set(g.cache_bounds, 4);
+    set(g.cache_select_workspace, 5);
+    set(g.cache_select, 6);
+    Py_RETURN_NONE;
+}
+
+// The cache's description, if its memory is on the current device.
+const CachePlain *cache_of(PyObject *o, Plain *p)
+{
+    if (!PyCapsule_CheckExact(o)) return nullptr;
+    const auto *c = static_cast<const CachePlain *>(PyCapsule_GetPointer(o, "stepq.cache"));
+    int device;
+    if (!c) {
+        PyErr_Clear();
+        return nullptr;
+    }
+    if (!g.cache_write || g.get_device(&device) != 0 || device != c->device) return nullptr;
+    p->device = device;
+    return c;
+}
+
+// page_table [requests][pages]
+bool take_table(PyObject *o, const Plain &p, int64_t *n, int64_t *m, void **out)
+{
+    const at::Tensor *t = tensor_of(o, 2);
+    if (!t || t->size(0) > INT32_MAX || t->size(1) > INT32_MAX) return false;
+    *n = t->size(0), *m = t->size(1);
+    return take(o, p, at::kInt, {*n, *m}, out);
+}
+
+// cache_rows(op, cache, k, v, page_table, starts, cu_seqlens, stream): write (0), read (1)
+PyObject *py_cache_rows(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded([&]() -> long {
+        Plain p{};
+        const CachePlain *c = n_args == 8 ? cache_of(a[1], &p) : nullptr;
+        int64_t op, n, m;
+        const at::Tensor *k = c ? tensor_of(a[2], 3) : nullptr;
+        if (!k || !take_long(a[0], &op) || !known(k->scalar_type())) return -1;
+        const int64_t T = k->size(0);
+        const at::ScalarType dt = k->scalar_type();
+        stepq_cache_tokens d{};
+        void *kp, *vp, *tp, *sp, *cp = nullptr, *st;
+        if (!take_tokens(a[2], p, dt, {T, c->desc.n_kv_heads, c->desc.head_dim}, &kp, &d.k_stride) ||
+            !take_tokens(a[3], p, dt, {T, c->desc.n_kv_heads, c->desc.head_dim}, &vp, &d.v_stride) ||
+            !take_table(a[4], p, &n, &m, &tp) || !take(a[5], p, at::kInt, {n}, &sp) ||
+            !(a[6] == Py_None ? T == n : take(a[6], p, at::kInt, {n + 1}, &cp)) || !take_stream(a[7], &st))
+            return -1;
+        d.n_tokens = T, d.n_seq = static_cast<int32_t>(n), d.max_pages = static_cast<int32_t>(m), d.act_dtype = code_of(dt);
+        const auto *table = static_cast<const int32_t *>(tp), *starts = static_cast<const int32_t *>(sp),
+                   *cu = static_cast<const int32_t *>(cp);
+        stepq_status e;
+        Py_BEGIN_ALLOW_THREADS;
+        e = op == 0 ? g.cache_write(&c->desc, &d, c->memory, table, starts, cu, kp, vp, st)
+                    : g.cache_read(&c->desc, &d, c->memory, table, starts, cu, kp, vp, st);
+        Py_END_ALLOW_THREADS;
+        return e;
+    });
+}
+
+// The query [requests][heads][d] of a cache's head_dim.
+bool take_query(PyObject *o, const Plain &p, const CachePlain &c, int64_t n, int64_t *heads, at::ScalarType *dt, void **out)
+{
+    const at::Tensor *q = tensor_of(o, 3);
+    if (!q || !known(q->scalar_type()) || q->size(1) > INT32_MAX) return false;
+    *heads = q->size(1), *dt = q->scalar_type();
+    return take(o, p, *dt, {n, *heads, c.desc.head_dim}, out);
+}
+
+// selected [requests][key/value heads][pages]
+bool take_selected(PyObject *o, const Plain &p, const CachePlain &c, int64_t n, int64_t *pages, void **out)
+{
+    const at::Tensor *t = tensor_of(o, 3);
+    if (!t || t->size(2) < 1 || t->size(2) > INT32_MAX) return false;
+    *pages = t->size(2);
+    return take(o, p, at::kInt, {n, c.desc.n_kv_heads, *pages}, out);
+}
+
+// cache_attention(cache, q, page_table, lengths, o, lse, selected, scale): on the current stream, in torch's memory
+PyObject *py_cache_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded([&]() -> long {
+        Plain p{};
+        const CachePlain *c = n_args == 8 ? cache_of(a[0], &p) : nullptr;
+        if (!c || !(a[7] == Py_None || PyFloat_CheckExact(a[7]))) return -1;
+        int64_t n, m, Hq, S = 0;
+        at::ScalarType dt;
+        void *tp, *qp, *lp, *op, *ep = nullptr, *sp = nullptr, *st;
+        if (!take_table(a[2], p, &n, &m, &tp) || !take_query(a[1], p, *c, n, &Hq, &dt, &qp) || !take(a[3], p, at::kInt, {n}, &lp) ||
+            !take(a[4], p, dt, {n, Hq, c->desc.head_dim}, &op) || (a[5] != Py_None && !take(a[5], p, at::kFloat, {n, Hq}, &ep)) ||
+            (a[6] != Py_None && !take_selected(a[6], p, *c, n, &S, &sp)))
+            return -1;
+        const double scale = a[7] == Py_None ? std::pow(static_cast<double>(c->desc.head_dim), -0.5) : PyFloat_AS_DOUBLE(a[7]);
+        const stepq_cache_attn_desc d{static_cast<int32_t>(n), static_cast<int32_t>(Hq), static_cast<int32_t>(m), code_of(dt),
+                                      static_cast<int32_t>(S), static_cast<float>(scale)};
+        size_t bytes = 0;
+        stepq_status e = g.cache_attention_workspace(&c->desc, &d, &bytes);
+        if (e != STEPQ_OK) return e;
+        if (!take_stream(Py_None, &st)) return -1;
+        const at::Tensor ws = bytes ? space(bytes, p.device) : at::Tensor();
+        void *wp = bytes ? ws.data_ptr() : nullptr;
+        Py_BEGIN_ALLOW_THREADS;
+        e = g.cache_attention(&c->desc, &d, c->memory, qp, static_cast<const int32_t *>(tp), static_cast<const int32_t *>(lp),
+                              static_cast<const int32_t *>(sp), op, static_cast<float *>(ep), wp, bytes, st);
+        Py_END_ALLOW_THREADS;
+        return e;
+    });
+}
+
+// cache_bounds(cache, page_table, starts, lengths, bounds, stream)
+PyObject *py_cache_bounds(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded([&]() -> long {
+        Plain p{};
+        const CachePlain *c = n_args == 6 ? cache_of(a[0], &p) : nullptr;
+        int64_t n, m;
+        void *tp, *sp, *lp, *bp, *st;
+        if (!c || !take_table(a[1], p, &n, &m, &tp) || !take(a[2], p, at::kInt, {n}, &sp) || !take(a[3], p, at::kInt, {n}, &lp) ||
+            !take(a[4], p, at::kBFloat16, {c->desc.n_pages, c->desc.n_kv_heads, 2, c->desc.head_dim}, &bp) ||
+            !take_stream(a[5], &st))
+            return -1;
+        stepq_status e;
+        Py_BEGIN_ALLOW_THREADS;
+        e = g.cache_bounds(&c->desc, c->memory, static_cast<int32_t>(n), static_cast<int32_t>(m), static_cast<const int32_t *>(tp),
+                           static_cast<const int32_t *>(sp), static_cast<const int32_t *>(lp), bp, st);
+        Py_END_ALLOW_THREADS;
+        return e;
+    });
+}
+
+// cache_select(cache, q, bounds, page_table, lengths, selected, n_first, n_last): on the current stream, in torch's memory
+PyObject *py_cache_select(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded([&]() -> long {
+        Plain p{};
+        const CachePlain *c = n_args == 8 ? cache_of(a[0], &p) : nullptr;
+        int64_t n, m, Hq, S, first, last;
+        at::ScalarType dt;
+        void *tp, *qp, *lp, *bp, *sp, *st;
+        if (!c || !take_table(a[3], p, &n, &m, &tp) || !take_query(a[1], p, *c, n, &Hq, &dt, &qp) ||
+            !take(a[2], p, at::kBFloat16, {c->desc.n_pages, c->desc.n_kv_heads, 2, c->desc.head_dim}, &bp) ||
+            !take(a[4], p, at::kInt, {n}, &lp) || !take_selected(a[5], p, *c, n, &S, &sp) || !take_int(a[6], &first) ||
+            !take_int(a[7], &last))
+            return -1;
+        const stepq_cache_select_desc d{static_cast<int32_t>(n), static_cast<int32_t>(Hq), static_cast<int32_t>(m), code_of(dt),
+                                        static_cast<int32_t>(S), static_cast<int32_t>(first), static_cast<int32_t>(last)};
+        size_t bytes = 0;
+        stepq_status e = g.cache_select_workspace(&c->desc, &d, &bytes);
+        if (e != STEPQ_OK) return e;
+        if (!take_stream(Py_None, &st)) return -1;
+        const at::Tensor ws = bytes ? space(bytes, p.device) : at::Tensor();
+        void *wp = bytes ? ws.data_ptr() : nullptr;
+        Py_BEGIN_ALLOW_THREADS;
+        e = g.cache_select(&c->desc, &d, bp, qp, static_cast<const int32_t *>(tp), static_cast<const int32_t *>(lp),
+                           static_cast<int32_t *>(sp), wp, bytes, st);
+        Py_END_ALLOW_THREADS;
+        return e;
+    });
+}
+
 PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, "addresses of the C calls, torch's raw stream query and stream class"},
     {"plain", py_plain, METH_VARARGS, "a pool's handle, device and sizes"},
@@ -463,6 +663,16 @@ PyMethodDef methods[] = {
     {"prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_prompt)), METH_FASTCALL, "packed prompts"},
     {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_attention)), METH_FASTCALL,
      "attention over a shared prefix"},
+    {"bind_caches", py_bind_caches, METH_VARARGS, "addresses of the C calls on quantized caches"},
+    {"cache", py_cache, METH_VARARGS, "a cache's sizes, device and memory"},
+    {"cache_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_cache_rows)), METH_FASTCALL,
+     "tokens written or read back"},
+    {"cache_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_cache_attention)), METH_FASTCALL,
+     "attention over a cache"},
+    {"cache_bounds", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_cache_bounds)), METH_FASTCALL,
+     "bounds of pages' keys"},
+    {"cache_select", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_cache_select)), METH_FASTCALL,
+     "pages by their scores"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_stepq_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -165,6 +165,8 @@ class _PythonChecks:
     plain = staticmethod(lambda *a: None)
     decode = scaled = tiles = staticmethod(lambda *a: -1)
     state_step = prompt = attention = staticmethod(lambda *a: -1)
+    cache = staticmethod(lambda *a: None)
+    cache_rows = cache_attention = cache_bounds = cache_select = staticmethod(lambda *a: -1)
 
 
 def native():
@@ -186,6 +188,9 @@ def native():
         _stepq_args.bind_calls(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
             "stepq_state_step", "stepq_prompt_workspace", "stepq_prompt", "stepq_prefix_attention_workspace",
             "stepq_prefix_attention")))
+        _stepq_args.bind_caches(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
+            "stepq_cache_write", "stepq_cache_read", "stepq_cache_attention_workspace", "stepq_cache_attention",
+            "stepq_cache_bounds", "stepq_cache_select_workspace", "stepq_cache_select")))
         _native = _stepq_args
     return _native
 
@@ -763,6 +768,9 @@ class Cache:
         if memory.numel() < self.bytes or (self.bytes and memory.data_ptr() % 128):
             raise ValueError(f"memory must hold {self.bytes} bytes, 128-byte aligned")
         self.memory, self.device = memory, memory.device
+        # what the native checks compare with
+        self._plain = native().cache(self.n_pages, self.Hkv, self.page_size, self.D, self.bits,
+                                     -1 if memory.device.index is None else memory.device.index, memory.data_ptr())
 
     def write(self, k, v, page_table, starts, cu_seqlens=None, stream=None):
         stepq_cache_write(self, k, v, page_table, starts, cu_seqlens, stream)
@@ -826,6 +834,8 @@ def stepq_cache_write(cache: Cache, k, v, page_table, starts, cu_seqlens=None, s
 
 def stepq_cache_read(cache: Cache, page_table, starts, k, v, cu_seqlens=None, stream=None):
     """The values that the cache holds into k, v (arguments as in stepq_cache_write)."""
+    if isinstance(cache, Cache) and _done(_native.cache_rows(1, cache._plain, k, v, page_table, starts, cu_seqlens, stream)):
+        return
     _cache_rows(cache, lib().stepq_cache_read, k, v, page_table, starts, cu_seqlens, stream)
 
 
@@ -858,6 +868,9 @@ def stepq_cache_attention(cache: Cache, q, page_table, lengths, o, lse=None, sel
     lengths [B] int32, lse [B][Hq] float32 (None: not wanted), selected
     [B][Hkv][S] int32 the positions in page_table of the pages that are read
     (None: all); scale defaults to D ** -0.5."""
+    if workspace is None and stream is None and isinstance(cache, Cache) and _done(_native.cache_attention(
+            cache._plain, q, page_table, lengths, o, lse, selected, scale)):
+        return
     dev = _cache_device(cache)
     dt, code = _act_dtype(q, "q")
     if q.dim() != 3:
@@ -882,6 +895,8 @@ def stepq_cache_bounds(cache: Cache, page_table, starts, lengths, bounds, stream
     """Bring the bounds of the pages up to date that hold tokens starts[b] ..
     lengths[b] - 1 of each request: page_table [B][M], starts, lengths [B]
     int32, bounds [n_pages][Hkv][2][D] bfloat16 (below, above)."""
+    if isinstance(cache, Cache) and _done(_native.cache_bounds(cache._plain, page_table, starts, lengths, bounds, stream)):
+        return
     dev = _cache_device(cache)
     tp, n, M = _paged(page_table, dev)
     _check(lib().stepq_cache_bounds(
@@ -906,6 +921,9 @@ def stepq_cache_select(cache: Cache, q, bounds, page_table, lengths, selected, n
     head: selected [B][Hkv][S] int32 receives positions in page_table,
     ascending, then -1; the n_first first and n_last last pages among them
     (the other arguments as in stepq_cache_bounds and stepq_cache_attention)."""
+    if workspace is None and stream is None and isinstance(cache, Cache) and _done(_native.cache_select(
+            cache._plain, q, bounds, page_table, lengths, selected, n_first, n_last)):
+        return
     dev = _cache_device(cache)
     dt, code = _act_dtype(q, "q")
     if q.dim() != 3:
