@@ -536,7 +536,7 @@ void launch(AttnArgs a, const Split &s, hipStream_t st)
             attn_prefix_kernel<D><<<dim3(static_cast<unsigned>(grid)), 512, 0, st>>>(a);
         }
     attn_rows_kernel<T, D><<<dim3(static_cast<unsigned>(a.prefix_items + own)), 256, 0, st>>>(a);
-    join_parts<T, D>({a.ml, a.acc, a.o, a.lse, static_cast<size_t>(a.batch) * a.Hq, a.prefix_parts + a.own_parts}, st);
+    join_parts<T, D>({a.ml, a.acc, a.o, a.lse, static_cast<size_t>(a.batch) * a.Hq, a.prefix_parts + a.own_parts, nullptr, 0, 0, 0}, st);
 }
 
 template <typename T>

@@ -68,6 +68,10 @@ struct JoinArgs {
     float *lse;              // NULL: not wanted
     size_t rows;
     int32_t parts;
+    // lengths not NULL: rows b Hq .. + Hq - 1 have as many parts as lengths[b] tokens (at most `most`) take, `chunk` each;
+    // of one part or none the row is there already
+    const int32_t *lengths;
+    int32_t Hq, most, chunk;
 };
 
 // The parts of each row joined: W waves per row take parts in turn, a few at a
@@ -89,7 +93,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs a)
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % W, lane = threadIdx.x & 63;
     const size_t total = a.rows, row = static_cast<size_t>(blockIdx.x) * (4 / W) + w / W;
     if (W == 1 && row >= total) return;
-    const int parts = a.parts;
+    int parts = a.parts;
+    if (a.lengths) {
+        const int len = min(a.lengths[row / a.Hq], a.most);
+        if (len <= a.chunk) return;
+        parts = (len + a.chunk - 1) / a.chunk;
+    }
     const auto stats = [&](int c) { return c + lane < parts ? a.ml[(c + lane) * total + row] : make_float2(-INFINITY, 0.0f); };
     const float2 first = stats(0);
     float top = first.x;
