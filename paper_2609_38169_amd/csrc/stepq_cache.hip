@@ -16,6 +16,8 @@ stepq_status check_cache(const stepq_cache_desc *d)
     if (d->page_size > (1 << 20)) return set_error(STEPQ_E_UNSUPPORTED, "more than 2^20 tokens in a page");
     if (static_cast<int64_t>(d->n_pages) * d->n_kv_heads >= (int64_t(1) << 31))
         return set_error(STEPQ_E_UNSUPPORTED, "2^31 or more (page, head) records in a cache");
+    if (static_cast<double>(d->n_pages) * d->n_kv_heads * cache_shape(d).record >= 0x1p37)      // offsets in 32 bytes have 32 bits
+        return set_error(STEPQ_E_UNSUPPORTED, "2^37 bytes or more in a cache");
     return STEPQ_OK;
 }
 
@@ -225,21 +227,25 @@ struct BoundsArgs {
     int32_t batch, max_pages, turns;     // workgroups that take the pages of one (request, head) in turn
 };
 
-// Towards -inf to bfloat16; a NaN stays one.
+// Towards -inf to bfloat16.
 __device__ __forceinline__ bf16_t bf16_below(float x)
 {
     const uint32_t u = __float_as_uint(x);
-    if (x != x) return 0x7fc0;
     return static_cast<bf16_t>((u >> 31 ? u + 0xffffu : u) >> 16);
 }
 
+// A thread takes 4 bytes of every row of its group: 4 dimensions of 8-bit codes,
+// nibbles 0 .. 3 of 2 words of 4-bit ones; the groups of rows join in LDS.
 template <int D, int BITS>
 __global__ __launch_bounds__(kThreads) void cache_bounds_kernel(BoundsArgs a)
 {
-    using S = Share<D, BITS>;
-    constexpr int rows = kThreads / S::lanes;
-    __shared__ float part[4][2][D];
-    const int lane = threadIdx.x % S::lanes, wave = threadIdx.x >> 6;
+    using Row = RowOf<D, BITS>;
+    constexpr int cols = Row::bytes / 4, groups = kThreads / cols, E = 32 / BITS, NG = Row::scales, U = 4;
+    __shared__ float part[2][groups][D];
+    __shared__ uint32_t nans;                         // of each group of dimensions
+    const int col = threadIdx.x % cols, group = threadIdx.x / cols;
+    const auto dim = [&](int i) { return BITS == 8 ? 4 * col + i : i % 4 * (D / 4) + 2 * col + i / 4; };
+    const auto scale_of = [](int i) { return NG == 1 ? 0 : i % 4 * (D / 4) / kGroup4; };
     int x = blockIdx.x;
     const int turn = x % a.turns;
     x /= a.turns;
@@ -253,39 +259,48 @@ __global__ __launch_bounds__(kThreads) void cache_bounds_kernel(BoundsArgs a)
         const uint8_t *rec = record_of(a.c, id, hk);
         if (!rec) continue;
         const int n = min(a.c.page, len - p * a.c.page);
-        float lo[16], hi[16];
+        if (threadIdx.x == 0) nans = 0;
+        float lo[E], hi[E];
+        uint32_t nan = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
-        const auto join = [](float &l, float &h, float yl, float yh) {      // a NaN stays
-            l = yl < l || yl != yl ? yl : l;
-            h = yh > h || yh != yh ? yh : h;
-        };
-        for (int r = threadIdx.x / S::lanes; r < n; r += rows) {
-            float e[16];
-            values_of<D, BITS>(rec, a.c.page, false, r, lane, e);
+        for (int i = 0; i < E; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
+        for (int r0 = group; r0 < n; r0 += groups * U) {
+            uint32_t w[U];
+            float s[U][NG];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) join(lo[i], hi[i], e[i], e[i]);
+            for (int u = 0; u < U; ++u) {             // past the end: the last row again
+                const int r = min(r0 + u * groups, n - 1);
+                w[u] = reinterpret_cast<const uint32_t *>(rec + Row::codes(a.c.page, false, r))[col];
+                const bf16_t *sc = reinterpret_cast<const bf16_t *>(rec + Row::scale(a.c.page, false, r));
+#pragma unroll
+                for (int m = 0; m < NG; ++m) s[u][m] = widen(sc[m]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int m = 0; m < NG; ++m) nan |= (s[u][m] != s[u][m]) << m;
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const int c = BITS == 8 ? static_cast<int8_t>(w[u] >> (8 * i))
+                                            : static_cast<int32_t>(w[u] << (28 - 16 * (i / 4) - 4 * (i % 4))) >> 28;
+                    const float y = s[u][scale_of(i)] * static_cast<float>(c);
+                    lo[i] = fminf(lo[i], y), hi[i] = fmaxf(hi[i], y);
+                }
+            }
         }
 #pragma unroll
-        for (int m = S::lanes; m < 64; m <<= 1)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) join(lo[i], hi[i], __shfl_xor(lo[i], m), __shfl_xor(hi[i], m));
-        if ((threadIdx.x & 63) < S::lanes)
-#pragma unroll
-            for (int j = 0; j < S::runs; ++j)
-#pragma unroll
-                for (int i = 0; i < S::run; ++i) {
-                    part[wave][0][S::dim(lane, j) + i] = lo[j * S::run + i];
-                    part[wave][1][S::dim(lane, j) + i] = hi[j * S::run + i];
-                }
+        for (int i = 0; i < E; ++i) part[0][group][dim(i)] = lo[i], part[1][group][dim(i)] = hi[i];
+        __syncthreads();
+        if (nan) atomicOr(&nans, nan);
         __syncthreads();
         bf16_t *to = a.bounds + (static_cast<size_t>(id) * a.c.Hkv + hk) * 2 * D;
-        for (int i = threadIdx.x; i < D; i += kThreads) {
-            float l = part[0][0][i], h = part[0][1][i];
+        for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
+            const int d = i % D;
+            float y = part[i / D][0][d];
 #pragma unroll
-            for (int w = 1; w < 4; ++w) join(l, h, part[w][0][i], part[w][1][i]);
-            to[i] = bf16_below(l);
-            to[D + i] = h != h ? 0x7fc0 : bf16_below(-h) ^ 0x8000u;
+            for (int j = 1; j < groups; ++j) y = i < D ? fminf(y, part[0][j][d]) : fmaxf(y, part[1][j][d]);
+            const bf16_t v = i < D ? bf16_below(y) : bf16_below(-y) ^ 0x8000u;
+            to[i] = nans >> (NG == 1 ? 0 : d / kGroup4) & 1 ? 0x7fc0 : v;
         }
         __syncthreads();
     }
@@ -399,7 +414,7 @@ extern "C" stepq_status stepq_cache_bounds(const stepq_cache_desc *d, const void
     if (!starts || !lengths || !bounds) return bad("NULL starts, lengths or bounds");
     if (!aligned(bounds, 16)) return bad("bounds must be 16-byte aligned");
     const int64_t pairs = static_cast<int64_t>(batch) * d->n_kv_heads;
-    const int32_t turns = static_cast<int32_t>(std::clamp<int64_t>(4096 / pairs, 1, max_pages));
+    const int32_t turns = static_cast<int32_t>(std::clamp<int64_t>(1024 / pairs, 1, max_pages));
     const BoundsArgs a{cache_view(d, cache), page_table, starts, lengths, static_cast<bf16_t *>(bounds), batch, max_pages, turns};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_shape(d, [&](auto D, auto B) {

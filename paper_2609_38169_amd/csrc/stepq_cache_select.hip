@@ -31,117 +31,204 @@ __device__ __forceinline__ uint32_t key_of(float x)
 }
 
 // score = sum_d hi_d sum_h max(q_hd, 0) + lo_d sum_h min(q_hd, 0): a lane keeps
-// the sums over the heads for 8 dimensions of one bound and takes page after page;
-// D/4 lanes make a page's score.  In 64 bits, so that no order of summation
-// tells: the score is rounded once.
+// the sums over the heads for 8 dimensions of one bound and takes page after page,
+// four at a time; D/4 lanes make a page's score.  In 64 bits, so that no order of
+// summation tells: the score is rounded once.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
 {
-    constexpr int lanes = D / 4, at_once = 256 / lanes;
+    constexpr int lanes = D / 4, at_once = 256 / lanes, U = 4;
     const int lane = threadIdx.x % lanes, sub = threadIdx.x / lanes;
     int x = blockIdx.x;
     const int turn = x % a.turns;
     x /= a.turns;
     const int hk = x % a.Hkv, b = x / a.Hkv;
-    const int pages = pages_of(a, b);
-    if (pages <= a.n_select) return;             // all are taken
-    const int end = pages - a.n_last;
+    const int pages = pages_of(a, b), end = pages - a.n_last;
+    if (pages <= a.n_select || a.n_first + turn * at_once * U >= end) return;
     const bool high = lane >= lanes / 2;
     const int d0 = lane % (lanes / 2) * 8;
     double w[8] = {};
     const T *q = static_cast<const T *>(a.q) + (static_cast<size_t>(b) * a.Hkv + hk) * a.G * D + d0;
-    for (int h = 0; h < a.G; ++h)
+    struct alignas(16) Eight {
+        T x[8];
+    };
+    for (int h = 0; h < a.G; ++h) {
+        const Eight e = *reinterpret_cast<const Eight *>(q + static_cast<size_t>(h) * D);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float y = widen(q[static_cast<size_t>(h) * D + i]);
+            const float y = widen(e.x[i]);
             // a NaN reaches both sums
             w[i] += static_cast<double>(high ? (y < 0.0f ? 0.0f : y) : (y > 0.0f ? 0.0f : y));
         }
+    }
     const int32_t *table = a.table + static_cast<size_t>(b) * a.max_pages;
     uint32_t *keys = a.keys + (static_cast<size_t>(b) * a.Hkv + hk) * a.max_pages;
-    for (int p0 = a.n_first + turn * at_once; p0 < end; p0 += a.turns * at_once) {
-        const int p = p0 + sub;
-        const int id = p < end ? table[p] : -1;
-        const bool there = id >= 0 && id < a.n_pages;
-        double sum = 0.0;
-        if (there) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(a.bounds + ((static_cast<size_t>(id) * a.Hkv + hk) * 2 + high) * D + d0);
-            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    const auto ids = [&](int p0, int (&id)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = p0 + u * at_once + sub;
+            id[u] = p < end ? table[p] : -1;
+        }
+    };
+    int next[U];
+    ids(a.n_first + turn * at_once * U, next);
+    for (int p0 = a.n_first + turn * at_once * U; p0 < end; p0 += a.turns * at_once * U) {
+        uint4 v[U];
+        bool there[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            there[u] = next[u] >= 0 && next[u] < a.n_pages;
+            v[u] = make_uint4(0, 0, 0, 0);
+            if (there[u])
+                v[u] = *reinterpret_cast<const uint4 *>(a.bounds + ((static_cast<size_t>(next[u]) * a.Hkv + hk) * 2 + high) * D + d0);
+        }
+        ids(p0 + a.turns * at_once * U, next);
+        double sum[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t y[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+            sum[u] = 0.0;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                sum = fma(w[i], static_cast<double>(__uint_as_float(i % 2 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16)), sum);
+                sum[u] = fma(w[i], static_cast<double>(__uint_as_float(i % 2 ? y[i / 2] & 0xffff0000u : y[i / 2] << 16)), sum[u]);
         }
 #pragma unroll
-        for (int m = 1; m < lanes; m <<= 1) sum += __shfl_xor(sum, m);
-        if (lane == 0 && p < end) keys[p] = there ? key_of(static_cast<float>(sum)) : 0;
+        for (int m = 1; m < lanes; m <<= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) sum[u] += __shfl_xor(sum[u], m);
+        // lane u of the page's lanes writes score u
+        double mine = sum[0];
+        bool mine_there = there[0];
+#pragma unroll
+        for (int u = 1; u < U; ++u)
+            if (lane == u) mine = sum[u], mine_there = there[u];
+        const int p = p0 + lane * at_once + sub;
+        if (lane < U && p < end) keys[p] = mine_there ? key_of(static_cast<float>(mine)) : 0;
     }
 }
 
 // The n_first first and n_last last pages and the highest scores between them,
-// ties to the lowest position: the lowest score that is taken found digit by digit
-// of its key (8 bits each), then one pass over the pages in order.
-__global__ __launch_bounds__(256) void cache_select_kernel(SelectArgs a)
+// ties to the lowest position.  The lowest score that is taken is found by
+// counting scores in 2048 intervals of [low, high], which becomes the interval that
+// holds it, until that is a single number (2 or 3 times as a rule: scores lie
+// close together, so that intervals of their own range tell them apart where
+// their first digits would not); then the pages are written in order.  A thread holds
+// EACH pages of a stretch; more pages are read again, stretch by stretch.
+template <int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void cache_select_kernel(SelectArgs a)
 {
-    __shared__ uint32_t count[256];
-    __shared__ uint32_t chosen[2], before[4][2];
-    const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    constexpr int BINS = 2048, PER = BINS / THREADS, W = THREADS / 64, STRETCH = THREADS * EACH;
+    __shared__ uint32_t count[BINS];
+    __shared__ uint32_t found[2], ends[W][2], waves[W];
+    __shared__ uint32_t mores[EACH][W], sames[EACH][W];
+    const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int pages = pages_of(a, b);
     int32_t *out = a.selected + (static_cast<size_t>(b) * a.Hkv + hk) * a.n_select;
     if (pages <= a.n_select) {
-        for (int i = tid; i < a.n_select; i += 256) out[i] = i < pages ? i : -1;
+        for (int i = tid; i < a.n_select; i += THREADS) out[i] = i < pages ? i : -1;
         return;
     }
     const uint32_t *keys = a.keys + (static_cast<size_t>(b) * a.Hkv + hk) * a.max_pages;
     const int end = pages - a.n_last;
-    uint32_t want = a.n_select - a.n_first - a.n_last, prefix = 0, mask = 0;
-    for (int i = tid; i < a.n_first; i += 256) out[i] = i;
-    for (int i = tid; i < a.n_last; i += 256) out[a.n_select - a.n_last + i] = end + i;
+    uint32_t want = a.n_select - a.n_first - a.n_last;
+    for (int i = tid; i < a.n_first; i += THREADS) out[i] = i;
+    for (int i = tid; i < a.n_last; i += THREADS) out[a.n_select - a.n_last + i] = end + i;
     if (want == 0) return;
-    // of the keys that begin with `prefix`, the want-th highest is looked for
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        count[tid] = 0;
-        __syncthreads();
-        for (int p = a.n_first + tid; p < end; p += 256) {
-            const uint32_t k = keys[p];
-            if ((k & mask) == prefix) atomicAdd(&count[k >> shift & 255], 1u);
+    const bool whole = end - a.n_first <= STRETCH;
+    uint32_t k[EACH];
+    const auto load = [&](int p0) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int p = p0 + i * THREADS + tid;
+            if (p < end) k[i] = keys[p];
         }
-        __syncthreads();
-        if (tid == 0) {
-            uint32_t left = want;
-            int d = 255;
-            for (; d > 0 && count[d] < left; --d) left -= count[d];
-            chosen[0] = static_cast<uint32_t>(d), chosen[1] = left;
-        }
-        __syncthreads();
-        prefix |= chosen[0] << shift, mask |= 255u << shift, want = chosen[1];
-        __syncthreads();
+    };
+    // f(i, p) for every page of the thread's, whose key is k[i]
+    const auto each = [&](int p0, auto &&f) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (p0 + i * THREADS + tid < end) f(i);
+    };
+    uint32_t low = 0xffffffffu, high = 0;
+    for (int p0 = a.n_first; p0 < end; p0 += STRETCH) {
+        load(p0);
+        each(p0, [&](int i) { low = min(low, k[i]), high = max(high, k[i]); });
     }
-    // keys above `prefix`, and the first `want` of those equal to it
-    uint32_t taken = 0, equal = 0;
-    for (int p0 = a.n_first; p0 < end; p0 += 256) {
-        const int p = p0 + tid;
-        const uint32_t k = p < end ? keys[p] : 0;
-        const bool more = p < end && k > prefix, same = p < end && k == prefix;
-        const uint64_t ms = __ballot(same);
-        const uint32_t es = __popcll(ms & ((1ull << lane) - 1));
-        if (lane == 0) before[wave][0] = __popcll(ms);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        low = min(low, static_cast<uint32_t>(__shfl_xor(static_cast<int>(low), m)));
+        high = max(high, static_cast<uint32_t>(__shfl_xor(static_cast<int>(high), m)));
+    }
+    if (lane == 0) ends[wave][0] = low, ends[wave][1] = high;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) low = min(low, ends[w][0]), high = max(high, ends[w][1]);
+    while (low < high) {                              // the want-th highest of those in [low, high] is looked for
+        const int shift = max(0, 21 - __clz(high - low));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) count[i * THREADS + tid] = 0;
         __syncthreads();
-        uint32_t e = equal + es, all_e = equal;
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) e += before[w][0];
-            all_e += before[w][0];
+        for (int p0 = a.n_first; p0 < end; p0 += STRETCH) {
+            if (!whole) load(p0);
+            each(p0, [&](int i) {
+                if (k[i] >= low && k[i] <= high) atomicAdd(&count[(k[i] - low) >> shift], 1u);
+            });
         }
-        const bool take = more || (same && e < want);
-        const uint64_t mt = __ballot(take);
-        if (lane == 0) before[wave][1] = __popcll(mt);
         __syncthreads();
-        uint32_t at = taken + __popcll(mt & ((1ull << lane) - 1)), all_t = taken;
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) at += before[w][1];
-            all_t += before[w][1];
+        // how many lie above each thread's intervals, PER neighbours of them
+        uint32_t mine[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) mine[i] = count[tid * PER + i], sum += mine[i];
+        uint32_t from = sum;                          // its own and those of the wave's higher lanes
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const uint32_t y = __shfl_down(static_cast<int>(from), m);
+            if (lane + m < 64) from += y;
         }
-        if (take) out[a.n_first + at] = p;
-        taken = all_t, equal = all_e;
+        if (lane == 0) waves[wave] = from;
+        __syncthreads();
+        uint32_t above = from - sum;
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (w > wave) above += waves[w];
+#pragma unroll
+        for (int i = PER - 1; i >= 0; --i) {
+            if (above < want && above + mine[i] >= want) found[0] = tid * PER + i, found[1] = want - above;
+            above += mine[i];
+        }
+        __syncthreads();
+        low += found[0] << shift;
+        high = low + min(high - low, (1u << shift) - 1);
+        want = found[1];
+    }
+    // keys above `low`, and the first `want` of those equal to it
+    uint32_t more0 = 0, same0 = 0;                    // of the stretches before
+    for (int p0 = a.n_first; p0 < end; p0 += STRETCH) {
+        if (!whole) load(p0);
+        uint64_t bm[EACH], bs[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const bool in = p0 + i * THREADS + tid < end;
+            bm[i] = __ballot(in && k[i] > low), bs[i] = __ballot(in && k[i] == low);
+            if (lane == 0) mores[i][wave] = __popcll(bm[i]), sames[i][wave] = __popcll(bs[i]);
+        }
+        __syncthreads();
+        const uint64_t below = (1ull << lane) - 1;
+        uint32_t m = more0, s = same0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            uint32_t mw = m, sw = s;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                if (w < wave) mw += mores[i][w], sw += sames[i][w];
+                m += mores[i][w], s += sames[i][w];
+            }
+            const uint32_t before = mw + __popcll(bm[i] & below), equal = sw + __popcll(bs[i] & below);
+            if ((bm[i] >> lane & 1) || ((bs[i] >> lane & 1) && equal < want))
+                out[a.n_first + before + min(equal, want)] = p0 + i * THREADS + tid;
+        }
+        more0 = m, same0 = s;
         __syncthreads();
     }
 }
@@ -199,7 +286,7 @@ extern "C" stepq_status stepq_cache_select(const stepq_cache_desc *c, const step
     if (d->max_pages && !page_table) return bad("page_table is NULL");
     if (!q || !lengths || !selected) return bad("NULL q, lengths or selected");
     if (c->n_pages && !bounds) return bad("NULL bounds");
-    if (!aligned(q, d->act_dtype == STEPQ_F32 ? 4 : 2) || !aligned(bounds, 16)) return bad("bounds must be 16-byte aligned, q to its type");
+    if (!aligned(q, 16) || !aligned(bounds, 16)) return bad("q and bounds must be 16-byte aligned");
     const size_t need = workspace_of(c, d);
     if (need && (!workspace || workspace_bytes < need)) return bad("workspace is smaller than stepq_cache_select_workspace()");
     if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
@@ -209,11 +296,13 @@ extern "C" stepq_status stepq_cache_select(const stepq_cache_desc *c, const step
                  d->n_first, d->n_last, 1, fast_div(static_cast<uint32_t>(c->page_size))};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (need) {
-        const int64_t at_once = 1024 / c->head_dim;          // pages of a workgroup's turn
+        const int64_t at_once = 4 * 1024 / c->head_dim;      // pages of a workgroup's turn
         a.turns = static_cast<int32_t>(std::clamp<int64_t>(2048 / pairs, 1, (d->max_pages + at_once - 1) / at_once));
         if (d->act_dtype == STEPQ_BF16) score<bf16_t>(a, c->head_dim, s);
         else score<float>(a, c->head_dim, s);
     }
-    cache_select_kernel<<<dim3(static_cast<unsigned>(pairs)), 256, 0, s>>>(a);
+    const dim3 grid(static_cast<unsigned>(pairs));
+    if (d->max_pages <= 256 * 4) cache_select_kernel<256, 4><<<grid, 256, 0, s>>>(a);
+    else cache_select_kernel<1024, 8><<<grid, 1024, 0, s>>>(a);
     return launched("cache select launch");
 }
