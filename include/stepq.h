@@ -465,7 +465,7 @@ stepq_status stepq_prefix_attention(const stepq_attn_desc *desc, const void *q, 
  * [0, n_pages) is no page: nothing is written there or read from there.
  */
 typedef struct {
-    int32_t n_pages;          /* >= 0 */
+    int32_t n_pages;          /* >= 0; the whole cache takes less than 2^37 bytes */
     int32_t n_kv_heads;       /* Hkv >= 1 */
     int32_t page_size;        /* P: tokens per page, 1 .. 2^20 */
     int32_t head_dim;         /* D: 64, 128 or 256 */

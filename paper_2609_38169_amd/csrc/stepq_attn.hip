@@ -33,6 +33,18 @@ __device__ __forceinline__ int token_row(const AttnArgs &a, const int32_t *pages
     return id >= 0 && id < a.n_pages ? (id * a.Hkv + hk) * a.page + (t - p * a.page) : -1;
 }
 
+// A running softmax: maximum and sum of what was seen; next() returns the
+// factor on everything so far when scores of maximum m join.
+struct Running {
+    float m = -INFINITY, l = 0.0f, base = 0.0f;
+    __device__ __forceinline__ float next(float top)
+    {
+        const float to = fmaxf(m, top), b = to == -INFINITY ? 0.0f : to, f = __builtin_amdgcn_exp2f(m - b);
+        m = to, base = b, l *= f;
+        return f;
+    }
+};
+
 // ---------------------------------------------------------------------------
 // Few queries per key: a workgroup takes 16 query rows (the group's heads of
 // one request over a range of its own tokens, or 16 rows of all requests over a
@@ -457,6 +469,65 @@ __global__ __launch_bounds__(512, 2) void attn_prefix_kernel(AttnArgs a)
     }
 }
 
+// The parts of each row joined: W waves per row take parts in turn, a few at a
+// time so that their loads overlap.  Few rows (up to 1024): 4 waves, as latency
+// counts; a request over 16384 tokens, 16 heads of 256 in 65 parts, in all: 37 us
+// with one load after the other in a wave, 20 so.  More: a wave each, bound by
+// the parts' bytes; 9 x 8192 rows of 256 (75 MB) in 14 us, 3 more with 4 waves.
+// Whole calls, one wave / 4, us, 64 dimensions over 1024 tokens: 32 rows 8.6 / 7.3,
+// 1024 13.5 / 12.1, 2048 17.9 / 17.1, 8192 48 / 50; 256 over 4096: 128 19.3 / 17.5,
+// 1024 51.5 / 50.7, 2048 50.5 / 53.2, 16384 178 / 185.
+// (Joined in attn_rows_kernel instead, which has few waves to wait with, 512
+// requests take 225 us in all, not 208.)
+template <typename T, int D, int W>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+{
+    constexpr int E = D / 64, U = 4;
+    using Piece = __attribute__((ext_vector_type(E))) float;
+    __shared__ alignas(16) float sum[4][D];
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % W, lane = threadIdx.x & 63;
+    const size_t total = static_cast<size_t>(a.batch) * a.Hq, row = static_cast<size_t>(blockIdx.x) * (4 / W) + w / W;
+    if (W == 1 && row >= total) return;
+    const int parts = a.prefix_parts + a.own_parts;
+    const auto stats = [&](int c) { return c + lane < parts ? a.ml[(c + lane) * total + row] : make_float2(-INFINITY, 0.0f); };
+    const float2 first = stats(0);
+    float top = first.x;
+    for (int c = 64; c < parts; c += 64) top = fmaxf(top, stats(c).x);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float base = top == -INFINITY ? 0.0f : top;
+    Piece y = {};
+    float z = 0.0f;
+    for (int c = 0; c < parts; c += 64) {
+        const float2 ml = c == 0 ? first : stats(c);
+        const float f = __builtin_amdgcn_exp2f(ml.x - base);
+        z = fmaf(ml.y, f, z);
+        const int n = min(64, parts - c);
+        for (int p = wave; p < n; p += W * U) {
+            Piece x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                x[u] = reinterpret_cast<const Piece *>(a.acc + ((c + min(p + W * u, n - 1)) * total + row) * D)[lane];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + W * u < n) y += x[u] * __shfl(f, p + W * u);
+        }
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) z += __shfl_xor(z, x);
+    T *o = static_cast<T *>(a.o) + row * D;
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[lane * E + e] = narrow<T>(z == 0.0f ? 0.0f : y[e] / z);
+    } else {
+        *reinterpret_cast<Piece *>(&sum[w][lane * E]) = y;
+        __syncthreads();
+        const int d = threadIdx.x;
+        if (d < D) o[d] = narrow<T>(z == 0.0f ? 0.0f : (sum[0][d] + sum[1][d] + sum[2][d] + sum[3][d]) / z);
+    }
+    if (wave == 0 && lane == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
+}
+
 stepq_status check(const stepq_attn_desc *d)
 {
     if (!d) return bad("desc is NULL");
@@ -536,7 +607,9 @@ void launch(AttnArgs a, const Split &s, hipStream_t st)
             attn_prefix_kernel<D><<<dim3(static_cast<unsigned>(grid)), 512, 0, st>>>(a);
         }
     attn_rows_kernel<T, D><<<dim3(static_cast<unsigned>(a.prefix_items + own)), 256, 0, st>>>(a);
-    join_parts<T, D>({a.ml, a.acc, a.o, a.lse, static_cast<size_t>(a.batch) * a.Hq, a.prefix_parts + a.own_parts, nullptr, 0, 0, 0}, st);
+    const unsigned rows = static_cast<unsigned>(a.batch) * a.Hq;
+    if (rows <= 1024) attn_join_kernel<T, D, 4><<<dim3(rows), 256, 0, st>>>(a);
+    else attn_join_kernel<T, D, 1><<<dim3((rows + 3) / 4), 256, 0, st>>>(a);
 }
 
 template <typename T>

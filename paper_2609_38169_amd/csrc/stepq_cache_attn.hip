@@ -17,17 +17,25 @@ struct CacheAttnArgs {
     float2 *ml;              // [parts][batch * Hq]: a part's maximum (in powers of two) and sum
     float *acc;              // [parts][batch * Hq][D]: its unnormalised output
     int32_t batch, Hq, G, max_pages, n_select, parts, chunk;
+    FastDiv div_items, div_blocks, div_hkv;      // by the workgroups of one part, by the blocks of 16 heads, by Hkv
     float scale;             // times log2 e: scores are kept in powers of two
 };
 
 #ifndef CUT_WGS
-#define CUT_WGS 2048
+#define CUT_WGS 4096
 #endif
 #ifndef CUT_MIN
 #define CUT_MIN 256
 #endif
+constexpr int kMaxChunk = 1024;
 constexpr int kTile = 32;    // keys of a wave's turn
-constexpr int kMaxChunk = 2048;
+// Waves of a SIMD that the registers are for.
+template <typename T, int D>
+constexpr int waves_of()
+{
+    if (D == 256) return 1;
+    return sizeof(T) == 4 ? 2 : 3;
+}
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -38,21 +46,17 @@ __device__ __forceinline__ uint32_t bytes_of(uint32_t w, int i, int j)
 {
     return pack_bf16(static_cast<float>(static_cast<int8_t>(w >> (8 * i))), static_cast<float>(static_cast<int8_t>(w >> (8 * j))));
 }
-// The low nibble of byte B as a sixteenth of its code (exact), and nibble j of both halves of a word so.
-template <int B>
-__device__ __forceinline__ float sixteenth(uint32_t w)
+// The nibbles of a word as sixteenths of their codes (exact): byte b's lower one, or of w >> 4 its upper one.
+__device__ __forceinline__ float sixteenth(uint32_t w, int b) { return __builtin_amdgcn_cvt_off_f32_i4(w >> (8 * b) & 0xff); }
+// Nibble j of both halves of a word so, as bfloat16, for all four.
+__device__ __forceinline__ void nibbles_of(uint32_t w, uint32_t (&y)[4])
 {
-    float y;
-    if constexpr (B == 0) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(y) : "v"(w));
-    if constexpr (B == 1) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(y) : "v"(w));
-    if constexpr (B == 2) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(y) : "v"(w));
-    if constexpr (B == 3) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(y) : "v"(w));
-    return y;
-}
-__device__ __forceinline__ uint32_t nibbles_of(uint32_t w, int j)
-{
-    const uint32_t u = j % 2 ? w >> 4 : w;
-    return j / 2 ? pack_bf16(sixteenth<1>(u), sixteenth<3>(u)) : pack_bf16(sixteenth<0>(u), sixteenth<2>(u));
+    uint32_t u = w >> 4;
+    asm("" : "+v"(u));                   // one shift, and bytes chosen by the conversions
+    y[0] = pack_bf16(sixteenth(w, 0), sixteenth(w, 2));
+    y[1] = pack_bf16(sixteenth(u, 0), sixteenth(u, 2));
+    y[2] = pack_bf16(sixteenth(w, 1), sixteenth(w, 3));
+    y[3] = pack_bf16(sixteenth(u, 1), sixteenth(u, 3));
 }
 // The same as bfloat16 1.5 + code / 16, put into the upper bits of a 1's mantissa with the sign turned: two
 // instructions in place of 3 1/4.  Only for sums that 1.5 times the other operand may be taken off.
@@ -62,56 +66,56 @@ __device__ __forceinline__ uint32_t raised_nibbles_of(uint32_t w, int j)
 }
 constexpr uint32_t kRaised = 0x3fc03fc0u;           // 1.5 twice
 
+// Two floats rounded to bfloat16, and what that leaves of them so.
+__device__ __forceinline__ void two_planes(float a, float b, bf16x2 &hi, bf16x2 &lo)
+{
+    hi = __builtin_convertvector((f32x2{a, b}), bf16x2);
+    lo = __builtin_convertvector((f32x2{a - static_cast<float>(hi[0]), b - static_cast<float>(hi[1])}), bf16x2);
+}
+
 // One of a request's key heads, 16 of its query heads, `chunk` of its tokens
-// (all of them, or those of its selected pages): the waves take tiles of 32 keys
-// in turn.  Scores are formed transposed, keys x queries, from codes as bfloat16
+// (all of them, or those of its selected pages): the waves take tiles of keys in
+// turn.  Scores are formed transposed, keys x queries, from codes as bfloat16
 // (exact), each group's sum times its scale; values pass through LDS of the wave's
 // own as codes, to be read by columns of 16 bits, 2 or 4 dimensions at once, and
 // their scales go into the weights.  The next tile's codes and scales are on their way
 // meanwhile, into the registers that the tile's codes have left.
 template <typename T, int D, int BITS>
-__global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (D == 256 ? 1 : 2) : D == 256 ? 2 : 3)) void cache_attn_kernel(CacheAttnArgs a)
+__global__ __launch_bounds__(256, (waves_of<T, D>()))
+void cache_attn_kernel(CacheAttnArgs a)
 {
-    constexpr bool BF = sizeof(T) == 2;
+    constexpr bool BF = sizeof(T) == 2, RAISED = BITS == 4 && BF;
     using Row = RowOf<D, BITS>;
-    constexpr int RB = Row::bytes, NG = Row::scales, RT = kTile / 16;
+    constexpr int RB = Row::bytes, NG = Row::scales, KT = kTile, RT = KT / 16;
     constexpr int LB = RB / 4, PB = LB < 16 ? LB : 16, PIECES = LB / PB;     // bytes of a row per lane group, in loads of PB
     constexpr int STEPS = D / 32, QP = BF ? 1 : 3, PP = BF ? 2 : 3;          // products over D; planes of queries and weights
     constexpr int VS = 32 * (RB / 32 | 1);            // a row of values in LDS: 16 rows' 32 bytes fall on all banks
-    constexpr int LD = D + 4, VB = 4 * kTile * VS, SB = 16 * LD * 4;
-    __shared__ alignas(16) uint8_t vs[VB > SB ? VB : SB];
-    __shared__ alignas(16) float sc[4][2][NG][kTile];
+    constexpr int LD = D + 4, VB = 4 * KT * VS, SB = 4 * 16 * LD * 4;
+    constexpr int PAGES = (kMaxChunk + 1) * static_cast<int>(sizeof(int2));
+    __shared__ alignas(16) uint8_t vs[VB + PAGES > SB ? VB + PAGES : SB];     // values and pages; in the end the waves' sums
+    __shared__ alignas(16) float sc[4][2][NG][KT];
     __shared__ float sm[4][16], sl[4][16];
-    __shared__ int2 pages[kMaxChunk + 1];             // the chunk's pages: record (-1: none), tokens that count
+    int2 *pages = reinterpret_cast<int2 *>(vs + VB);  // the chunk's pages: record (-1: none), tokens that count
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
-    const int blocks = (a.G + 15) / 16, Hkv = a.c.Hkv, page = a.c.page;
-    int x = blockIdx.x;
-    const int part = x % a.parts;
-    x /= a.parts;
-    const int row0 = x % blocks * 16;
-    x /= blocks;
-    const int hk = x % Hkv, b = x / Hkv, rows = min(16, a.G - row0);
-    const int len = min(max(a.lengths[b], 0), a.max_pages * page);
-    const int total = a.selected ? a.n_select * page : len;
-    const int from = part * a.chunk, to = min(total, from + a.chunk);
-    if (part && from >= total) return;
+    const int Hkv = a.c.Hkv, page = a.c.page;
+    const int part = fdiv(blockIdx.x, a.div_items), item = blockIdx.x - part * (a.batch * Hkv * ((a.G + 15) / 16));
+    const int bh = fdiv(item, a.div_blocks), row0 = (item - bh * ((a.G + 15) / 16)) * 16;
+    const int b = fdiv(bh, a.div_hkv), hk = bh - b * Hkv, rows = min(16, a.G - row0);
     const int32_t *table = a.table + static_cast<size_t>(b) * a.max_pages;
-    const int32_t *chosen = a.selected ? a.selected + (static_cast<size_t>(b) * Hkv + hk) * a.n_select : nullptr;
-    const int first_page = page_of(from, a.c.div_page);
-    if (from < to)
-        for (int p = first_page + threadIdx.x, last = page_of(to - 1, a.c.div_page); p <= last; p += 256) {
-            const int pos = chosen ? chosen[p] : p;
-            int2 e = make_int2(-1, 0);
-            if (pos >= 0 && pos < a.max_pages && pos * page < len) {
-                const int id = table[pos];
-                if (id >= 0 && id < a.c.n_pages) e = make_int2(id * Hkv + hk, len - pos * page);
-            }
-            pages[p - first_page] = e;
-        }
+    const int32_t *chosen = a.selected ? a.selected + static_cast<size_t>(bh) * a.n_select : nullptr;
+    const int from = part * a.chunk, most = (chosen ? a.n_select : a.max_pages) * page;
+    const int first_page = page_of(from, a.c.div_page), end_page = page_of(min(most, from + a.chunk) - 1, a.c.div_page) + 1;
+    // page p's position and id; both are looked up before the length is there
+    const auto look = [&](int p, int &pos, int &id) {
+        pos = chosen ? chosen[p] : p;
+        id = pos >= 0 && pos < a.max_pages ? table[pos] : -1;
+    };
+    int pos0 = 0, id0 = -1;
+    if (most && first_page + static_cast<int>(threadIdx.x) < end_page) look(first_page + threadIdx.x, pos0, id0);
 
     // queries, operand B: query n, the 8 dimensions of each step that the codes of a lane group stand for
     const size_t qrow = static_cast<size_t>(b) * a.Hq + hk * a.G + row0 + min(n, rows - 1);
-    bf16x8 q[STEPS][QP];
+    u32x4 raw[STEPS][BF ? 1 : 2];
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
         // 8 bits: half st % 2 of piece st / 2; 4 bits: nibble st % 4 of piece st / 4 (D = 64: two nibbles of 4 words)
@@ -122,13 +126,32 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
         const T *from_q = static_cast<const T *>(a.q) + qrow * D;
         if constexpr (BF) {
             const u32x2 lo = *reinterpret_cast<const u32x2 *>(from_q + d0), hi = *reinterpret_cast<const u32x2 *>(from_q + d1);
-            q[st][0] = __builtin_bit_cast(bf16x8, with_sign(u32x4{lo[0], lo[1], hi[0], hi[1]}, a.scale, 0x80008000u));
+            raw[st][0] = u32x4{lo[0], lo[1], hi[0], hi[1]};
         } else {
-            const auto take = [&](int d) {
-                return __builtin_bit_cast(f32x4, with_sign(*reinterpret_cast<const u32x4 *>(from_q + d), a.scale, 0x80000000u));
-            };
+            raw[st][0] = *reinterpret_cast<const u32x4 *>(from_q + d0), raw[st][1] = *reinterpret_cast<const u32x4 *>(from_q + d1);
+        }
+    }
+    const int len = min(max(a.lengths[b], 0), a.max_pages * page);
+    const int total = chosen ? most : len, to = min(total, from + a.chunk);
+    if (part && from >= total) return;
+    const auto entry = [&](int pos, int id) {
+        return id >= 0 && id < a.c.n_pages && pos * page < len ? make_int2(id * Hkv + hk, len - pos * page) : make_int2(-1, 0);
+    };
+    if (first_page + static_cast<int>(threadIdx.x) < end_page) pages[threadIdx.x] = entry(pos0, id0);
+    for (int p = first_page + 256 + threadIdx.x; p < end_page; p += 256) {
+        int pos, id;
+        look(p, pos, id);
+        pages[p - first_page] = entry(pos, id);
+    }
+    bf16x8 q[STEPS][QP];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+        if constexpr (BF) {
+            q[st][0] = __builtin_bit_cast(bf16x8, with_sign(raw[st][0], a.scale, 0x80008000u));
+        } else {
             bf16x8 p[3];
-            split(take(d0), take(d1), p);
+            split(__builtin_bit_cast(f32x4, with_sign(raw[st][0], a.scale, 0x80000000u)),
+                  __builtin_bit_cast(f32x4, with_sign(raw[st][1], a.scale, 0x80000000u)), p);
 #pragma unroll
             for (int i = 0; i < 3; ++i) q[st][i] = p[i];
         }
@@ -136,7 +159,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
     // the group that a step's dimensions lie in
     const auto group_of = [](int st) { return NG == 1 ? 0 : st % 4 * (D / 4) / kGroup4; };
     // raised codes: what 1.5 adds to each query's sums is taken off where they begin
-    constexpr bool RAISED = BITS == 4 && BF;
     f32x4 qz[NG] = {};
     if constexpr (RAISED) {
         const bf16x8 zero[1] = {__builtin_bit_cast(bf16x8, (u32x4{kRaised, kRaised, kRaised, kRaised}))};
@@ -145,7 +167,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
 #pragma unroll
         for (int m = 0; m < NG; ++m) qz[m] = -qz[m];
     }
-    const auto key_nibbles = [](uint32_t w, int j) { return RAISED ? raised_nibbles_of(w, j) : nibbles_of(w, j); };
     const float scale = scale_of(a.scale);
     const auto wave_sync = [] {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -154,32 +175,31 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
     };
     __syncthreads();
 
-    uint8_t *mine = vs + wave * kTile * VS;
-    // a tile's key: lane l has key l % 32's record, row and whether it is there
+    uint8_t *mine = vs + wave * KT * VS;
+    // a tile's keys: lane l has the record and row of key l % KT; there: the keys that are (row 0 of the cache stands in)
     int64_t at = 0;
+    uint32_t unit = 0;                                // of its row, in 32 bytes
     int row = 0;
-    uint32_t none = ~0u;
+    uint32_t there = 0;
+    const uint32_t record_units = static_cast<uint32_t>(a.c.record / 32);
     const auto locate = [&](int t0) {
-        const int t = t0 + lane % kTile;
-        at = 0, row = 0;
-        bool there = false;
+        const int t = t0 + lane % KT;
+        at = 0, unit = 0, row = 0;
+        bool ok = false;
         if (t < to) {
             const int p = page_of(t, a.c.div_page), r = t - p * page;
             const int2 e = pages[p - first_page];
-            there = e.x >= 0 && r < e.y;
-            if (there) at = static_cast<int64_t>(e.x) * a.c.record, row = r;
+            ok = e.x >= 0 && r < e.y;
+            if (ok) at = static_cast<int64_t>(e.x) * a.c.record, row = r, unit = e.x * record_units + r * (RB / 32);
         }
-        none = ~static_cast<uint32_t>(__ballot(there));
+        there = static_cast<uint32_t>(__ballot(ok));
     };
     uint32_t kx[RT][LB / 4], vx[RT][LB / 4], sx[(NG + 1) / 2];
     const uint8_t *base[RT];
     const auto bases = [&] {
-        const int64_t off = at + row * RB;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const uint32_t lo = __shfl(static_cast<int>(off), 16 * rt + n), hi = __shfl(static_cast<int>(off >> 32), 16 * rt + n);
-            base[rt] = a.c.mem + static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo) + g * PB;
-        }
+        for (int rt = 0; rt < RT; ++rt)
+            base[rt] = a.c.mem + static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(unit), 16 * rt + n))) * 32 + g * PB;
     };
     const auto fetch = [&](uint32_t (&y)[RT][LB / 4], int behind) {
 #pragma unroll
@@ -192,19 +212,19 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
     };
     // lanes 0 .. 31: their key's scales; 32 .. 63: those of its value
     const auto fetch_scales = [&] {
-        const uint8_t *s = a.c.mem + at + Row::scale(page, lane >= kTile, row);
+        const uint8_t *s = a.c.mem + at + Row::scale(page, lane >= KT, row);
         if constexpr (NG == 1) sx[0] = *reinterpret_cast<const bf16_t *>(s);
         else
 #pragma unroll
-            for (int m = 0; m < NG / 2; ++m) sx[m] = reinterpret_cast<const uint32_t *>(s)[m];
+            for (int i = 0; i < NG / 2; ++i) sx[i] = reinterpret_cast<const uint32_t *>(s)[i];
     };
     float m = -INFINITY, low = 0.0f, l = 0.0f;        // the maximum, what is taken off the scores, the sum
     f32x4 acc[D / 16] = {};
     const int value_at = page * RB;
-    int t0 = from + wave * kTile;
-    for (; t0 < to; t0 += 4 * kTile) {                // the first tile with a key
+    int t0 = from + wave * KT;
+    for (; t0 < to; t0 += 4 * KT) {                   // the first tile with a key
         locate(t0);
-        if (none != ~0u) break;
+        if (there) break;
     }
     if (t0 < to) {
         bases();
@@ -213,12 +233,12 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
         fetch(kx, 0);
     }
     while (t0 < to) {
-        const uint32_t gone = none;
-        const bool there = !(gone >> (lane % kTile) & 1);
+        const uint32_t have = there;
+        const bool mine_there = have >> (lane % KT) & 1;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const float y = i % 2 ? upper_bf16(sx[i / 2]) : lower_bf16(sx[i / 2]);
-            sc[wave][lane / kTile][i][lane % kTile] = there ? (BITS == 4 ? 16.0f * y : y) : 0.0f;
+            sc[wave][lane / KT][i][lane % KT] = mine_there ? (BITS == 4 ? 16.0f * y : y) : 0.0f;
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -231,9 +251,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
                 *reinterpret_cast<Piece *>(mine + (16 * rt + n) * VS + (4 * i + g) * PB) = y;
             }
         wave_sync();
-        for (t0 += 4 * kTile; t0 < to; t0 += 4 * kTile) {
+        for (t0 += 4 * KT; t0 < to; t0 += 4 * KT) {
             locate(t0);
-            if (none != ~0u) break;
+            if (there) break;
         }
         if (t0 < to) {
             bases();
@@ -242,36 +262,57 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
         }
         // scores: lane (g, n) holds keys 16 rt + 4 g .. + 3 of query n
         f32x4 s[RT];
-        float top = -INFINITY;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             f32x4 y[NG];
 #pragma unroll
             for (int i = 0; i < NG; ++i) y[i] = qz[i];
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                u32x4 w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (BITS == 8) w[i] = bytes_of(kx[rt][st * 2 + i / 2], i % 2 * 2, i % 2 * 2 + 1);
-                    else if constexpr (D == 64) w[i] = key_nibbles(kx[rt][i % 2], 2 * st + i / 2);
-                    else w[i] = key_nibbles(kx[rt][st / 4 * 4 + i], st % 4);
-                }
+            const auto step = [&](int st, const u32x4 &w) {
                 const bf16x8 k[1] = {__builtin_bit_cast(bf16x8, w)};
                 mma(y[group_of(st)], k, q[st]);
-            }
-            s[rt] = f32x4{};
+            };
+            if constexpr (BITS == 8) {
 #pragma unroll
-            for (int i = 0; i < NG; ++i) s[rt] += y[i] * *reinterpret_cast<const f32x4 *>(&sc[wave][0][i][16 * rt + 4 * g]);
+                for (int st = 0; st < STEPS; ++st) {
+                    const uint32_t u = kx[rt][st * 2], v = kx[rt][st * 2 + 1];
+                    step(st, u32x4{bytes_of(u, 0, 1), bytes_of(u, 2, 3), bytes_of(v, 0, 1), bytes_of(v, 2, 3)});
+                }
+            } else {
+                constexpr int W = D == 64 ? 2 : 4;    // words of a piece
+#pragma unroll
+                for (int i = 0; i < LB / 4 / W; ++i) {
+                    uint32_t y4[W][4];
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        if constexpr (RAISED)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) y4[w][j] = raised_nibbles_of(kx[rt][i * W + w], j);
+                        else nibbles_of(kx[rt][i * W + w], y4[w]);
+                    }
+                    if constexpr (D == 64) {
+#pragma unroll
+                        for (int st = 0; st < 2; ++st)
+                            step(st, u32x4{y4[0][2 * st], y4[1][2 * st], y4[0][2 * st + 1], y4[1][2 * st + 1]});
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) step(4 * i + j, u32x4{y4[0][j], y4[1][j], y4[2][j], y4[3][j]});
+                    }
+                }
+            }
+            s[rt] = y[0] * *reinterpret_cast<const f32x4 *>(&sc[wave][0][0][16 * rt + 4 * g]);
+#pragma unroll
+            for (int i = 1; i < NG; ++i) s[rt] += y[i] * *reinterpret_cast<const f32x4 *>(&sc[wave][0][i][16 * rt + 4 * g]);
         }
         if (t0 < to) fetch(kx, 0);
-        if (gone) {
+        if (~have) {                                  // not all of the tile's keys are
+            const uint32_t x = have >> (4 * g);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (gone >> (16 * rt + 4 * g + i) & 1) s[rt][i] = -INFINITY;
+                    if (!(x >> (16 * rt + i) & 1)) s[rt][i] = -INFINITY;
         }
+        float top = s[0][0];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -298,14 +339,17 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
         bf16x8 p[NG][PP];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-            const f32x4 y0 = s[0] * *reinterpret_cast<const f32x4 *>(&sc[wave][1][i][4 * g]);
-            const f32x4 y1 = s[1] * *reinterpret_cast<const f32x4 *>(&sc[wave][1][i][16 + 4 * g]);
+            const float *vsc = &sc[wave][1][i][4 * g];
+            const f32x4 y0 = s[0] * *reinterpret_cast<const f32x4 *>(vsc);
+            const f32x4 y1 = s[1] * *reinterpret_cast<const f32x4 *>(vsc + 16);
             if constexpr (BF) {
-                const float y[8] = {y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    p[i][0][j] = static_cast<__bf16>(y[j]);
-                    p[i][1][j] = static_cast<__bf16>(y[j] - static_cast<float>(p[i][0][j]));
+                for (int j = 0; j < 4; ++j) {
+                    bf16x2 hi, lo;
+                    if (j < 2) two_planes(y0[2 * j], y0[2 * j + 1], hi, lo);
+                    else two_planes(y1[2 * j - 4], y1[2 * j - 3], hi, lo);
+                    p[i][0][2 * j] = hi[0], p[i][0][2 * j + 1] = hi[1];
+                    p[i][1][2 * j] = lo[0], p[i][1][2 * j + 1] = lo[1];
                 }
             } else {
                 split(y0, y1, p[i]);
@@ -313,19 +357,28 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
         }
 #pragma unroll
         for (int cb = 0; cb < RB / 32; ++cb) {
-            uint32_t w[4];                            // 16 columns of 16 bits: keys 4 g .. + 3, then 16 + 4 g .. + 3
+            uint32_t w[4];                        // 16 columns of 16 bits: keys 4 g .. + 3, then 16 + 4 g .. + 3
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x2 y = read_columns(mine + (16 * h + 4 * g + (n >> 2)) * VS + cb * 32 + (n & 3) * 8);
-                w[2 * h] = y[0], w[2 * h + 1] = y[1];
+            for (int i = 0; i < 2; ++i) {
+                const u32x2 y = read_columns(mine + (16 * i + 4 * g + (n >> 2)) * VS + cb * 32 + (n & 3) * 8);
+                w[2 * i] = y[0], w[2 * i + 1] = y[1];
             }
-            constexpr int per = BITS == 8 ? 2 : 4;    // dimensions in a column
+            constexpr int per = BITS == 8 ? 2 : 4;          // dimensions in a column
+            u32x4 u[per];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (BITS == 8) {
+                    u[0][i] = bytes_of(w[i], 0, 2), u[1][i] = bytes_of(w[i], 1, 3);
+                } else {
+                    uint32_t y[4];
+                    nibbles_of(w[i], y);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) u[j][i] = y[j];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < per; ++j) {
-                u32x4 u;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) u[i] = BITS == 8 ? bytes_of(w[i], j, j + 2) : nibbles_of(w[i], j);
-                const bf16x8 v[1] = {__builtin_bit_cast(bf16x8, u)};
+                const bf16x8 v[1] = {__builtin_bit_cast(bf16x8, u[j])};
                 mma(acc[cb * per + j], v, p[NG == 1 ? 0 : j * (D / 4) / kGroup4]);
             }
         }
@@ -335,7 +388,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
     l = swap_add32(swap_add16(l));
     const float mine_m = m == -INFINITY ? m : low;
     if (g == 0) sm[wave][n] = mine_m, sl[wave][n] = l;
-    __syncthreads();
+    __syncthreads();                                  // no wave reads its values any more
     float top = -INFINITY, z = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w][n]);
@@ -343,41 +396,120 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 || (D == 256 && BITS == 4) ? (
 #pragma unroll
     for (int w = 0; w < 4; ++w) z += sl[w][n] * __builtin_amdgcn_exp2f(sm[w][n] - base_m);
     const float own = __builtin_amdgcn_exp2f(mine_m - base_m);
-    float *sum = reinterpret_cast<float *>(vs);
-#pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
-        if (wave == w) {
+    float *sum = reinterpret_cast<float *>(vs);       // [wave][row][LD]
+    if (n < rows) {
+        float *to_row = sum + (wave * 16 + n) * LD;
 #pragma unroll
-            for (int tile = 0; tile < D / 16; ++tile)
+        for (int i = 0; i < D / 16; ++i) acc[i] *= own;
+        if constexpr (BITS == 8) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = BITS == 8 ? tile / 2 * 32 + 2 * (4 * g + i) + tile % 2
-                                            : tile % 4 * (D / 4) + tile / 4 * 16 + 4 * g + i;
-                    float *to_d = sum + n * LD + d;
-                    const float y = acc[tile][i] * own;
-                    *to_d = w == 0 ? y : *to_d + y;
-                }
+            for (int cb = 0; cb < D / 32; ++cb) {
+                const f32x4 x = acc[2 * cb], y = acc[2 * cb + 1];
+                *reinterpret_cast<f32x4 *>(to_row + 32 * cb + 8 * g) = f32x4{x[0], y[0], x[1], y[1]};
+                *reinterpret_cast<f32x4 *>(to_row + 32 * cb + 8 * g + 4) = f32x4{x[2], y[2], x[3], y[3]};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                *reinterpret_cast<f32x4 *>(to_row + i % 4 * (D / 4) + i / 4 * 16 + 4 * g) = acc[i];
         }
-        __syncthreads();
     }
     const size_t all = static_cast<size_t>(a.batch) * a.Hq, first = static_cast<size_t>(b) * a.Hq + hk * a.G + row0;
-    if (total <= a.chunk) {                           // the only part
-        if (wave == 0 && g == 0) {
+    const bool only = total <= a.chunk;               // the only part
+    __syncthreads();                                  // sm and sl are read, the sums are there
+    if (wave == 0 && g == 0 && n < rows) {
+        if (only) {
             sl[0][n] = z;
-            if (n < rows && a.lse) a.lse[first + n] = z == 0.0f ? -INFINITY : (base_m + log2f(z)) * kLn2;
+            if (a.lse) a.lse[first + n] = z == 0.0f ? -INFINITY : (base_m + log2f(z)) * kLn2;
+        } else {
+            a.ml[part * all + first + n] = make_float2(top, z);
         }
-        __syncthreads();
-        for (int e = threadIdx.x; e < rows * D; e += 256) {
-            const float y = sl[0][e / D];
-            static_cast<T *>(a.o)[first * D + e] = narrow<T>(y == 0.0f ? 0.0f : sum[e / D * LD + e % D] / y);
-        }
-        return;
     }
+    if (only) __syncthreads();
     for (int e = threadIdx.x; e < rows * (D / 4); e += 256) {
         const int r = e / (D / 4), c = e % (D / 4);
-        reinterpret_cast<f32x4 *>(a.acc + (part * all + first + r) * D)[c] = *reinterpret_cast<const f32x4 *>(sum + r * LD + 4 * c);
+        f32x4 y = *reinterpret_cast<const f32x4 *>(sum + r * LD + 4 * c);
+#pragma unroll
+        for (int w = 1; w < 4; ++w) y += *reinterpret_cast<const f32x4 *>(sum + (w * 16 + r) * LD + 4 * c);
+        if (only) {
+            const float d = sl[0][r];
+            T *o = static_cast<T *>(a.o) + (first + r) * D + 4 * c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = narrow<T>(d == 0.0f ? 0.0f : y[i] / d);
+        } else {
+            reinterpret_cast<f32x4 *>(a.acc + (part * all + first + r) * D)[c] = y;
+        }
     }
-    if (wave == 0 && g == 0 && n < rows) a.ml[part * all + first + n] = make_float2(top, z);
+}
+
+// The parts of each row joined, 64 dimensions by 16 lanes; SLOTS such lane groups
+// take a row's parts in turn, four at a time so that their loads overlap.  Rows of
+// one part or none are there already.
+template <typename T, int D, int SLOTS>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a)
+{
+    constexpr int U = 4, units = 16 / SLOTS;          // (row, 64 dimensions) of a workgroup
+    __shared__ float tops[4];
+    __shared__ alignas(16) f32x4 sums[4][16];
+    __shared__ float zs[4];
+    const int lane = threadIdx.x & 15, slot = (threadIdx.x >> 4) % SLOTS, wave = threadIdx.x >> 6;
+    const uint32_t unit = blockIdx.x * units + (threadIdx.x >> 4) / SLOTS;
+    const size_t row = unit / (D / 64), all = static_cast<size_t>(a.batch) * a.Hq;
+    const int d = unit % (D / 64) * 64 + lane * 4;
+    if (row >= all) return;                           // whole workgroups only where SLOTS = 16
+    int parts = a.parts;
+    if (!a.selected) {
+        const int len = min(a.lengths[row / a.Hq], a.max_pages * a.c.page);
+        if (len <= a.chunk) return;
+        parts = (len + a.chunk - 1) / a.chunk;
+    }
+    float top = -INFINITY;
+    for (int p = slot; p < parts; p += SLOTS) top = fmaxf(top, a.ml[p * all + row].x);
+    if constexpr (SLOTS >= 4) top = swap_max32(swap_max16(top));
+    if constexpr (SLOTS == 16) {
+        if ((threadIdx.x & 63) == 0) tops[wave] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    }
+    const float base = top == -INFINITY ? 0.0f : top;
+    f32x4 y = {};
+    float z = 0.0f;
+    for (int p0 = slot; p0 < parts; p0 += SLOTS * U) {
+        f32x4 x[U];
+        float2 ml[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const size_t at = static_cast<size_t>(min(p0 + u * SLOTS, parts - 1)) * all + row;
+            ml[u] = a.ml[at];
+            x[u] = *reinterpret_cast<const f32x4 *>(a.acc + at * D + d);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p0 + u * SLOTS < parts) {
+                const float f = __builtin_amdgcn_exp2f(ml[u].x - base);
+                z = fmaf(ml[u].y, f, z);
+                y += x[u] * f;
+            }
+    }
+    if constexpr (SLOTS >= 4) {
+        z = swap_add32(swap_add16(z));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = swap_add32(swap_add16(y[i]));
+    }
+    if constexpr (SLOTS == 16) {
+        if ((threadIdx.x & 63) < 16) sums[wave][lane] = y;
+        if ((threadIdx.x & 63) == 0) zs[wave] = z;
+        __syncthreads();
+        if (threadIdx.x >= 16) return;
+        y = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+        z = zs[0] + zs[1] + zs[2] + zs[3];
+    } else if (slot) {
+        return;
+    }
+    T *o = static_cast<T *>(a.o) + row * D + d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = narrow<T>(z == 0.0f ? 0.0f : y[i] / z);
+    if (d == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
 }
 
 stepq_status check(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
@@ -422,8 +554,10 @@ void launch(const CacheAttnArgs &a, int bits, hipStream_t st)
     const int64_t grid = static_cast<int64_t>(a.batch) * a.c.Hkv * ((a.G + 15) / 16) * a.parts;
     if (bits == 8) cache_attn_kernel<T, D, 8><<<dim3(static_cast<unsigned>(grid)), 256, 0, st>>>(a);
     else cache_attn_kernel<T, D, 4><<<dim3(static_cast<unsigned>(grid)), 256, 0, st>>>(a);
-    if (a.parts > 1) join_parts<T, D>({a.ml, a.acc, a.o, a.lse, static_cast<size_t>(a.batch) * a.Hq, a.parts, a.selected ? nullptr : a.lengths, a.Hq,
-                          a.max_pages * a.c.page, a.chunk}, st);
+    if (a.parts == 1) return;
+    const unsigned units = static_cast<unsigned>(a.batch) * a.Hq * (D / 64);
+    if (a.parts > 8) cache_join_kernel<T, D, 16><<<dim3(units), 256, 0, st>>>(a);
+    else cache_join_kernel<T, D, 4><<<dim3((units + 3) / 4), 256, 0, st>>>(a);
 }
 
 template <typename T>
@@ -469,6 +603,9 @@ extern "C" stepq_status stepq_cache_attention(const stepq_cache_desc *c, const s
     a.o = o, a.lse = lse;
     a.batch = d->batch, a.Hq = d->n_q_heads, a.G = d->n_q_heads / c->n_kv_heads;
     a.max_pages = d->max_pages, a.n_select = d->n_select, a.parts = cut.parts, a.chunk = cut.chunk;
+    const uint32_t blocks = static_cast<uint32_t>((a.G + 15) / 16);
+    a.div_items = fast_div(static_cast<uint32_t>(a.batch) * a.c.Hkv * blocks);
+    a.div_blocks = fast_div(blocks), a.div_hkv = fast_div(static_cast<uint32_t>(a.c.Hkv));
     a.acc = static_cast<float *>(workspace);
     if (need) a.ml = reinterpret_cast<float2 *>(a.acc + rows * c->head_dim * a.parts);
     a.scale = d->scale * 1.4426950408889634f;

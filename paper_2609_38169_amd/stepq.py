@@ -829,6 +829,8 @@ def stepq_cache_write(cache: Cache, k, v, page_table, starts, cu_seqlens=None, s
     slices of a wider token are taken as they are), page_table [n][M] int32,
     starts [n] int32 the position of each sequence's first token (< 0: none of
     it is written), cu_seqlens [n+1] int32 (None: one token each)."""
+    if isinstance(cache, Cache) and _done(_native.cache_rows(0, cache._plain, k, v, page_table, starts, cu_seqlens, stream)):
+        return
     _cache_rows(cache, lib().stepq_cache_write, k, v, page_table, starts, cu_seqlens, stream)
 
 

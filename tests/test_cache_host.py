@@ -152,7 +152,10 @@ def test_nothing_to_do():
 def test_sizes(page, D, bits):
     n, r = stepq.stepq_cache_bytes(1000, 3, page, D, bits)
     assert r == C.record_bytes(page, D, bits) and n == 3000 * r
-    assert stepq.stepq_cache_bytes(1 << 26, 8, page, D, bits)[0] == (1 << 29) * r       # past 32 bits
+    most = (2 ** 37 - 1) // r                               # past 32 bits, up to 2^37 bytes
+    assert stepq.stepq_cache_bytes(most, 1, page, D, bits)[0] == most * r
+    with pytest.raises(stepq.StepqError):
+        stepq.stepq_cache_bytes(most + 1, 1, page, D, bits)
 
 
 def test_values_that_no_field_holds():
