@@ -39,35 +39,49 @@ struct RowsArgs {
     const int32_t *table, *starts, *cu;  // cu NULL: token i is sequence i's only one
     const void *k, *v;                   // write: the tokens' rows; read: where they go
     int64_t sk, sv;                      // elements from one token to the next
-    int32_t n_tokens, n_seq, max_pages;
+    int32_t n_tokens, n_seq, max_pages, slices;      // workgroups that share a token's 2 Hkv rows
+    FastDiv div_slices;
 };
 
-// The sequence that token t belongs to, the last one that begins at or before it; -1: none.
-__device__ __forceinline__ int sequence_of(const RowsArgs &a, int t)
+// The sequence that token t belongs to, the last one that begins at or before it (-1: none), and where it begins.
+// A wave's lanes hold 64 of the bounds, spread over all of them; where that does not tell, the rest is looked up.
+__device__ __forceinline__ int sequence_of(const RowsArgs &a, int t, int *begin)
 {
+    *begin = t;
     if (!a.cu) return t;
-    int lo = 0, hi = a.n_seq + 1;        // the first entry beyond t lies in [lo, hi]
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (a.cu[mid] > t) hi = mid;
-        else lo = mid + 1;
+    const int lane = threadIdx.x & 63, apart = a.n_seq / 64 + 1, held = a.cu[min(lane * apart, a.n_seq)];
+    int at = 0, first = __shfl(held, 0);
+    if (first > t) at = -1;
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) {
+        const int next = __shfl(held, max(at, 0) + m);
+        if (at >= 0 && next <= t) at += m, first = next;
     }
-    return lo == 0 || lo > a.n_seq ? -1 : lo - 1;
+    if (at < 0) return -1;
+    int lo = min(at * apart, a.n_seq), hi = min(lo + apart, a.n_seq + 1);      // begins at or before t; does not, or was not asked
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1, y = a.cu[mid];
+        if (y <= t) lo = mid, first = y;
+        else hi = mid;
+    }
+    *begin = first;
+    return lo < a.n_seq ? lo : -1;
 }
 
-// Where token t's rows of head hk are: the record (NULL: nowhere) and the row.
-// held: whether t lies in a sequence at all.
-__device__ __forceinline__ uint8_t *place_of(const RowsArgs &a, int t, int hk, int *row, bool *held)
+// Where token t's rows are: the record of head 0 (NULL: nowhere) and the row.
+// held: whether t lies in a sequence at all.  All lanes of a wave take part.
+__device__ __forceinline__ uint8_t *place_of(const RowsArgs &a, int t, int *row, bool *held)
 {
-    const int s = sequence_of(a, t);
+    int begin;
+    const int s = sequence_of(a, t, &begin);
     *held = s >= 0;
     if (s < 0) return nullptr;
     const int start = a.starts[s];
-    const int64_t pos = static_cast<int64_t>(start) + (a.cu ? static_cast<int64_t>(t) - a.cu[s] : 0);
+    const int64_t pos = static_cast<int64_t>(start) + (static_cast<int64_t>(t) - begin);
     if (start < 0 || pos >= static_cast<int64_t>(a.max_pages) * a.c.page) return nullptr;
     const int p = page_of(static_cast<int>(pos), a.c.div_page);
     *row = static_cast<int>(pos) - p * a.c.page;
-    return record_of(a.c, a.table[static_cast<size_t>(s) * a.max_pages + p], hk);
+    return record_of(a.c, a.table[static_cast<size_t>(s) * a.max_pages + p], 0);
 }
 
 // A thread's 16 elements of a row in RUNS runs of neighbours: 8-bit codes one
@@ -83,6 +97,12 @@ struct __attribute__((packed, aligned(sizeof(T)))) Raw {     // N elements at an
     T x[N];
 };
 
+#ifndef WRITE_WGS
+#define WRITE_WGS 4096
+#endif
+#ifndef READ_WGS
+#define READ_WGS 2048
+#endif
 constexpr int kThreads = 256;
 
 // Quantizes rows: scale s, the smallest bfloat16 with top s >= the group's
@@ -94,129 +114,122 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(RowsArgs a)
 {
     using S = Share<D, BITS>;
     using Row = RowOf<D, BITS>;
-    constexpr int rows = kThreads / S::lanes;
+    constexpr int rows = kThreads / S::lanes, per = S::runs / Row::scales;    // runs of one group: all (8 bits, D = 64), 2 or 1
+    constexpr float q = BITS == 8 ? 127.0f : 7.0f;
     const int lane = threadIdx.x % S::lanes;
-    int x = blockIdx.x;
-    const bool value = x & 1;
-    x >>= 1;
-    const int hk = x % a.c.Hkv;
-    const int64_t t64 = static_cast<int64_t>(x / a.c.Hkv) * rows + threadIdx.x / S::lanes;
+    const int block = page_of(blockIdx.x, a.div_slices), slice = blockIdx.x - block * a.slices;
+    const int64_t t64 = static_cast<int64_t>(block) * rows + threadIdx.x / S::lanes;
     const int t = static_cast<int>(min(t64, static_cast<int64_t>(a.n_tokens - 1)));
     int row = 0;
     bool held;
-    uint8_t *rec = t64 < a.n_tokens ? place_of(a, t, hk, &row, &held) : nullptr;
-    const T *from = static_cast<const T *>(value ? a.v : a.k) + static_cast<size_t>(t) * (value ? a.sv : a.sk) +
-                    static_cast<size_t>(hk) * D;
-    float e[16];
-    uint32_t top[S::runs] = {};
+    uint8_t *const rec0 = place_of(a, t, &row, &held);
+    if (!rec0 || t64 >= a.n_tokens) return;           // a row's lanes together
+    for (int x = slice; x < 2 * a.c.Hkv; x += a.slices) {
+        const bool value = x & 1;
+        const int hk = x >> 1;
+        uint8_t *const rec = rec0 + hk * a.c.record;
+        const T *from = static_cast<const T *>(value ? a.v : a.k) + static_cast<size_t>(t) * (value ? a.sv : a.sk) +
+                        static_cast<size_t>(hk) * D;
+        float e[16];
+        uint32_t top[S::runs] = {};
 #pragma unroll
-    for (int j = 0; j < S::runs; ++j) {
-        const auto r = *reinterpret_cast<const Raw<T, S::run> *>(from + S::dim(lane, j));
+        for (int j = 0; j < S::runs; ++j) {
+            const auto r = *reinterpret_cast<const Raw<T, S::run> *>(from + S::dim(lane, j));
 #pragma unroll
-        for (int i = 0; i < S::run; ++i) {
-            const float y = widen(r.x[i]);
-            e[j * S::run + i] = y;
-            top[j] = max(top[j], __float_as_uint(y) & 0x7fffffffu);     // what is not finite is largest
+            for (int i = 0; i < S::run; ++i) {
+                const float y = widen(r.x[i]);
+                e[j * S::run + i] = y;
+                top[j] = max(top[j], __float_as_uint(y) & 0x7fffffffu);     // what is not finite is largest
+            }
         }
-    }
-    // runs of one group: all (8 bits, D = 64), two and two (128), each its own (256)
-    constexpr int per = S::runs / Row::scales;
-    uint32_t g[Row::scales];
-    bf16_t s16[Row::scales];
-    float s[Row::scales];
-    constexpr float q = BITS == 8 ? 127.0f : 7.0f;
+        bf16_t mine = 0;
+        float s[Row::scales];
 #pragma unroll
-    for (int n = 0; n < Row::scales; ++n) {
-        g[n] = top[n * per];
+        for (int n = 0; n < Row::scales; ++n) {
+            uint32_t g = top[n * per];
 #pragma unroll
-        for (int j = 1; j < per; ++j) g[n] = max(g[n], top[n * per + j]);
+            for (int j = 1; j < per; ++j) g = max(g, top[n * per + j]);
 #pragma unroll
-        for (int m = 1; m < S::lanes; m <<= 1) g[n] = max(g[n], static_cast<uint32_t>(__shfl_xor(static_cast<int>(g[n]), m)));
-        const float big = __uint_as_float(g[n]);
-        uint32_t u = (__float_as_uint(big / q) + 0xffffu) & 0xffff0000u;
-        if (__uint_as_float(u) * q < big) u += 0x10000u;
-        if (big < 0x1p-100f) u = 0;
-        if (g[n] >= 0x7f800000u) u = 0x7fc00000u;
-        s16[n] = static_cast<bf16_t>(u >> 16);
-        s[n] = __uint_as_float(u);
-    }
-    uint32_t word[BITS == 8 ? 4 : 2] = {};
-#pragma unroll
-    for (int j = 0; j < S::runs; ++j)
-#pragma unroll
-        for (int i = 0; i < S::run; ++i) {
-            const float sc = s[j / per];
-            const int c = sc > 0.0f ? static_cast<int>(rintf(e[j * S::run + i] / sc)) : 0;
-            if constexpr (BITS == 8) word[i / 4] |= (static_cast<uint32_t>(c) & 0xffu) << (8 * (i % 4));
-            else word[i / 2] |= (static_cast<uint32_t>(c) & 0xfu) << (16 * (i % 2) + 4 * j);
+            for (int m = 1; m < S::lanes; m <<= 1) g = max(g, static_cast<uint32_t>(__shfl_xor(static_cast<int>(g), m)));
+            const float big = __uint_as_float(g);
+            uint32_t u = (__float_as_uint(big / q) + 0xffffu) & 0xffff0000u;
+            if (__uint_as_float(u) * q < big) u += 0x10000u;
+            if (big < 0x1p-100f) u = 0;
+            if (g >= 0x7f800000u) u = 0x7fc00000u;
+            if (lane == n) mine = static_cast<bf16_t>(u >> 16);
+            s[n] = __uint_as_float(u);
         }
-    if (!rec) return;
-    uint8_t *to = rec + Row::codes(a.c.page, value, row) + lane * (BITS * 2);
-    if constexpr (BITS == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(word[0], word[1], word[2], word[3]);
-    else *reinterpret_cast<uint2 *>(to) = make_uint2(word[0], word[1]);
-    if (lane < Row::scales) {
-        bf16_t mine = s16[0];
+        uint32_t word[BITS == 8 ? 4 : 2] = {};
 #pragma unroll
-        for (int n = 1; n < Row::scales; ++n) mine = lane == n ? s16[n] : mine;
-        reinterpret_cast<bf16_t *>(rec + Row::scale(a.c.page, value, row))[lane] = mine;
+        for (int j = 0; j < S::runs; ++j)
+#pragma unroll
+            for (int i = 0; i < S::run; ++i) {
+                const float sc = s[j / per];
+                const int c = sc > 0.0f ? static_cast<int>(rintf(e[j * S::run + i] / sc)) : 0;
+                if constexpr (BITS == 8) word[i / 4] |= (static_cast<uint32_t>(c) & 0xffu) << (8 * (i % 4));
+                else word[i / 2] |= (static_cast<uint32_t>(c) & 0xfu) << (16 * (i % 2) + 4 * j);
+            }
+        uint8_t *to = rec + Row::codes(a.c.page, value, row) + lane * (BITS * 2);
+        if constexpr (BITS == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(word[0], word[1], word[2], word[3]);
+        else *reinterpret_cast<uint2 *>(to) = make_uint2(word[0], word[1]);
+        if (lane < Row::scales) reinterpret_cast<bf16_t *>(rec + Row::scale(a.c.page, value, row))[lane] = mine;
     }
 }
 
-// A thread's 16 values of a row.
-template <int D, int BITS>
-__device__ __forceinline__ void values_of(const uint8_t *rec, int page, bool value, int row, int lane, float (&e)[16])
-{
-    using S = Share<D, BITS>;
-    using Row = RowOf<D, BITS>;
-    constexpr int per = S::runs / Row::scales;
-    const uint8_t *from = rec + Row::codes(page, value, row) + lane * (BITS * 2);
-    const bf16_t *sc = reinterpret_cast<const bf16_t *>(rec + Row::scale(page, value, row));
-    float s[Row::scales];
-#pragma unroll
-    for (int n = 0; n < Row::scales; ++n) s[n] = widen(sc[n]);
-    if constexpr (BITS == 8) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(from);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] = s[0] * static_cast<float>(static_cast<int8_t>(u[i / 4] >> (8 * (i % 4))));
-    } else {
-        const uint2 w = *reinterpret_cast<const uint2 *>(from);
-        const uint32_t u[2] = {w.x, w.y};
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                e[4 * j + i] = s[j / per] * static_cast<float>(static_cast<int32_t>(u[i / 2] << (28 - 16 * (i % 2) - 4 * j)) >> 28);
-    }
-}
-
+// Read back: a thread takes 8 neighbouring dimensions, so that a row's values are written in one piece: 8 bytes of
+// codes, or one nibble of 8 words.
 template <typename T, int D, int BITS>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(RowsArgs a)
 {
-    using S = Share<D, BITS>;
-    constexpr int rows = kThreads / S::lanes;
-    const int lane = threadIdx.x % S::lanes;
-    int x = blockIdx.x;
-    const bool value = x & 1;
-    x >>= 1;
-    const int hk = x % a.c.Hkv;
-    const int64_t t64 = static_cast<int64_t>(x / a.c.Hkv) * rows + threadIdx.x / S::lanes;
-    if (t64 >= a.n_tokens) return;
-    const int t = static_cast<int>(t64);
+    using Row = RowOf<D, BITS>;
+    constexpr int lanes = D / 8, rows = kThreads / lanes, U = 4;
+    const int lane = threadIdx.x % lanes, d0 = lane * 8;
+    const int block = page_of(blockIdx.x, a.div_slices), slice = blockIdx.x - block * a.slices;
+    const int64_t t64 = static_cast<int64_t>(block) * rows + threadIdx.x / lanes;
+    const int t = static_cast<int>(min(t64, static_cast<int64_t>(a.n_tokens - 1)));
     int row = 0;
     bool held;
-    const uint8_t *rec = place_of(a, t, hk, &row, &held);
-    if (!held) return;
-    float e[16] = {};
-    if (rec) values_of<D, BITS>(rec, a.c.page, value, row, lane, e);
-    T *to = static_cast<T *>(const_cast<void *>(value ? a.v : a.k)) + static_cast<size_t>(t) * (value ? a.sv : a.sk) +
-            static_cast<size_t>(hk) * D;
+    const uint8_t *rec0 = place_of(a, t, &row, &held);
+    if (!held || t64 >= a.n_tokens) return;
+    const int nibble = d0 / (D / 4);
+    for (int x0 = slice; x0 < 2 * a.c.Hkv; x0 += U * a.slices) {
+        uint32_t w[U][BITS == 8 ? 2 : 4];
+        float s[U];
 #pragma unroll
-    for (int j = 0; j < S::runs; ++j) {
-        Raw<T, S::run> r;
+        for (int u = 0; u < U; ++u) {
+            const int x = min(x0 + u * a.slices, 2 * a.c.Hkv - 1);
+            const bool value = x & 1;
+            s[u] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < S::run; ++i) r.x[i] = narrow<T>(e[j * S::run + i]);
-        *reinterpret_cast<Raw<T, S::run> *>(to + S::dim(lane, j)) = r;
+            for (uint32_t &y : w[u]) y = 0;
+            if (rec0) {
+                const uint8_t *rec = rec0 + (x >> 1) * a.c.record, *codes = rec + Row::codes(a.c.page, value, row);
+                s[u] = widen(reinterpret_cast<const bf16_t *>(rec + Row::scale(a.c.page, value, row))[BITS == 8 ? 0 : d0 / kGroup4]);
+                if constexpr (BITS == 8) {
+                    const uint2 y = reinterpret_cast<const uint2 *>(codes)[lane];
+                    w[u][0] = y.x, w[u][1] = y.y;
+                } else {
+                    const uint4 y = *reinterpret_cast<const uint4 *>(codes + d0 % (D / 4) * 2);
+                    w[u][0] = y.x, w[u][1] = y.y, w[u][2] = y.z, w[u][3] = y.w;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int x = x0 + u * a.slices;
+            if (x >= 2 * a.c.Hkv) break;
+            const bool value = x & 1;
+            Raw<T, 8> r;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = BITS == 8 ? static_cast<int8_t>(w[u][i / 4] >> (8 * (i % 4)))
+                                        : static_cast<int32_t>(w[u][i / 2] << (28 - 16 * (i % 2) - 4 * nibble)) >> 28;
+                r.x[i] = narrow<T>(s[u] * static_cast<float>(c));
+            }
+            T *to = static_cast<T *>(const_cast<void *>(value ? a.v : a.k)) + static_cast<size_t>(t) * (value ? a.sv : a.sk) +
+                    static_cast<size_t>(x >> 1) * D + d0;
+            *reinterpret_cast<Raw<T, 8> *>(to) = r;
+        }
     }
 }
 
@@ -331,9 +344,9 @@ stepq_status check_tokens(const stepq_cache_desc *d, const stepq_cache_tokens *t
         if (s < 0 || (s && s < heads)) return bad("tokens must not overlap");
         if (s > (int64_t(1) << 26)) return set_error(STEPQ_E_UNSUPPORTED, "a token stride past 2^26 elements");
     }
-    // a launch has less than 2^32 threads, 16 elements each
-    if (t->n_tokens >= (int64_t(1) << 31) || static_cast<double>(t->n_tokens) * heads >= 0x1p34)
-        return set_error(STEPQ_E_UNSUPPORTED, "2^31 tokens or 2^34 elements or more in one call: split it");
+    // a launch has less than 2^32 threads, 8 elements each of keys and values
+    if (t->n_tokens >= (int64_t(1) << 31) || static_cast<double>(t->n_tokens) * heads >= 0x1p33)
+        return set_error(STEPQ_E_UNSUPPORTED, "2^31 tokens or 2^33 elements or more in one call: split it");
     if (const stepq_status st = check_paged(d, cache, t->n_seq, t->max_pages, table)) return st;
     if (t->n_tokens && t->n_seq && (!starts || !k || !v)) return bad("NULL starts or token rows");
     const int el = t->act_dtype == STEPQ_F32 ? 4 : 2;
@@ -346,14 +359,18 @@ RowsArgs rows_args(const stepq_cache_desc *d, const stepq_cache_tokens *t, const
 {
     const int64_t heads = static_cast<int64_t>(d->n_kv_heads) * d->head_dim;
     return {cache_view(d, cache), table, starts, cu, k, v, t->k_stride ? t->k_stride : heads, t->v_stride ? t->v_stride : heads,
-            static_cast<int32_t>(t->n_tokens), t->n_seq, t->max_pages};
+            static_cast<int32_t>(t->n_tokens), t->n_seq, t->max_pages, 1, {}};
 }
 
-template <int D>
-unsigned rows_grid(const RowsArgs &a)
+// EACH elements a thread; a token's rows go to as many workgroups as fill the chip, 8 on a CU.
+template <int D, int EACH>
+unsigned rows_grid(RowsArgs &a, int64_t workgroups)
 {
-    constexpr int rows = kThreads / (D / 16);
-    return static_cast<unsigned>((static_cast<int64_t>(a.n_tokens) + rows - 1) / rows * a.c.Hkv * 2);
+    constexpr int rows = kThreads / (D / EACH);
+    const int64_t blocks = (static_cast<int64_t>(a.n_tokens) + rows - 1) / rows;
+    a.slices = static_cast<int32_t>(std::clamp<int64_t>(workgroups / blocks, 1, 2 * a.c.Hkv));
+    a.div_slices = fast_div(static_cast<uint32_t>(a.slices));
+    return static_cast<unsigned>(blocks * a.slices);
 }
 
 }  // namespace
@@ -377,11 +394,12 @@ extern "C" stepq_status stepq_cache_write(const stepq_cache_desc *d, const stepq
 {
     if (const stepq_status st = check_tokens(d, t, cache, page_table, starts, cu_seqlens, k, v)) return st;
     if (t->n_tokens == 0 || t->n_seq == 0) return STEPQ_OK;
-    const RowsArgs a = rows_args(d, t, cache, page_table, starts, cu_seqlens, k, v);
+    RowsArgs a = rows_args(d, t, cache, page_table, starts, cu_seqlens, k, v);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_shape(d, [&](auto D, auto B) {
-        if (t->act_dtype == STEPQ_BF16) cache_write_kernel<bf16_t, D, B><<<dim3(rows_grid<D>(a)), kThreads, 0, s>>>(a);
-        else cache_write_kernel<float, D, B><<<dim3(rows_grid<D>(a)), kThreads, 0, s>>>(a);
+        const dim3 grid(rows_grid<D, 16>(a, WRITE_WGS));
+        if (t->act_dtype == STEPQ_BF16) cache_write_kernel<bf16_t, D, B><<<grid, kThreads, 0, s>>>(a);
+        else cache_write_kernel<float, D, B><<<grid, kThreads, 0, s>>>(a);
     });
     return launched("cache write launch");
 }
@@ -392,11 +410,12 @@ extern "C" stepq_status stepq_cache_read(const stepq_cache_desc *d, const stepq_
 {
     if (const stepq_status st = check_tokens(d, t, cache, page_table, starts, cu_seqlens, k, v)) return st;
     if (t->n_tokens == 0 || t->n_seq == 0) return STEPQ_OK;
-    const RowsArgs a = rows_args(d, t, cache, page_table, starts, cu_seqlens, k, v);
+    RowsArgs a = rows_args(d, t, cache, page_table, starts, cu_seqlens, k, v);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_shape(d, [&](auto D, auto B) {
-        if (t->act_dtype == STEPQ_BF16) cache_read_kernel<bf16_t, D, B><<<dim3(rows_grid<D>(a)), kThreads, 0, s>>>(a);
-        else cache_read_kernel<float, D, B><<<dim3(rows_grid<D>(a)), kThreads, 0, s>>>(a);
+        const dim3 grid(rows_grid<D, 8>(a, READ_WGS));
+        if (t->act_dtype == STEPQ_BF16) cache_read_kernel<bf16_t, D, B><<<grid, kThreads, 0, s>>>(a);
+        else cache_read_kernel<float, D, B><<<grid, kThreads, 0, s>>>(a);
     });
     return launched("cache read launch");
 }

@@ -21,13 +21,10 @@ struct CacheAttnArgs {
     float scale;             // times log2 e: scores are kept in powers of two
 };
 
-#ifndef CUT_WGS
-#define CUT_WGS 4096
+#ifndef MAXC
+#define MAXC 1024
 #endif
-#ifndef CUT_MIN
-#define CUT_MIN 256
-#endif
-constexpr int kMaxChunk = 1024;
+constexpr int kMaxChunk = MAXC;
 constexpr int kTile = 32;    // keys of a wave's turn
 // Waves of a SIMD that the registers are for.
 template <typename T, int D>
@@ -442,7 +439,7 @@ void cache_attn_kernel(CacheAttnArgs a)
     }
 }
 
-// The parts of each row joined, 64 dimensions by 16 lanes; SLOTS such lane groups
+// The parts of each row joined, 64 dimensions by 16 lanes; SLOTS (4 or 16) such lane groups
 // take a row's parts in turn, four at a time so that their loads overlap.  Rows of
 // one part or none are there already.
 template <typename T, int D, int SLOTS>
@@ -463,9 +460,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a)
         if (len <= a.chunk) return;
         parts = (len + a.chunk - 1) / a.chunk;
     }
+    constexpr int of = SLOTS == 16 ? 256 : 64;        // threads that look for the largest maximum
     float top = -INFINITY;
-    for (int p = slot; p < parts; p += SLOTS) top = fmaxf(top, a.ml[p * all + row].x);
-    if constexpr (SLOTS >= 4) top = swap_max32(swap_max16(top));
+    for (int p = threadIdx.x % of; p < parts; p += of) top = fmaxf(top, a.ml[p * all + row].x);
+#pragma unroll
+    for (int i = 1; i < 16; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+    top = swap_max32(swap_max16(top));
     if constexpr (SLOTS == 16) {
         if ((threadIdx.x & 63) == 0) tops[wave] = top;
         __syncthreads();
@@ -491,11 +491,9 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a)
                 y += x[u] * f;
             }
     }
-    if constexpr (SLOTS >= 4) {
-        z = swap_add32(swap_add16(z));
+    z = swap_add32(swap_add16(z));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = swap_add32(swap_add16(y[i]));
-    }
+    for (int i = 0; i < 4; ++i) y[i] = swap_add32(swap_add16(y[i]));
     if constexpr (SLOTS == 16) {
         if ((threadIdx.x & 63) < 16) sums[wave][lane] = y;
         if ((threadIdx.x & 63) == 0) zs[wave] = z;
@@ -536,9 +534,12 @@ Cut cut_of(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
 {
     const int64_t tokens = static_cast<int64_t>(d->n_select ? d->n_select : d->max_pages) * c->page_size;
     if (d->batch == 0 || tokens == 0) return {kMaxChunk, 1};
+    // A second launch, which joins, takes about 3 us: as long as a workgroup takes for 768 tokens (512 in fp32).
+    const bool bf = d->act_dtype == STEPQ_BF16;
     const int64_t G = d->n_q_heads / c->n_kv_heads, blocks = static_cast<int64_t>(d->batch) * c->n_kv_heads * ((G + 15) / 16);
-    const int64_t want = std::clamp<int64_t>((blocks * tokens + CUT_WGS - 1) / CUT_WGS, CUT_MIN, kMaxChunk);
-    const int64_t chunk = (want + 127) / 128 * 128;
+    const int64_t slots = 256 * (c->head_dim == 256 ? 1 : bf ? 3 : 2);       // workgroups that the chip runs at once
+    const int64_t want = std::clamp<int64_t>((blocks * tokens + slots - 1) / slots, 256, kMaxChunk);
+    const int64_t chunk = tokens <= (bf ? 768 : 512) ? 768 : (want + 127) / 128 * 128;
     return {static_cast<int32_t>(chunk), static_cast<int32_t>((tokens + chunk - 1) / chunk)};
 }
 

@@ -3,6 +3,12 @@
 
 #include "stepq_cache.h"
 
+#ifndef SCORE_WGS
+#define SCORE_WGS 2048
+#endif
+#ifndef SCORE_U
+#define SCORE_U 4
+#endif
 namespace stepq {
 namespace {
 
@@ -37,33 +43,15 @@ __device__ __forceinline__ uint32_t key_of(float x)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
 {
-    constexpr int lanes = D / 4, at_once = 256 / lanes, U = 4;
+    constexpr int lanes = D / 4, at_once = 256 / lanes, U = SCORE_U;
     const int lane = threadIdx.x % lanes, sub = threadIdx.x / lanes;
     int x = blockIdx.x;
     const int turn = x % a.turns;
     x /= a.turns;
     const int hk = x % a.Hkv, b = x / a.Hkv;
-    const int pages = pages_of(a, b), end = pages - a.n_last;
-    if (pages <= a.n_select || a.n_first + turn * at_once * U >= end) return;
-    const bool high = lane >= lanes / 2;
-    const int d0 = lane % (lanes / 2) * 8;
-    double w[8] = {};
-    const T *q = static_cast<const T *>(a.q) + (static_cast<size_t>(b) * a.Hkv + hk) * a.G * D + d0;
-    struct alignas(16) Eight {
-        T x[8];
-    };
-    for (int h = 0; h < a.G; ++h) {
-        const Eight e = *reinterpret_cast<const Eight *>(q + static_cast<size_t>(h) * D);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y = widen(e.x[i]);
-            // a NaN reaches both sums
-            w[i] += static_cast<double>(high ? (y < 0.0f ? 0.0f : y) : (y > 0.0f ? 0.0f : y));
-        }
-    }
+    // page ids and queries are asked for before the length is there
     const int32_t *table = a.table + static_cast<size_t>(b) * a.max_pages;
-    uint32_t *keys = a.keys + (static_cast<size_t>(b) * a.Hkv + hk) * a.max_pages;
-    const auto ids = [&](int p0, int (&id)[U]) {
+    const auto ids = [&](int p0, int (&id)[U], int end) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int p = p0 + u * at_once + sub;
@@ -71,18 +59,38 @@ __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
         }
     };
     int next[U];
-    ids(a.n_first + turn * at_once * U, next);
+    ids(a.n_first + turn * at_once * U, next, a.max_pages);
+    const bool high = lane >= lanes / 2;
+    const int d0 = lane % (lanes / 2) * 8;
+    double w[8] = {};
+    const T *q = static_cast<const T *>(a.q) + (static_cast<size_t>(b) * a.Hkv + hk) * a.G * D + d0;
+    struct alignas(16) Eight {
+        T x[8];
+    };
+    Eight e = *reinterpret_cast<const Eight *>(q);
+    const int pages = pages_of(a, b), end = pages - a.n_last;
+    if (pages <= a.n_select || a.n_first + turn * at_once * U >= end) return;
+    for (int h = 0; h < a.G; ++h) {
+        if (h) e = *reinterpret_cast<const Eight *>(q + static_cast<size_t>(h) * D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = widen(e.x[i]);
+            // a NaN reaches both sums
+            w[i] += static_cast<double>(high ? (y < 0.0f ? 0.0f : y) : (y > 0.0f ? 0.0f : y));
+        }
+    }
+    uint32_t *keys = a.keys + (static_cast<size_t>(b) * a.Hkv + hk) * a.max_pages;
     for (int p0 = a.n_first + turn * at_once * U; p0 < end; p0 += a.turns * at_once * U) {
         uint4 v[U];
         bool there[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            there[u] = next[u] >= 0 && next[u] < a.n_pages;
+            there[u] = next[u] >= 0 && next[u] < a.n_pages && p0 + u * at_once + sub < end;
             v[u] = make_uint4(0, 0, 0, 0);
             if (there[u])
                 v[u] = *reinterpret_cast<const uint4 *>(a.bounds + ((static_cast<size_t>(next[u]) * a.Hkv + hk) * 2 + high) * D + d0);
         }
-        ids(p0 + a.turns * at_once * U, next);
+        if (p0 + a.turns * at_once * U < end) ids(p0 + a.turns * at_once * U, next, end);
         double sum[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -214,21 +222,40 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(SelectArgs a)
             if (lane == 0) mores[i][wave] = __popcll(bm[i]), sames[i][wave] = __popcll(bs[i]);
         }
         __syncthreads();
+        if (wave == 0) {                              // how many before each (i, wave), and of all
+            constexpr int N = EACH * W / 64 ? EACH * W / 64 : 1;
+            uint32_t m[N], s[N], ms = 0, ss = 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int e = lane * N + j;
+                m[j] = e < EACH * W ? (&mores[0][0])[e] : 0, s[j] = e < EACH * W ? (&sames[0][0])[e] : 0;
+                ms += m[j], ss += s[j];
+            }
+            uint32_t mx = ms, sx = ss;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t y = __shfl_up(static_cast<int>(mx), d), z = __shfl_up(static_cast<int>(sx), d);
+                if (lane >= d) mx += y, sx += z;
+            }
+            if (lane == 63) waves[0] = mx, waves[1] = sx;
+            mx -= ms, sx -= ss;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int e = lane * N + j;
+                if (e < EACH * W) (&mores[0][0])[e] = mx, (&sames[0][0])[e] = sx;
+                mx += m[j], sx += s[j];
+            }
+        }
+        __syncthreads();
         const uint64_t below = (1ull << lane) - 1;
-        uint32_t m = more0, s = same0;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            uint32_t mw = m, sw = s;
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                if (w < wave) mw += mores[i][w], sw += sames[i][w];
-                m += mores[i][w], s += sames[i][w];
-            }
-            const uint32_t before = mw + __popcll(bm[i] & below), equal = sw + __popcll(bs[i] & below);
+            const uint32_t before = more0 + mores[i][wave] + __popcll(bm[i] & below);
+            const uint32_t equal = same0 + sames[i][wave] + __popcll(bs[i] & below);
             if ((bm[i] >> lane & 1) || ((bs[i] >> lane & 1) && equal < want))
                 out[a.n_first + before + min(equal, want)] = p0 + i * THREADS + tid;
         }
-        more0 = m, same0 = s;
+        more0 += waves[0], same0 += waves[1];
         __syncthreads();
     }
 }
@@ -296,8 +323,8 @@ extern "C" stepq_status stepq_cache_select(const stepq_cache_desc *c, const step
                  d->n_first, d->n_last, 1, fast_div(static_cast<uint32_t>(c->page_size))};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (need) {
-        const int64_t at_once = 4 * 1024 / c->head_dim;      // pages of a workgroup's turn
-        a.turns = static_cast<int32_t>(std::clamp<int64_t>(2048 / pairs, 1, (d->max_pages + at_once - 1) / at_once));
+        const int64_t at_once = SCORE_U * 1024 / c->head_dim;      // pages of a workgroup's turn
+        a.turns = static_cast<int32_t>(std::clamp<int64_t>(SCORE_WGS / pairs, 1, (d->max_pages + at_once - 1) / at_once));
         if (d->act_dtype == STEPQ_BF16) score<bf16_t>(a, c->head_dim, s);
         else score<float>(a, c->head_dim, s);
     }
