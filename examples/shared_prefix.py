@@ -10,8 +10,13 @@ decay per head, fp32 states) and "attention" (softmax over paged caches).
 - The delta layers' states are fitted and packed into pools.
 - Decoding: Pool.step, stepq_state_step and stepq_prefix_attention, one token of
   every request at a time.
+With cache_bits 8 or 4 the attention layers' caches are quantized as they are
+written (stepq.Cache): a request's pages are the prefix's whole ones, which all
+share, and its own, which begin with what is left of the prefix.  With `select`
+a decoded token reads that many of a request's pages, chosen by their bounds.
 
     python examples/shared_prefix.py --requests 64 --prefix 4096
+    python examples/shared_prefix.py --requests 64 --prefix 4096 --cache-bits 8 --select 16
 """
 import argparse
 import os
@@ -74,20 +79,31 @@ class Stack:
 class Server:
     """States and caches of up to `capacity` requests over one prefix [P][width]."""
 
-    def __init__(self, stack: Stack, prefix, capacity: int, own_tokens: int, page: int = 64, quantized: bool = True):
+    def __init__(self, stack: Stack, prefix, capacity: int, own_tokens: int, page: int = 64, quantized: bool = True,
+                 cache_bits: int = 16, select: int = 0):
         s = self.stack = stack
         self.page, self.P, self.capacity, self.quantized = page, prefix.shape[0], capacity, quantized
-        self.own_pages = -(-own_tokens // page)
+        self.cache_bits, self.select = cache_bits, select
+        self.left = self.P % page if cache_bits < 16 else 0         # of the prefix, in the requests' own pages
+        self.own_pages = -(-(self.left + own_tokens) // page)
         n_prefix = -(-self.P // page)
         i32 = dict(dtype=torch.int32, device=s.device)
         self.prefix_pages = torch.arange(n_prefix, **i32)
         self.table = n_prefix + torch.arange(capacity * self.own_pages, **i32).view(capacity, -1)
         self.ids = torch.arange(capacity, **i32)
         self.lengths = torch.zeros(capacity, **i32)
-        self.pools, self.states, self.start, self.caches = {}, {}, {}, {}
+        if cache_bits < 16:                         # all of a request's pages
+            shared = self.prefix_pages[:self.P // page].expand(capacity, -1)
+            self.table = torch.cat([shared, self.table], 1).contiguous()
+            self.selected = torch.empty((capacity, s.kv_heads, max(select, 1)), **i32)
+        self.pools, self.states, self.start, self.caches, self.bounds, self.tail = {}, {}, {}, {}, {}, {}
         for i, kind in enumerate(s.kinds):
             if kind == "attention":
                 n = n_prefix + capacity * self.own_pages
+                if cache_bits < 16:
+                    self.caches[i] = stepq.Cache(n, s.kv_heads, page, s.head_dim, cache_bits)
+                    self.bounds[i] = torch.zeros((n, s.kv_heads, 2, s.head_dim), dtype=torch.bfloat16, device=s.device)
+                    continue
                 self.caches[i] = [torch.zeros((n, s.kv_heads, page, s.head_dim), dtype=s.dtype, device=s.device) for _ in "kv"]
             else:
                 self.states[i] = torch.zeros((capacity, s.v_heads, s.d, s.d), device=s.device)
@@ -102,6 +118,18 @@ class Server:
         for cache, x in zip(self.caches[i], (k, v)):
             cache[pages, :, (at % self.page).long()] = x
 
+    def _cached(self, i, q, k, v, table, starts, cu, row_table, row_lengths, select=False):
+        """Sequences' tokens into the quantized cache, then attention of one row for each of them."""
+        cache, last = self.caches[i], starts + (1 if cu is None else cu[1:] - cu[:-1])
+        cache.write(k, v, table, starts, cu)
+        if self.select:
+            cache.bounds(table, starts, last, self.bounds[i])
+        q, o = q.contiguous(), torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if select:
+            cache.select(q, self.bounds[i], table, last, self.selected)
+        cache.attend(q, row_table, row_lengths, o, selected=self.selected if select else None)
+        return o
+
     def _attend(self, i, q, prefix_len, table, lengths):
         o = torch.empty_like(q)
         stepq.stepq_prefix_attention(q.contiguous(), *self.caches[i], self.prefix_pages, prefix_len, table, lengths, o)
@@ -113,7 +141,10 @@ class Server:
         table = self.prefix_pages.expand(P, -1).contiguous()       # every token reads the pages up to itself
         for i, kind in enumerate(s.kinds):
             q, k, v, alpha, beta = s.project(i, x)
-            if kind == "attention":
+            if kind == "attention" and self.cache_bits < 16:
+                o = self._cached(i, q, k, v, table[:1], at[:1], torch.tensor([0, P], dtype=torch.int32, device=s.device), table, at + 1)
+                self.tail[i] = k[P - self.left:], v[P - self.left:]
+            elif kind == "attention":
                 self._write(i, table, at, k, v)
                 o = self._attend(i, q, 0, table, at + 1)
             else:
@@ -127,7 +158,7 @@ class Server:
         """The requests' own prompts [T_b][width], one per request of the capacity; returns each one's last output."""
         s, B = self.stack, self.capacity
         n = [p.shape[0] for p in prompts]
-        if len(n) != B or min(n) < 1 or max(n) > self.own_pages * self.page:
+        if len(n) != B or min(n) < 1 or max(n) > self.own_pages * self.page - self.left:
             raise ValueError("a prompt of 1 token or more, within its pages, for each request")
         cu = torch.tensor([0] + n, dtype=torch.int32).cumsum(0, dtype=torch.int32).to(s.device)
         self.lengths.copy_(torch.tensor(n, dtype=torch.int32))
@@ -137,7 +168,16 @@ class Server:
         x = torch.cat(list(prompts))
         for i, kind in enumerate(s.kinds):
             q, k, v, alpha, beta = s.project(i, x)
-            if kind == "attention":
+            if kind == "attention" and self.cache_bits < 16:
+                if self.left:                       # the prefix's last tokens, once for each request
+                    n_left = self.left * torch.arange(B + 1, dtype=torch.int32, device=s.device)
+                    self.caches[i].write(*(z.repeat(B, 1, 1) for z in self.tail[i]), self.table,
+                                         torch.full_like(self.lengths, self.P - self.left), n_left)
+                    if self.select:
+                        self.caches[i].bounds(self.table, torch.full_like(self.lengths, self.P - self.left),
+                                              torch.full_like(self.lengths, self.P), self.bounds[i])
+                o = self._cached(i, q, k, v, self.table, torch.full_like(self.lengths, self.P), cu, table, self.P + at + 1)
+            elif kind == "attention":
                 self._write(i, table, at, k, v)
                 o = self._attend(i, q, self.P, table, at + 1)
             else:
@@ -158,7 +198,9 @@ class Server:
         self.lengths += 1
         for i, kind in enumerate(s.kinds):
             q, k, v, alpha, beta = s.project(i, x)
-            if kind == "attention":
+            if kind == "attention" and self.cache_bits < 16:
+                o = self._cached(i, q, k, v, self.table, self.P + at, None, self.table, self.P + self.lengths, bool(self.select))
+            elif kind == "attention":
                 self._write(i, self.table, at, k, v)
                 o = self._attend(i, q, self.P, self.table, self.lengths)
             else:
@@ -182,6 +224,8 @@ def main():
     p.add_argument("--prefix", type=int, default=4096)
     p.add_argument("--prompt", type=int, default=200, help="longest prompt of a request's own")
     p.add_argument("--steps", type=int, default=32)
+    p.add_argument("--cache-bits", type=int, default=16, choices=(16, 8, 4))
+    p.add_argument("--select", type=int, default=0, help="pages that a decoded token reads (quantized caches; 0: all)")
     a = p.parse_args()
     stack = Stack()
     g = torch.Generator().manual_seed(1)
@@ -197,7 +241,8 @@ def main():
         return y
 
     for _ in range(2):                          # the second time without first-use costs
-        server = timed(f"prefix of {a.prefix} tokens", lambda: Server(stack, prefix, a.requests, a.prompt + 2 * a.steps))
+        server = timed(f"prefix of {a.prefix} tokens", lambda: Server(stack, prefix, a.requests, a.prompt + 2 * a.steps,
+                                                                              cache_bits=a.cache_bits, select=a.select))
         x = timed(f"{sum(map(len, prompts))} tokens of {a.requests} prompts, states packed", lambda: server.admit(prompts))
 
     def decode(n):

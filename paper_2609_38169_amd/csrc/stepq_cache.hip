@@ -97,12 +97,6 @@ struct __attribute__((packed, aligned(sizeof(T)))) Raw {     // N elements at an
     T x[N];
 };
 
-#ifndef WRITE_WGS
-#define WRITE_WGS 4096
-#endif
-#ifndef READ_WGS
-#define READ_WGS 2048
-#endif
 constexpr int kThreads = 256;
 
 // Quantizes rows: scale s, the smallest bfloat16 with top s >= the group's
@@ -197,12 +191,12 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(RowsArgs a)
         float s[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int x = min(x0 + u * a.slices, 2 * a.c.Hkv - 1);
+            const int x = x0 + u * a.slices;
             const bool value = x & 1;
             s[u] = 0.0f;
 #pragma unroll
             for (uint32_t &y : w[u]) y = 0;
-            if (rec0) {
+            if (rec0 && x < 2 * a.c.Hkv) {
                 const uint8_t *rec = rec0 + (x >> 1) * a.c.record, *codes = rec + Row::codes(a.c.page, value, row);
                 s[u] = widen(reinterpret_cast<const bf16_t *>(rec + Row::scale(a.c.page, value, row))[BITS == 8 ? 0 : d0 / kGroup4]);
                 if constexpr (BITS == 8) {
@@ -368,7 +362,8 @@ unsigned rows_grid(RowsArgs &a, int64_t workgroups)
 {
     constexpr int rows = kThreads / (D / EACH);
     const int64_t blocks = (static_cast<int64_t>(a.n_tokens) + rows - 1) / rows;
-    a.slices = static_cast<int32_t>(std::clamp<int64_t>(workgroups / blocks, 1, 2 * a.c.Hkv));
+    const int64_t all = 2 * int64_t(a.c.Hkv), most = std::clamp<int64_t>(workgroups / blocks, 1, all), each = (all + most - 1) / most;
+    a.slices = static_cast<int32_t>((all + each - 1) / each);
     a.div_slices = fast_div(static_cast<uint32_t>(a.slices));
     return static_cast<unsigned>(blocks * a.slices);
 }
@@ -397,7 +392,7 @@ extern "C" stepq_status stepq_cache_write(const stepq_cache_desc *d, const stepq
     RowsArgs a = rows_args(d, t, cache, page_table, starts, cu_seqlens, k, v);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_shape(d, [&](auto D, auto B) {
-        const dim3 grid(rows_grid<D, 16>(a, WRITE_WGS));
+        const dim3 grid(rows_grid<D, 16>(a, 4096));
         if (t->act_dtype == STEPQ_BF16) cache_write_kernel<bf16_t, D, B><<<grid, kThreads, 0, s>>>(a);
         else cache_write_kernel<float, D, B><<<grid, kThreads, 0, s>>>(a);
     });
@@ -413,7 +408,7 @@ extern "C" stepq_status stepq_cache_read(const stepq_cache_desc *d, const stepq_
     RowsArgs a = rows_args(d, t, cache, page_table, starts, cu_seqlens, k, v);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_shape(d, [&](auto D, auto B) {
-        const dim3 grid(rows_grid<D, 8>(a, READ_WGS));
+        const dim3 grid(rows_grid<D, 8>(a, 2048));
         if (t->act_dtype == STEPQ_BF16) cache_read_kernel<bf16_t, D, B><<<grid, kThreads, 0, s>>>(a);
         else cache_read_kernel<float, D, B><<<grid, kThreads, 0, s>>>(a);
     });

@@ -21,10 +21,7 @@ struct CacheAttnArgs {
     float scale;             // times log2 e: scores are kept in powers of two
 };
 
-#ifndef MAXC
-#define MAXC 1024
-#endif
-constexpr int kMaxChunk = MAXC;
+constexpr int kMaxChunk = 1024;
 constexpr int kTile = 32;    // keys of a wave's turn
 // Waves of a SIMD that the registers are for.
 template <typename T, int D>
@@ -101,14 +98,15 @@ void cache_attn_kernel(CacheAttnArgs a)
     const int32_t *table = a.table + static_cast<size_t>(b) * a.max_pages;
     const int32_t *chosen = a.selected ? a.selected + static_cast<size_t>(bh) * a.n_select : nullptr;
     const int from = part * a.chunk, most = (chosen ? a.n_select : a.max_pages) * page;
-    const int first_page = page_of(from, a.c.div_page), end_page = page_of(min(most, from + a.chunk) - 1, a.c.div_page) + 1;
+    const int first_page = page_of(from, a.c.div_page);
+    const int end_page = most ? page_of(min(most, from + a.chunk) - 1, a.c.div_page) + 1 : 0;
     // page p's position and id; both are looked up before the length is there
     const auto look = [&](int p, int &pos, int &id) {
         pos = chosen ? chosen[p] : p;
         id = pos >= 0 && pos < a.max_pages ? table[pos] : -1;
     };
     int pos0 = 0, id0 = -1;
-    if (most && first_page + static_cast<int>(threadIdx.x) < end_page) look(first_page + threadIdx.x, pos0, id0);
+    if (first_page + static_cast<int>(threadIdx.x) < end_page) look(first_page + threadIdx.x, pos0, id0);
 
     // queries, operand B: query n, the 8 dimensions of each step that the codes of a lane group stand for
     const size_t qrow = static_cast<size_t>(b) * a.Hq + hk * a.G + row0 + min(n, rows - 1);
@@ -143,12 +141,14 @@ void cache_attn_kernel(CacheAttnArgs a)
     bf16x8 q[STEPS][QP];
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
+        if (!(a.scale > 0.0f))
+#pragma unroll
+            for (u32x4 &y : raw[st]) y = with_sign(y, a.scale, BF ? 0x80008000u : 0x80000000u);
         if constexpr (BF) {
-            q[st][0] = __builtin_bit_cast(bf16x8, with_sign(raw[st][0], a.scale, 0x80008000u));
+            q[st][0] = __builtin_bit_cast(bf16x8, raw[st][0]);
         } else {
             bf16x8 p[3];
-            split(__builtin_bit_cast(f32x4, with_sign(raw[st][0], a.scale, 0x80000000u)),
-                  __builtin_bit_cast(f32x4, with_sign(raw[st][1], a.scale, 0x80000000u)), p);
+            split(__builtin_bit_cast(f32x4, raw[st][0]), __builtin_bit_cast(f32x4, raw[st][1]), p);
 #pragma unroll
             for (int i = 0; i < 3; ++i) q[st][i] = p[i];
         }

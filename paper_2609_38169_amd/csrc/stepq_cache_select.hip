@@ -3,12 +3,6 @@
 
 #include "stepq_cache.h"
 
-#ifndef SCORE_WGS
-#define SCORE_WGS 2048
-#endif
-#ifndef SCORE_U
-#define SCORE_U 4
-#endif
 namespace stepq {
 namespace {
 
@@ -43,7 +37,7 @@ __device__ __forceinline__ uint32_t key_of(float x)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
 {
-    constexpr int lanes = D / 4, at_once = 256 / lanes, U = SCORE_U;
+    constexpr int lanes = D / 4, at_once = 256 / lanes, U = 4;
     const int lane = threadIdx.x % lanes, sub = threadIdx.x / lanes;
     int x = blockIdx.x;
     const int turn = x % a.turns;
@@ -323,8 +317,8 @@ extern "C" stepq_status stepq_cache_select(const stepq_cache_desc *c, const step
                  d->n_first, d->n_last, 1, fast_div(static_cast<uint32_t>(c->page_size))};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (need) {
-        const int64_t at_once = SCORE_U * 1024 / c->head_dim;      // pages of a workgroup's turn
-        a.turns = static_cast<int32_t>(std::clamp<int64_t>(SCORE_WGS / pairs, 1, (d->max_pages + at_once - 1) / at_once));
+        const int64_t at_once = 4 * 1024 / c->head_dim;      // pages of a workgroup's turn
+        a.turns = static_cast<int32_t>(std::clamp<int64_t>(2048 / pairs, 1, (d->max_pages + at_once - 1) / at_once));
         if (d->act_dtype == STEPQ_BF16) score<bf16_t>(a, c->head_dim, s);
         else score<float>(a, c->head_dim, s);
     }

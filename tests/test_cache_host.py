@@ -108,7 +108,7 @@ def test_pointers_and_workspaces():
     L = stepq.lib()
     b = ctypes.byref
     n = ctypes.c_size_t()
-    c, t, a, s = cache(), tokens(), attn(), select()
+    c, t, a, s = cache(), tokens(), attn(), select(max_pages=2000)
     assert L.stepq_cache_bytes(None, b(n), None) == BAD and L.stepq_cache_bytes(b(c), None, None) == BAD
     assert L.stepq_cache_attention_workspace(b(c), None, b(n)) == BAD
     assert L.stepq_cache_attention_workspace(b(c), b(a), None) == BAD

@@ -96,6 +96,11 @@ def check_select(q, bounds, table, lengths, P, S, first, last, bits=8, workspace
     return want
 
 
+# columns of the page table that lead to each form of the selection (up to 1024, more): as many as the pages, or more,
+# which no request uses
+FORMS = [None, 1500]
+
+
 def setup(lens, Hq, Hkv, D, P, act, seed=1, max_pages=None):
     g = torch.Generator().manual_seed(seed)
     B, M = len(lens), -(-max(lens) // P) if max_pages is None else max_pages
@@ -108,12 +113,19 @@ def setup(lens, Hq, Hkv, D, P, act, seed=1, max_pages=None):
 
 @pytest.mark.parametrize("act", [F32, BF16])
 @pytest.mark.parametrize("D", [64, 128, 256])
-@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (6, 2), (20, 1)])
-def test_select(Hq, Hkv, D, act):
-    lens = [100, 0, 1, 700, 333, 161]
-    x = setup(lens, Hq, Hkv, D, 16, act, seed=D)
-    for S, first, last in ((10, 1, 1), (1, 0, 0), (1, 0, 1), (7, 3, 4), (12, 0, 2), (100, 1, 1)):
-        check_select(*x, 16, S, first, last)
+@pytest.mark.parametrize("M", FORMS)
+def test_select(M, D, act):
+    for Hq, Hkv in ((1, 1), (6, 2), (20, 1)):
+        x = setup([100, 0, 1, 700, 333, 161], Hq, Hkv, D, 16, act, seed=D, max_pages=M)
+        for S, first, last in ((10, 1, 1), (1, 0, 0), (1, 0, 1), (7, 3, 4), (12, 0, 2), (100, 1, 1)):
+            check_select(*x, 16, S, first, last)
+
+
+@pytest.mark.parametrize("pages", [255, 1023, 1024, 1025, 8192, 8200])
+def test_pages_at_the_borders_of_the_forms(pages):
+    x = setup([pages, pages - 1, pages - 3, 30], 2, 1, 64, 1, BF16, max_pages=pages)
+    for S, first, last in ((20, 1, 2), (pages - 1, 0, 1), (pages // 2, 0, 0)):
+        check_select(*x, 1, S, first, last)
 
 
 @pytest.mark.parametrize("P", [1, 24, 64])
@@ -130,8 +142,9 @@ def test_long():
     check_select(*x, 1, 1, 0, 0)
 
 
-def test_equal_scores_go_to_the_lowest_position():
-    q, bounds, table, lengths = setup([1600, 1599], 2, 1, 64, 4, F32)
+@pytest.mark.parametrize("M", FORMS)
+def test_equal_scores_go_to_the_lowest_position(M):
+    q, bounds, table, lengths = setup([1600, 1599], 2, 1, 64, 4, F32, max_pages=M)
     bounds[:] = bounds[0]
     want = check_select(q, bounds, table, lengths, 4, 30, 2, 3)
     assert want[0, 0].tolist() == list(range(27)) + [397, 398, 399]
@@ -139,9 +152,10 @@ def test_equal_scores_go_to_the_lowest_position():
     check_select(q, bounds, table, lengths, 4, 333, 2, 3)
 
 
-def test_scores_that_differ_in_their_last_place():
-    """Neighbouring scores, some equal once rounded: whole multiples of 2^-26 beside 1."""
-    q, bounds, table, lengths = setup([800], 1, 1, 64, 4, F32)
+@pytest.mark.parametrize("M", FORMS)
+def test_scores_that_differ_in_their_last_place(M):
+    """Neighbouring scores, some equal once rounded: whole multiples of 2^-30 beside 1."""
+    q, bounds, table, lengths = setup([800], 1, 1, 64, 4, F32, max_pages=M)
     q[:] = 0.0
     q[0, 0, 0], q[0, 0, 1] = 1.0, 2.0 ** -30
     bounds[:] = 0.0
@@ -151,9 +165,10 @@ def test_scores_that_differ_in_their_last_place():
     check_select(q, bounds, table, lengths, 4, 50, 0, 1)
 
 
-def test_scores_that_are_not_finite():
+@pytest.mark.parametrize("M", FORMS)
+def test_scores_that_are_not_finite(M):
     """NaN counts as the highest, then +inf; -inf as the lowest but for pages that are none."""
-    q, bounds, table, lengths = setup([400, 400], 2, 1, 64, 4, F32)
+    q, bounds, table, lengths = setup([400, 400], 2, 1, 64, 4, F32, max_pages=M)
     q[:, :, 0] = 1.0
     n = [int(x) for x in table[0]]
     for i, x in ((10, math.nan), (40, math.nan), (20, math.inf), (60, math.inf)):
@@ -166,9 +181,10 @@ def test_scores_that_are_not_finite():
         check_select(q, bounds, table, lengths, 4, S, 0, 1)
 
 
-def test_what_is_not_used_does_not_matter():
+@pytest.mark.parametrize("M", [40, 1500])
+def test_what_is_not_used_does_not_matter(M):
     """Page ids past a request's pages, and the bounds of pages that always are taken."""
-    q, bounds, table, lengths = setup([100, 90], 4, 2, 64, 4, BF16, max_pages=40)
+    q, bounds, table, lengths = setup([100, 90], 4, 2, 64, 4, BF16, max_pages=M)
     for b in range(2):
         pages = -(-int(lengths[b]) // 4)
         table[b, pages:] = -5
@@ -176,16 +192,18 @@ def test_what_is_not_used_does_not_matter():
     check_select(q, bounds, table, lengths, 4, 9, 1, 2)
 
 
-def test_queries_of_any_size():
+@pytest.mark.parametrize("M", FORMS)
+def test_queries_of_any_size(M):
     """Sums over the heads and dimensions in 64 bits: queries of very different sizes, and zeros."""
-    q, bounds, table, lengths = setup([400], 16, 1, 128, 4, F32)
+    q, bounds, table, lengths = setup([400], 16, 1, 128, 4, F32, max_pages=M)
     q *= 2.0 ** torch.randint(-30, 30, q.shape, generator=torch.Generator().manual_seed(1))
     check_select(q, bounds, table, lengths, 4, 20, 1, 1)
     check_select(torch.zeros_like(q), bounds, table, lengths, 4, 20, 1, 1)
 
 
-def test_a_request_of_no_pages():
-    q, bounds, table, lengths = setup([0, 0], 2, 1, 64, 4, BF16)
+@pytest.mark.parametrize("M", FORMS)
+def test_a_request_of_no_pages(M):
+    q, bounds, table, lengths = setup([0, 0], 2, 1, 64, 4, BF16, max_pages=M)
     want = check_select(q, bounds, table, lengths, 4, 3, 1, 1)
     assert (want == -1).all()
 
