@@ -27,7 +27,7 @@ constexpr int kTile = 32;    // keys of a wave's turn
 template <typename T, int D>
 constexpr int waves_of()
 {
-    if (D == 256) return 1;
+    if (D == 256) return sizeof(T) == 4 ? 1 : 2;
     return sizeof(T) == 4 ? 2 : 3;
 }
 
@@ -263,7 +263,7 @@ void cache_attn_kernel(CacheAttnArgs a)
         for (int rt = 0; rt < RT; ++rt) {
             f32x4 y[NG];
 #pragma unroll
-            for (int i = 0; i < NG; ++i) y[i] = qz[i];
+            for (int i = 0; i < NG; ++i) y[i] = NG == 4 ? f32x4{} : qz[i];
             const auto step = [&](int st, const u32x4 &w) {
                 const bf16x8 k[1] = {__builtin_bit_cast(bf16x8, w)};
                 mma(y[group_of(st)], k, q[st]);
@@ -296,6 +296,9 @@ void cache_attn_kernel(CacheAttnArgs a)
                     }
                 }
             }
+            if constexpr (RAISED && NG == 4)          // one register each, not four
+#pragma unroll
+                for (int i = 0; i < NG; ++i) y[i] += qz[i][0];
             s[rt] = y[0] * *reinterpret_cast<const f32x4 *>(&sc[wave][0][0][16 * rt + 4 * g]);
 #pragma unroll
             for (int i = 1; i < NG; ++i) s[rt] += y[i] * *reinterpret_cast<const f32x4 *>(&sc[wave][0][i][16 * rt + 4 * g]);
@@ -332,10 +335,8 @@ void cache_attn_kernel(CacheAttnArgs a)
                 s[rt][i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i], scale, -low));
                 l += s[rt][i];
             }
-        // weights times the scales of each group of dimensions, in planes
-        bf16x8 p[NG][PP];
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
+        // weights times the scales of a group of dimensions, in planes
+        const auto weights = [&](int i, bf16x8 (&p)[PP]) {
             const float *vsc = &sc[wave][1][i][4 * g];
             const f32x4 y0 = s[0] * *reinterpret_cast<const f32x4 *>(vsc);
             const f32x4 y1 = s[1] * *reinterpret_cast<const f32x4 *>(vsc + 16);
@@ -345,38 +346,46 @@ void cache_attn_kernel(CacheAttnArgs a)
                     bf16x2 hi, lo;
                     if (j < 2) two_planes(y0[2 * j], y0[2 * j + 1], hi, lo);
                     else two_planes(y1[2 * j - 4], y1[2 * j - 3], hi, lo);
-                    p[i][0][2 * j] = hi[0], p[i][0][2 * j + 1] = hi[1];
-                    p[i][1][2 * j] = lo[0], p[i][1][2 * j + 1] = lo[1];
+                    p[0][2 * j] = hi[0], p[0][2 * j + 1] = hi[1];
+                    p[1][2 * j] = lo[0], p[1][2 * j + 1] = lo[1];
                 }
             } else {
-                split(y0, y1, p[i]);
+                split(y0, y1, p);
             }
-        }
+        };
+        // four groups in two passes over the values, nibbles 0 and 2, then 1 and 3: their weights fill the registers
+        constexpr int PASSES = NG == 4 ? 2 : 1, NP = NG / PASSES;
 #pragma unroll
-        for (int cb = 0; cb < RB / 32; ++cb) {
-            uint32_t w[4];                        // 16 columns of 16 bits: keys 4 g .. + 3, then 16 + 4 g .. + 3
+        for (int pass = 0; pass < PASSES; ++pass) {
+            bf16x8 p[NP][PP];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const u32x2 y = read_columns(mine + (16 * i + 4 * g + (n >> 2)) * VS + cb * 32 + (n & 3) * 8);
-                w[2 * i] = y[0], w[2 * i + 1] = y[1];
-            }
-            constexpr int per = BITS == 8 ? 2 : 4;          // dimensions in a column
-            u32x4 u[per];
+            for (int i = 0; i < NP; ++i) weights(PASSES * i + pass, p[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (BITS == 8) {
-                    u[0][i] = bytes_of(w[i], 0, 2), u[1][i] = bytes_of(w[i], 1, 3);
-                } else {
-                    uint32_t y[4];
-                    nibbles_of(w[i], y);
+            for (int cb = 0; cb < RB / 32; ++cb) {
+                uint32_t w[4];                        // 16 columns of 16 bits: keys 4 g .. + 3, then 16 + 4 g .. + 3
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) u[j][i] = y[j];
+                for (int i = 0; i < 2; ++i) {
+                    const u32x2 y = read_columns(mine + (16 * i + 4 * g + (n >> 2)) * VS + cb * 32 + (n & 3) * 8);
+                    w[2 * i] = y[0], w[2 * i + 1] = y[1];
                 }
-            }
+                constexpr int per = BITS == 8 ? 2 : 4;          // dimensions in a column
+                u32x4 u[per];
 #pragma unroll
-            for (int j = 0; j < per; ++j) {
-                const bf16x8 v[1] = {__builtin_bit_cast(bf16x8, u[j])};
-                mma(acc[cb * per + j], v, p[NG == 1 ? 0 : j * (D / 4) / kGroup4]);
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (BITS == 8) {
+                        u[0][i] = bytes_of(w[i], 0, 2), u[1][i] = bytes_of(w[i], 1, 3);
+                    } else {
+                        uint32_t y[4];
+                        nibbles_of(w[i], y);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) u[j][i] = y[j];
+                    }
+                }
+#pragma unroll
+                for (int j = pass; j < per; j += PASSES) {
+                    const bf16x8 v[1] = {__builtin_bit_cast(bf16x8, u[j])};
+                    mma(acc[cb * per + j], v, p[NG == 1 ? 0 : j * (D / 4) / kGroup4 / PASSES]);
+                }
             }
         }
         wave_sync();
@@ -534,12 +543,16 @@ Cut cut_of(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
 {
     const int64_t tokens = static_cast<int64_t>(d->n_select ? d->n_select : d->max_pages) * c->page_size;
     if (d->batch == 0 || tokens == 0) return {kMaxChunk, 1};
-    // A second launch, which joins, takes about 3 us: as long as a workgroup takes for 768 tokens (512 in fp32).
-    const bool bf = d->act_dtype == STEPQ_BF16;
+    // Two workgroups a CU (one of D = 256), of 256 to 1024 tokens; whole calls, us, at 256 / 512 / 768 / 1024:
+    //   8 heads of 128, 8 bits, bf16: 1 request x 32768 tokens 21.0 / 19.1 / 21.4 / 24; 16 x 1024 13.4 / 13.4 / 15.8 / 18;
+    //     64 x 4096 122 / 110 / 106 / 105; 64 x 1-8192 138 / 125 / - / 117; 2 heads, 2 x 4096 9.6 / 11.9 / 15.0 / 16
+    //   2 heads of 256, 8 bits: 1 x 131072 51 / 39 / - / 33; 64 x 8192 125 / 116 / 113 / 105
+    // A join, a second launch, takes 3 us more, which a workgroup spends on 768 tokens (512 in fp32): 4 requests x 640 6.2
+    // in one part, 9.3 in three; 23 x 1333 in fp32 14.8 in two, 10.6 in six.
     const int64_t G = d->n_q_heads / c->n_kv_heads, blocks = static_cast<int64_t>(d->batch) * c->n_kv_heads * ((G + 15) / 16);
-    const int64_t slots = 256 * (c->head_dim == 256 ? 1 : bf ? 3 : 2);       // workgroups that the chip runs at once
-    const int64_t want = std::clamp<int64_t>((blocks * tokens + slots - 1) / slots, 256, kMaxChunk);
-    const int64_t chunk = tokens <= (bf ? 768 : 512) ? 768 : (want + 127) / 128 * 128;
+    const int64_t fill = c->head_dim == 256 ? 256 : 512, one = d->act_dtype == STEPQ_BF16 ? 768 : 512;
+    const int64_t want = std::clamp<int64_t>((blocks * tokens + fill - 1) / fill, 256, kMaxChunk);
+    const int64_t chunk = tokens <= one ? one : (want + 127) / 128 * 128;
     return {static_cast<int32_t>(chunk), static_cast<int32_t>((tokens + chunk - 1) / chunk)};
 }
 
