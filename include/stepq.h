@@ -537,7 +537,9 @@ stepq_status stepq_cache_attention(const stepq_cache_desc *desc, const stepq_cac
  * where one is.  Brings those pages up to date that hold tokens starts[b] ..
  * lengths[b] - 1 of request b (none: starts[b] < 0, or not below the length): a
  * prompt's pages after it is written, the last page after each new token.  A page's
- * tokens from the length on do not count; other pages' bounds stay as they are. */
+ * tokens from the length on do not count; other pages' bounds stay as they are.  Where
+ * several requests bring one page up to date in a call, its tokens have to be the same
+ * ones. */
 stepq_status stepq_cache_bounds(const stepq_cache_desc *desc, const void *cache, int32_t batch, int32_t max_pages,
                                 const int32_t *page_table, const int32_t *starts, const int32_t *lengths, void *bounds,
                                 void *stream);

@@ -519,21 +519,6 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a)
     if (d == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
 }
 
-stepq_status check(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
-{
-    if (const stepq_status st = check_cache(c)) return st;
-    if (!d) return bad("desc is NULL");
-    if (d->n_q_heads < 1 || d->n_q_heads % c->n_kv_heads) return bad("n_q_heads must be a multiple of the cache's n_kv_heads, >= 1");
-    if (!known_dtype(d->act_dtype)) return bad("unknown activation dtype");
-    if (d->batch < 0 || d->max_pages < 0 || d->n_select < 0) return bad("negative count");
-    if (!std::isfinite(d->scale)) return bad("scale must be finite");
-    if (static_cast<int64_t>(std::max(d->max_pages, d->n_select)) * c->page_size >= (int64_t(1) << 30))
-        return set_error(STEPQ_E_UNSUPPORTED, "2^30 tokens or more in a request's pages or in its selected ones");
-    if (static_cast<int64_t>(d->batch) * d->n_q_heads > (int64_t(1) << 23))      // a launch has less than 2^32 threads
-        return set_error(STEPQ_E_UNSUPPORTED, "more than 2^23 (request, head) rows in one call: split the batch");
-    return STEPQ_OK;
-}
-
 // Tokens of a part (the last of a request's may have fewer), and the most parts that a request takes.
 struct Cut {
     int32_t chunk, parts;
@@ -554,6 +539,26 @@ Cut cut_of(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
     const int64_t want = std::clamp<int64_t>((blocks * tokens + fill - 1) / fill, 256, kMaxChunk);
     const int64_t chunk = tokens <= one ? one : (want + 127) / 128 * 128;
     return {static_cast<int32_t>(chunk), static_cast<int32_t>((tokens + chunk - 1) / chunk)};
+}
+
+stepq_status check(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
+{
+    if (const stepq_status st = check_cache(c)) return st;
+    if (!d) return bad("desc is NULL");
+    if (d->n_q_heads < 1 || d->n_q_heads % c->n_kv_heads) return bad("n_q_heads must be a multiple of the cache's n_kv_heads, >= 1");
+    if (!known_dtype(d->act_dtype)) return bad("unknown activation dtype");
+    if (d->batch < 0 || d->max_pages < 0 || d->n_select < 0) return bad("negative count");
+    if (!std::isfinite(d->scale)) return bad("scale must be finite");
+    if (static_cast<int64_t>(std::max(d->max_pages, d->n_select)) * c->page_size >= (int64_t(1) << 30))
+        return set_error(STEPQ_E_UNSUPPORTED, "2^30 tokens or more in a request's pages or in its selected ones");
+    if (static_cast<int64_t>(d->batch) * d->n_q_heads > (int64_t(1) << 23))      // a launch has less than 2^32 threads
+        return set_error(STEPQ_E_UNSUPPORTED, "more than 2^23 (request, head) rows in one call: split the batch");
+    const Cut cut = cut_of(c, d);
+    const int64_t rows = static_cast<int64_t>(d->batch) * d->n_q_heads, G = d->n_q_heads / c->n_kv_heads;
+    if (static_cast<int64_t>(d->batch) * c->n_kv_heads * ((G + 15) / 16) * cut.parts >= (int64_t(1) << 24) ||
+        (cut.parts > 8 && rows * (c->head_dim / 64) >= (int64_t(1) << 24)))
+        return set_error(STEPQ_E_UNSUPPORTED, "2^24 or more workgroups for these requests and pages: split the batch");
+    return STEPQ_OK;
 }
 
 size_t workspace_of(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)

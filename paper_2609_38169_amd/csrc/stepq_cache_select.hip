@@ -254,6 +254,8 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(SelectArgs a)
     }
 }
 
+constexpr int kFewPages = 256 * 4;     // of a table: a quarter of the threads select among them
+
 stepq_status check(const stepq_cache_desc *c, const stepq_cache_select_desc *d)
 {
     if (const stepq_status st = check_cache(c)) return st;
@@ -267,6 +269,8 @@ stepq_status check(const stepq_cache_desc *c, const stepq_cache_select_desc *d)
         return set_error(STEPQ_E_UNSUPPORTED, "2^30 tokens or more in a request's pages or in its selected ones");
     if (static_cast<int64_t>(d->batch) * d->n_q_heads > (int64_t(1) << 23))
         return set_error(STEPQ_E_UNSUPPORTED, "more than 2^23 (request, head) rows in one call: split the batch");
+    if (d->max_pages > kFewPages && static_cast<int64_t>(d->batch) * c->n_kv_heads >= (int64_t(1) << 22))
+        return set_error(STEPQ_E_UNSUPPORTED, "2^22 or more (request, key/value head) pairs of many pages: split the batch");
     return STEPQ_OK;
 }
 
@@ -323,7 +327,7 @@ extern "C" stepq_status stepq_cache_select(const stepq_cache_desc *c, const step
         else score<float>(a, c->head_dim, s);
     }
     const dim3 grid(static_cast<unsigned>(pairs));
-    if (d->max_pages <= 256 * 4) cache_select_kernel<256, 4><<<grid, 256, 0, s>>>(a);
+    if (d->max_pages <= kFewPages) cache_select_kernel<256, 4><<<grid, 256, 0, s>>>(a);
     else cache_select_kernel<1024, 8><<<grid, 1024, 0, s>>>(a);
     return launched("cache select launch");
 }

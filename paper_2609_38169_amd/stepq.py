@@ -767,10 +767,14 @@ class Cache:
             raise ValueError(f"memory is on {memory.device}, not on {device}")
         if memory.numel() < self.bytes or (self.bytes and memory.data_ptr() % 128):
             raise ValueError(f"memory must hold {self.bytes} bytes, 128-byte aligned")
-        self.memory, self.device = memory, memory.device
+        self._memory, self.device = memory, memory.device
         # what the native checks compare with
         self._plain = native().cache(self.n_pages, self.Hkv, self.page_size, self.D, self.bits,
                                      -1 if memory.device.index is None else memory.device.index, memory.data_ptr())
+
+    @property
+    def memory(self):
+        return self._memory                     # the same for good: its address is with the native checks
 
     def write(self, k, v, page_table, starts, cu_seqlens=None, stream=None):
         stepq_cache_write(self, k, v, page_table, starts, cu_seqlens, stream)
@@ -791,7 +795,9 @@ class Cache:
 def _cache_device(cache):
     if not isinstance(cache, Cache):
         raise TypeError("cache must be a stepq.Cache")
-    if cache.device.type != "cuda" or cache.device.index != torch.cuda.current_device():
+    if cache.device.type != "cuda":
+        raise ValueError(f"the cache is on {cache.device}, not on a GPU")
+    if cache.device.index != torch.cuda.current_device():
         raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
     return cache.device
 

@@ -3,6 +3,7 @@ host only, nothing here reaches a launch."""
 import ctypes
 
 import pytest
+import torch
 
 import _cache as C
 from paper_2609_38169_amd import stepq
@@ -99,6 +100,18 @@ def test_select_descriptors(bad, status):
     assert L.stepq_cache_select(ctypes.byref(cache()), ctypes.byref(select(**bad)), P, P, P, P, P, P, 1 << 40, None) == status
 
 
+def test_more_workgroups_than_a_launch_takes():
+    L = stepq.lib()
+    c = cache(n_kv_heads=64)
+    many = dict(batch=1 << 17, n_q_heads=64)                 # 2^23 rows: one part each, or more
+    assert size(L.stepq_cache_attention_workspace, c, attn(max_pages=16, **many)) == (0, 0)
+    assert size(L.stepq_cache_attention_workspace, c, attn(max_pages=128, **many))[0] == UNSUPPORTED
+    d = attn(max_pages=128, **many)
+    assert L.stepq_cache_attention(ctypes.byref(c), ctypes.byref(d), P, P, P, P, None, P, P, P, 1 << 50, None) == UNSUPPORTED
+    assert size(L.stepq_cache_select_workspace, c, select(max_pages=1024, **many))[0] == 0
+    assert size(L.stepq_cache_select_workspace, c, select(max_pages=1025, **many))[0] == UNSUPPORTED
+
+
 def refuse(call, args, changes):
     for i, x in changes:
         assert call(*(x if j == i else y for j, y in enumerate(args))) == BAD, (i, x)
@@ -156,6 +169,18 @@ def test_sizes(page, D, bits):
     assert stepq.stepq_cache_bytes(most, 1, page, D, bits)[0] == most * r
     with pytest.raises(stepq.StepqError):
         stepq.stepq_cache_bytes(most + 1, 1, page, D, bits)
+
+
+def test_the_memory_stays():
+    n = stepq.stepq_cache_bytes(2, 1, 4, 64, 8)[0]
+    m = torch.zeros(n + 128, dtype=torch.uint8)
+    m = m[-m.data_ptr() % 128:][:n]
+    c = stepq.Cache(2, 1, 4, 64, 8, memory=m)
+    assert c.memory is m and c.bytes == n
+    with pytest.raises(AttributeError):
+        c.memory = m.clone()
+    with pytest.raises(ValueError):                          # not on a GPU
+        c.write(*(torch.zeros(1, 1, 64),) * 2, torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
 
 
 def test_values_that_no_field_holds():
