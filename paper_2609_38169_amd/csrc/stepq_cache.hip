@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "stepq_cache.h"
+#include "stepq_device.h"
 
 namespace stepq {
 
@@ -99,17 +100,52 @@ struct __attribute__((packed, aligned(sizeof(T)))) Raw {     // N elements at an
 
 constexpr int kThreads = 256;
 
-// Quantizes rows: scale s, the smallest bfloat16 with top s >= the group's
-// largest magnitude; codes rint(x / s).  The quotient is rounded once before rint:
-// s has 8 bits and a tie 8 more, so that no fp32 value but the tie itself rounds
-// to it, and the codes are those of the exact quotient.
+// The largest of N neighbouring lanes, 4, 8 or 16; a group takes part as one.
+template <int N>
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t x)
+{
+    x = max(x, dpp_bits<0xB1, 0xF>(x));                               // quad_perm [1,0,3,2]
+    x = max(x, dpp_bits<0x4E, 0xF>(x));                               // quad_perm [2,3,0,1]
+    if constexpr (N > 4) x = max(x, dpp_bits<0x141, 0xF>(x));         // row_half_mirror: 8 lanes
+    if constexpr (N > 8) x = max(x, dpp_bits<0x140, 0xF>(x));         // row_mirror: 16 lanes
+    return x;
+}
+
+// rint(x / s) in the low bits of the result, in two's complement: of |x / s| < 128, s a bfloat16 and r = 1 / s
+// within 2^-22 of it.  Rounded to a whole number by adding 3 2^22, whose last bit counts ones.
+//   bfloat16: with s' and x' of 8 bits a quotient off a tie is at least 1 / 1020 off it (|x' 2^a - (c + 1/2) s'| >= 1/4,
+// and a > -3 there), while x r is within 2^-14 of it.  So x r, rounded first to a multiple of 2^-11, is on a tie only if
+// x / s is, and on the same side of it otherwise.
+//   float: x r corrected by its remainder is within 2^-43 of x / s before its last rounding.  x and a tie times s (16 bits)
+// are multiples of x's last bit, so that off a tie x / s is 2^-24 of itself off it.  Ties above 1/2 are 1.5 times a power of
+// two or more, and a rounding moves what lies beside them by 2^-24 / 1.5 of them; just below 1/2 by 2^-25.
+template <typename T>
+__device__ __forceinline__ uint32_t rounded_quotient(float x, float s, float r)
+{
+    constexpr float ones = 0x1.8p23f, steps = 0x1.8p12f;
+    if constexpr (std::is_same_v<T, float>) {
+        const float y = x * r;
+        return __float_as_uint(__builtin_fmaf(__builtin_fmaf(-y, s, x), r, y) + ones);
+    } else {
+        return __float_as_uint(__builtin_fmaf(x, r, steps) + (ones - steps));
+    }
+}
+
+// Quantizes rows: scale s, the smallest bfloat16 with top s >= the group's largest magnitude (rounded
+// up, so that no code is past the top); codes rint(x / s), those of the exact quotient.
+//   A workgroup takes 32 tokens (D = 128) whose places it looks up once, and a share
+// of their 2 Hkv rows: found again for every row, 50 us where 42 did.  Bound by memory: 25497
+// tokens of 8 heads of 128 bfloat16 out of a projection's output, 8 bits, 104 MB in 256-byte pieces
+// and 53 MB out, in 39 us, 4.0 TB/s, with the vector units busy 40 % of it (41 us with divisions and
+// conversions, 18.8 M vector instructions for 8.0, which filled them).  The next one or three
+// rows' loads ahead gain nothing (70 us with the read for 69, 18 for 16 of fp32).  4 tokens: 3.3 us, a launch.
 template <typename T, int D, int BITS>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(RowsArgs a)
 {
     using S = Share<D, BITS>;
     using Row = RowOf<D, BITS>;
     constexpr int rows = kThreads / S::lanes, per = S::runs / Row::scales;    // runs of one group: all (8 bits, D = 64), 2 or 1
-    constexpr float q = BITS == 8 ? 127.0f : 7.0f;
+    constexpr float q = BITS == 8 ? 127.0f : 7.0f, below = (1.0f - 0x1p-22f) / q;
     const int lane = threadIdx.x % S::lanes;
     const int block = page_of(blockIdx.x, a.div_slices), slice = blockIdx.x - block * a.slices;
     const int64_t t64 = static_cast<int64_t>(block) * rows + threadIdx.x / S::lanes;
@@ -143,11 +179,10 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(RowsArgs a)
             uint32_t g = top[n * per];
 #pragma unroll
             for (int j = 1; j < per; ++j) g = max(g, top[n * per + j]);
-#pragma unroll
-            for (int m = 1; m < S::lanes; m <<= 1) g = max(g, static_cast<uint32_t>(__shfl_xor(static_cast<int>(g), m)));
+            g = max_of_lanes<S::lanes>(g);
             const float big = __uint_as_float(g);
-            uint32_t u = (__float_as_uint(big / q) + 0xffffu) & 0xffff0000u;
-            if (__uint_as_float(u) * q < big) u += 0x10000u;
+            uint32_t u = (__float_as_uint(big * below) + 0xffffu) & 0xffff0000u;     // less than two of its last bits too low
+            if (__uint_as_float(u) * q < big) u += 0x10000u;                         // the product is exact
             if (big < 0x1p-100f) u = 0;
             if (g >= 0x7f800000u) u = 0x7fc00000u;
             if (lane == n) mine = static_cast<bf16_t>(u >> 16);
@@ -155,14 +190,23 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(RowsArgs a)
         }
         uint32_t word[BITS == 8 ? 4 : 2] = {};
 #pragma unroll
-        for (int j = 0; j < S::runs; ++j)
+        for (int j = 0; j < S::runs; ++j) {
+            const float sc = s[j / per], inv = __builtin_amdgcn_rcpf(sc);
+            const uint32_t keep = sc > 0.0f ? ~0u : 0u;                   // no scale, no codes: whatever came of them
+            uint32_t c[S::run];
 #pragma unroll
-            for (int i = 0; i < S::run; ++i) {
-                const float sc = s[j / per];
-                const int c = sc > 0.0f ? static_cast<int>(rintf(e[j * S::run + i] / sc)) : 0;
-                if constexpr (BITS == 8) word[i / 4] |= (static_cast<uint32_t>(c) & 0xffu) << (8 * (i % 4));
-                else word[i / 2] |= (static_cast<uint32_t>(c) & 0xfu) << (16 * (i % 2) + 4 * j);
+            for (int i = 0; i < S::run; ++i) c[i] = rounded_quotient<T>(e[j * S::run + i], sc, inv);
+            if constexpr (BITS == 8) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    word[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[4 * i + 3], c[4 * i + 2], 0x0c0c0400),
+                                                    __builtin_amdgcn_perm(c[4 * i + 1], c[4 * i], 0x0c0c0400), 0x05040100) & keep;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    word[i] |= (__builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100) & 0x000f000fu & keep) << 4 * j;
             }
+        }
         uint8_t *to = rec + Row::codes(a.c.page, value, row) + lane * (BITS * 2);
         if constexpr (BITS == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(word[0], word[1], word[2], word[3]);
         else *reinterpret_cast<uint2 *>(to) = make_uint2(word[0], word[1]);
@@ -170,8 +214,10 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(RowsArgs a)
     }
 }
 
-// Read back: a thread takes 8 neighbouring dimensions, so that a row's values are written in one piece: 8 bytes of
-// codes, or one nibble of 8 words.
+// Read back: a thread takes 8 neighbouring dimensions, so that a row's values are written in one piece (16 bytes a
+// lane): 8 bytes of codes, or one nibble of 8 words.  Four rows are under way at once; places are looked up as above (75 us
+// without, 39 with).  Bound by memory: 32048 tokens of 8 heads of 128 in 4 bits, 35 MB into 131 MB of bfloat16, in 39 us,
+// 4.3 TB/s.
 template <typename T, int D, int BITS>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(RowsArgs a)
 {
@@ -242,7 +288,10 @@ __device__ __forceinline__ bf16_t bf16_below(float x)
 }
 
 // A thread takes 4 bytes of every row of its group: 4 dimensions of 8-bit codes,
-// nibbles 0 .. 3 of 2 words of 4-bit ones; the groups of rows join in LDS.
+// nibbles 0 .. 3 of 2 words of 4-bit ones; the groups of rows join in LDS.  Minimum
+// and maximum leave out what is not a number, which its scale tells.  Bound by its chain
+// of loads (length, page, codes): 64 requests x 8 heads, a page of 64 tokens each, 5.2 us
+// (25 with 16 elements a thread and the joins by exchanges between lanes).
 template <int D, int BITS>
 __global__ __launch_bounds__(kThreads) void cache_bounds_kernel(BoundsArgs a)
 {
@@ -356,7 +405,9 @@ RowsArgs rows_args(const stepq_cache_desc *d, const stepq_cache_tokens *t, const
             static_cast<int32_t>(t->n_tokens), t->n_seq, t->max_pages, 1, {}};
 }
 
-// EACH elements a thread; a token's rows go to as many workgroups as fill the chip, 8 on a CU.
+// EACH elements a thread; a token's rows go to as many workgroups as there are with fewer tokens: written and read
+// back, 25497 tokens take 71, 70 and 69 us with 2048, 4096 and 8192 of them to write and 2048 to read, 32048 of 4 bits 45
+// with each; with 4096 to read 2 more.
 template <int D, int EACH>
 unsigned rows_grid(RowsArgs &a, int64_t workgroups)
 {
@@ -392,7 +443,7 @@ extern "C" stepq_status stepq_cache_write(const stepq_cache_desc *d, const stepq
     RowsArgs a = rows_args(d, t, cache, page_table, starts, cu_seqlens, k, v);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_shape(d, [&](auto D, auto B) {
-        const dim3 grid(rows_grid<D, 16>(a, 4096));
+        const dim3 grid(rows_grid<D, 16>(a, 8192));
         if (t->act_dtype == STEPQ_BF16) cache_write_kernel<bf16_t, D, B><<<grid, kThreads, 0, s>>>(a);
         else cache_write_kernel<float, D, B><<<grid, kThreads, 0, s>>>(a);
     });
