@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "stepq_cache.h"
+#include "stepq_device.h"
 
 namespace stepq {
 namespace {
@@ -30,10 +31,23 @@ __device__ __forceinline__ uint32_t key_of(float x)
     return x != x ? 0xffffffffu : u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 
+// Another lane's number, by the lane exchange that CTRL encodes.
+template <int CTRL>
+__device__ __forceinline__ double exchanged(double x)
+{
+    const uint64_t u = static_cast<uint64_t>(__double_as_longlong(x));
+    const uint64_t lo = dpp_bits<CTRL, 0xF>(static_cast<uint32_t>(u)), hi = dpp_bits<CTRL, 0xF>(static_cast<uint32_t>(u >> 32));
+    return __longlong_as_double(static_cast<long long>(hi << 32 | lo));
+}
+
 // score = sum_d hi_d sum_h max(q_hd, 0) + lo_d sum_h min(q_hd, 0): a lane keeps
 // the sums over the heads for 8 dimensions of one bound and takes page after page,
-// four at a time; D/4 lanes make a page's score.  In 64 bits, so that no order of
-// summation tells: the score is rounded once.
+// four at a time; D/4 lanes make a page's score.  Summed in 64 bits and rounded once: an error
+// of 2^-45 of the terms, so that the order of summation hardly ever tells.
+// Bound by vector issue (70 % of the cycles, half of them before the first page: the sums
+// over the heads) and latency: 64 requests x 8 heads x 217 pages of 128 dimensions
+// (57 MB) in 18.9 us, 8192 pages of one request (34 MB) in 11.8; 19.5 and 11.8 with every sum
+// added up by every lane; eight pages at a time, or half as many workgroups, are no faster.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
 {
@@ -94,16 +108,17 @@ __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
             for (int i = 0; i < 8; ++i)
                 sum[u] = fma(w[i], static_cast<double>(__uint_as_float(i % 2 ? y[i / 2] & 0xffff0000u : y[i / 2] << 16)), sum[u]);
         }
+        // each exchange halves the sums that a lane holds, so that lane u has score u (modulo 4), then adds their parts
+        double mine;
+        const bool odd = lane & 1, upper = lane & 2;
+        {
+            const double x = (odd ? sum[1] : sum[0]) + exchanged<0xB1>(odd ? sum[0] : sum[1]);     // quad_perm [1,0,3,2]
+            const double y = (odd ? sum[3] : sum[2]) + exchanged<0xB1>(odd ? sum[2] : sum[3]);
+            mine = (upper ? y : x) + exchanged<0x4E>(upper ? x : y);                               // quad_perm [2,3,0,1]
+        }
 #pragma unroll
-        for (int m = 1; m < lanes; m <<= 1)
-#pragma unroll
-            for (int u = 0; u < U; ++u) sum[u] += __shfl_xor(sum[u], m);
-        // lane u of the page's lanes writes score u
-        double mine = sum[0];
-        bool mine_there = there[0];
-#pragma unroll
-        for (int u = 1; u < U; ++u)
-            if (lane == u) mine = sum[u], mine_there = there[u];
+        for (int m = 4; m < lanes; m <<= 1) mine += __shfl_xor(mine, m);
+        const bool mine_there = upper ? (odd ? there[3] : there[2]) : (odd ? there[1] : there[0]);
         const int p = p0 + lane * at_once + sub;
         if (lane < U && p < end) keys[p] = mine_there ? key_of(static_cast<float>(mine)) : 0;
     }
@@ -115,7 +130,11 @@ __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
 // holds it, until that is a single number (2 or 3 times as a rule: scores lie
 // close together, so that intervals of their own range tell them apart where
 // their first digits would not); then the pages are written in order.  A thread holds
-// EACH pages of a stretch; more pages are read again, stretch by stretch.
+// EACH pages of a stretch; more pages are read again, stretch by stretch.  Bound by its
+// chain of steps: 64 of 217 pages, 512 times, in 6.6 us; 244 of 8180, 8 times, in 9 (17 with
+// every thread adding up the waves' counts; 32 and 60 with 256 intervals of one digit).
+// Counting for each of up to 512 scores how many are above it takes 12.8, not 6.6, and in one
+// launch with the scores 31, not 26.
 template <int THREADS, int EACH>
 __global__ __launch_bounds__(THREADS) void cache_select_kernel(SelectArgs a)
 {
