@@ -23,6 +23,7 @@ struct CacheAttnArgs {
 
 constexpr int kMaxChunk = 1024;
 constexpr int kTile = 32;    // keys of a wave's turn
+constexpr int kFewParts = 8;
 // Waves of a SIMD that the registers are for.
 template <typename T, int D>
 constexpr int waves_of()
@@ -74,7 +75,22 @@ __device__ __forceinline__ void two_planes(float a, float b, bf16x2 &hi, bf16x2 
 // own as codes, to be read by columns of 16 bits, 2 or 4 dimensions at once, and
 // their scales go into the weights.  The next tile's codes and scales are on their way
 // meanwhile, into the registers that the tile's codes have left.
-template <typename T, int D, int BITS>
+//   Rounded are the sums and weights only: bfloat16 weights to two planes (16 bits), so
+// that their rounding is far below the output's, fp32 ones and queries to three (24 bits).
+//   8 bits: bound by memory, 64 requests x 8 heads x 1-8192 tokens of 128 (550 MB) in 113
+// us, 4.9 TB/s (6.0 is what a kernel that only reads reaches here); 1 x 2 x 131072 of 256 (135 MB) in
+// 28 us.  4 bits: bound by vector issue, 361 instructions for 32 keys of a head, 104 of them
+// for the values' conversion, 64 for the keys' and 32 for the weights' planes: 256 x 8 x 1-4096
+// of 128 (539 MB) in 146 us, 3.7 TB/s, 66 % of the cycles issue.  With the values' codes raised as the keys'
+// it would be 40 fewer; but a sum of 1.5 times the weights leaves 2^-20 of a row's largest value in dimensions
+// whose codes are 0.  Tiles of 64 keys with two waves a SIMD take 7 % more; four waves a SIMD spill (twice the time).
+//   4 requests x 640 tokens: 5.8 us, the chain of loads.
+//   FOLD: few heads leave most of the matrix cores' columns idle, so each group of a row's scales has
+// columns of its own with the same queries: a lane makes the weights of one group, and sums of other groups'
+// dimensions in its column are left.  64 requests x 8192 tokens of 4 bits with 4 or 8 query heads each, whole
+// calls, us, without and with it: 8 heads of 128, bf16, 172 / 158 and 153 / 149, fp32 192 / 185 and 192 / 185;
+// 2 of 256 (4 query heads), bf16, 77 / 70, fp32 126 / 110; 4 requests x 640 9.2 / 8.5 and 9.4 / 9.6.
+template <typename T, int D, int BITS, bool FOLD>
 __global__ __launch_bounds__(256, (waves_of<T, D>()))
 void cache_attn_kernel(CacheAttnArgs a)
 {
@@ -94,7 +110,9 @@ void cache_attn_kernel(CacheAttnArgs a)
     const int Hkv = a.c.Hkv, page = a.c.page;
     const int part = fdiv(blockIdx.x, a.div_items), item = blockIdx.x - part * (a.batch * Hkv * ((a.G + 15) / 16));
     const int bh = fdiv(item, a.div_blocks), row0 = (item - bh * ((a.G + 15) / 16)) * 16;
-    const int b = fdiv(bh, a.div_hkv), hk = bh - b * Hkv, rows = min(16, a.G - row0);
+    // columns of queries: FOLD: the same ones for each group of a row's scales
+    constexpr int COLS = FOLD ? 16 / NG : 16, SETS = FOLD ? 1 : NG;          // of weights, that a lane makes
+    const int b = fdiv(bh, a.div_hkv), hk = bh - b * Hkv, rows = min(COLS, a.G - row0), r = n % COLS, group = n / COLS;
     const int32_t *table = a.table + static_cast<size_t>(b) * a.max_pages;
     const int32_t *chosen = a.selected ? a.selected + static_cast<size_t>(bh) * a.n_select : nullptr;
     const int from = part * a.chunk, most = (chosen ? a.n_select : a.max_pages) * page;
@@ -109,7 +127,7 @@ void cache_attn_kernel(CacheAttnArgs a)
     if (first_page + static_cast<int>(threadIdx.x) < end_page) look(first_page + threadIdx.x, pos0, id0);
 
     // queries, operand B: query n, the 8 dimensions of each step that the codes of a lane group stand for
-    const size_t qrow = static_cast<size_t>(b) * a.Hq + hk * a.G + row0 + min(n, rows - 1);
+    const size_t qrow = static_cast<size_t>(b) * a.Hq + hk * a.G + row0 + min(r, rows - 1);
     u32x4 raw[STEPS][BF ? 1 : 2];
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
@@ -184,10 +202,10 @@ void cache_attn_kernel(CacheAttnArgs a)
         at = 0, unit = 0, row = 0;
         bool ok = false;
         if (t < to) {
-            const int p = page_of(t, a.c.div_page), r = t - p * page;
+            const int p = page_of(t, a.c.div_page), in_page = t - p * page;
             const int2 e = pages[p - first_page];
-            ok = e.x >= 0 && r < e.y;
-            if (ok) at = static_cast<int64_t>(e.x) * a.c.record, row = r, unit = e.x * record_units + r * (RB / 32);
+            ok = e.x >= 0 && in_page < e.y;
+            if (ok) at = static_cast<int64_t>(e.x) * a.c.record, row = in_page, unit = e.x * record_units + in_page * (RB / 32);
         }
         there = static_cast<uint32_t>(__ballot(ok));
     };
@@ -337,7 +355,7 @@ void cache_attn_kernel(CacheAttnArgs a)
             }
         // weights times the scales of a group of dimensions, in planes
         const auto weights = [&](int i, bf16x8 (&p)[PP]) {
-            const float *vsc = &sc[wave][1][i][4 * g];
+            const float *vsc = &sc[wave][1][FOLD ? group : i][4 * g];
             const f32x4 y0 = s[0] * *reinterpret_cast<const f32x4 *>(vsc);
             const f32x4 y1 = s[1] * *reinterpret_cast<const f32x4 *>(vsc + 16);
             if constexpr (BF) {
@@ -354,7 +372,7 @@ void cache_attn_kernel(CacheAttnArgs a)
             }
         };
         // four groups in two passes over the values, nibbles 0 and 2, then 1 and 3: their weights fill the registers
-        constexpr int PASSES = NG == 4 ? 2 : 1, NP = NG / PASSES;
+        constexpr int PASSES = SETS == 4 ? 2 : 1, NP = SETS / PASSES;
 #pragma unroll
         for (int pass = 0; pass < PASSES; ++pass) {
             bf16x8 p[NP][PP];
@@ -384,7 +402,7 @@ void cache_attn_kernel(CacheAttnArgs a)
 #pragma unroll
                 for (int j = pass; j < per; j += PASSES) {
                     const bf16x8 v[1] = {__builtin_bit_cast(bf16x8, u[j])};
-                    mma(acc[cb * per + j], v, p[NG == 1 ? 0 : j * (D / 4) / kGroup4 / PASSES]);
+                    mma(acc[cb * per + j], v, p[SETS == 1 ? 0 : j * (D / 4) / kGroup4 / PASSES]);
                 }
             }
         }
@@ -403,8 +421,8 @@ void cache_attn_kernel(CacheAttnArgs a)
     for (int w = 0; w < 4; ++w) z += sl[w][n] * __builtin_amdgcn_exp2f(sm[w][n] - base_m);
     const float own = __builtin_amdgcn_exp2f(mine_m - base_m);
     float *sum = reinterpret_cast<float *>(vs);       // [wave][row][LD]
-    if (n < rows) {
-        float *to_row = sum + (wave * 16 + n) * LD;
+    if (r < rows) {
+        float *to_row = sum + (wave * 16 + r) * LD;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) acc[i] *= own;
         if constexpr (BITS == 8) {
@@ -417,7 +435,8 @@ void cache_attn_kernel(CacheAttnArgs a)
         } else {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
-                *reinterpret_cast<f32x4 *>(to_row + i % 4 * (D / 4) + i / 4 * 16 + 4 * g) = acc[i];
+                if (!FOLD || i % 4 * (D / 4) / kGroup4 == group)
+                    *reinterpret_cast<f32x4 *>(to_row + i % 4 * (D / 4) + i / 4 * 16 + 4 * g) = acc[i];
         }
     }
     const size_t all = static_cast<size_t>(a.batch) * a.Hq, first = static_cast<size_t>(b) * a.Hq + hk * a.G + row0;
@@ -433,53 +452,91 @@ void cache_attn_kernel(CacheAttnArgs a)
     }
     if (only) __syncthreads();
     for (int e = threadIdx.x; e < rows * (D / 4); e += 256) {
-        const int r = e / (D / 4), c = e % (D / 4);
-        f32x4 y = *reinterpret_cast<const f32x4 *>(sum + r * LD + 4 * c);
+        const int x = e / (D / 4), c = e % (D / 4);
+        f32x4 y = *reinterpret_cast<const f32x4 *>(sum + x * LD + 4 * c);
 #pragma unroll
-        for (int w = 1; w < 4; ++w) y += *reinterpret_cast<const f32x4 *>(sum + (w * 16 + r) * LD + 4 * c);
+        for (int w = 1; w < 4; ++w) y += *reinterpret_cast<const f32x4 *>(sum + (w * 16 + x) * LD + 4 * c);
         if (only) {
-            const float d = sl[0][r];
-            T *o = static_cast<T *>(a.o) + (first + r) * D + 4 * c;
+            const float d = sl[0][x];
+            T *o = static_cast<T *>(a.o) + (first + x) * D + 4 * c;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = narrow<T>(d == 0.0f ? 0.0f : y[i] / d);
         } else {
-            reinterpret_cast<f32x4 *>(a.acc + (part * all + first + r) * D)[c] = y;
+            reinterpret_cast<f32x4 *>(a.acc + (part * all + first + x) * D)[c] = y;
         }
     }
 }
 
-// The parts of each row joined, 64 dimensions by 16 lanes; SLOTS (4 or 16) such lane groups
-// take a row's parts in turn, four at a time so that their loads overlap.  Rows of
-// one part or none are there already.
-template <typename T, int D, int SLOTS>
+// The parts that row's tokens take; rows of one or none are there already.
+__device__ __forceinline__ int parts_of(const CacheAttnArgs &a, size_t row)
+{
+    if (a.selected) return a.parts;
+    const int len = min(a.lengths[row / a.Hq], a.max_pages * a.c.page);
+    return len <= a.chunk ? 0 : (len + a.chunk - 1) / a.chunk;
+}
+
+// The parts of each row joined where there are few: 4 dimensions a lane, every part's share in its registers.
+// 8192 rows of 128 in 1 to 4 parts: 6.0 us (9.0 with a wave's lane groups a part each, and their sums exchanged), 2048 in 1
+// to 8: 5.0.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnArgs a)
+{
+    const uint32_t x = blockIdx.x * 256 + threadIdx.x;
+    const size_t row = x / (D / 4), all = static_cast<size_t>(a.batch) * a.Hq;
+    const int d = x % (D / 4) * 4;
+    if (row >= all) return;
+    const int parts = parts_of(a, row);
+    if (!parts) return;
+    f32x4 y[kFewParts];
+    float2 ml[kFewParts];
+#pragma unroll
+    for (int p = 0; p < kFewParts; ++p) {             // past the end: the last again
+        const size_t at = min(p, parts - 1) * all + row;
+        ml[p] = a.ml[at];
+        y[p] = *reinterpret_cast<const f32x4 *>(a.acc + at * D + d);
+    }
+    float top = ml[0].x;
+#pragma unroll
+    for (int p = 1; p < kFewParts; ++p) top = fmaxf(top, ml[p].x);
+    const float base = top == -INFINITY ? 0.0f : top;
+    f32x4 sum = {};
+    float z = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kFewParts; ++p)
+        if (p < parts) {
+            const float f = __builtin_amdgcn_exp2f(ml[p].x - base);
+            z = fmaf(ml[p].y, f, z);
+            sum += y[p] * f;
+        }
+    T *o = static_cast<T *>(a.o) + row * D + d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = narrow<T>(z == 0.0f ? 0.0f : sum[i] / z);
+    if (d == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
+}
+
+// The same where there are many: a workgroup takes 64 dimensions of a row by 16 lanes, 16 such
+// lane groups its parts in turn, four at a time so that their loads overlap.
+// 16 rows of 256 in 128 parts: 5.1 us.
+template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a)
 {
-    constexpr int U = 4, units = 16 / SLOTS;          // (row, 64 dimensions) of a workgroup
+    constexpr int U = 4, SLOTS = 16;
     __shared__ float tops[4];
     __shared__ alignas(16) f32x4 sums[4][16];
     __shared__ float zs[4];
-    const int lane = threadIdx.x & 15, slot = (threadIdx.x >> 4) % SLOTS, wave = threadIdx.x >> 6;
-    const uint32_t unit = blockIdx.x * units + (threadIdx.x >> 4) / SLOTS;
-    const size_t row = unit / (D / 64), all = static_cast<size_t>(a.batch) * a.Hq;
-    const int d = unit % (D / 64) * 64 + lane * 4;
-    if (row >= all) return;                           // whole workgroups only where SLOTS = 16
-    int parts = a.parts;
-    if (!a.selected) {
-        const int len = min(a.lengths[row / a.Hq], a.max_pages * a.c.page);
-        if (len <= a.chunk) return;
-        parts = (len + a.chunk - 1) / a.chunk;
-    }
-    constexpr int of = SLOTS == 16 ? 256 : 64;        // threads that look for the largest maximum
+    const int lane = threadIdx.x & 15, slot = threadIdx.x >> 4, wave = threadIdx.x >> 6;
+    const size_t row = blockIdx.x / (D / 64), all = static_cast<size_t>(a.batch) * a.Hq;
+    const int d = blockIdx.x % (D / 64) * 64 + lane * 4;
+    const int parts = parts_of(a, row);
+    if (!parts) return;
     float top = -INFINITY;
-    for (int p = threadIdx.x % of; p < parts; p += of) top = fmaxf(top, a.ml[p * all + row].x);
+    for (int p = threadIdx.x; p < parts; p += 256) top = fmaxf(top, a.ml[p * all + row].x);
 #pragma unroll
     for (int i = 1; i < 16; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
     top = swap_max32(swap_max16(top));
-    if constexpr (SLOTS == 16) {
-        if ((threadIdx.x & 63) == 0) tops[wave] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    }
+    if ((threadIdx.x & 63) == 0) tops[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     const float base = top == -INFINITY ? 0.0f : top;
     f32x4 y = {};
     float z = 0.0f;
@@ -503,16 +560,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a)
     z = swap_add32(swap_add16(z));
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = swap_add32(swap_add16(y[i]));
-    if constexpr (SLOTS == 16) {
-        if ((threadIdx.x & 63) < 16) sums[wave][lane] = y;
-        if ((threadIdx.x & 63) == 0) zs[wave] = z;
-        __syncthreads();
-        if (threadIdx.x >= 16) return;
-        y = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
-        z = zs[0] + zs[1] + zs[2] + zs[3];
-    } else if (slot) {
-        return;
-    }
+    if ((threadIdx.x & 63) < 16) sums[wave][lane] = y;
+    if ((threadIdx.x & 63) == 0) zs[wave] = z;
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    y = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+    z = zs[0] + zs[1] + zs[2] + zs[3];
     T *o = static_cast<T *>(a.o) + row * D + d;
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = narrow<T>(z == 0.0f ? 0.0f : y[i] / z);
@@ -556,7 +609,7 @@ stepq_status check(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
     const Cut cut = cut_of(c, d);
     const int64_t rows = static_cast<int64_t>(d->batch) * d->n_q_heads, G = d->n_q_heads / c->n_kv_heads;
     if (static_cast<int64_t>(d->batch) * c->n_kv_heads * ((G + 15) / 16) * cut.parts >= (int64_t(1) << 24) ||
-        (cut.parts > 8 && rows * (c->head_dim / 64) >= (int64_t(1) << 24)))
+        (cut.parts > kFewParts && rows * (c->head_dim / 64) >= (int64_t(1) << 24)))
         return set_error(STEPQ_E_UNSUPPORTED, "2^24 or more workgroups for these requests and pages: split the batch");
     return STEPQ_OK;
 }
@@ -571,12 +624,15 @@ template <typename T, int D>
 void launch(const CacheAttnArgs &a, int bits, hipStream_t st)
 {
     const int64_t grid = static_cast<int64_t>(a.batch) * a.c.Hkv * ((a.G + 15) / 16) * a.parts;
-    if (bits == 8) cache_attn_kernel<T, D, 8><<<dim3(static_cast<unsigned>(grid)), 256, 0, st>>>(a);
-    else cache_attn_kernel<T, D, 4><<<dim3(static_cast<unsigned>(grid)), 256, 0, st>>>(a);
+    const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), 256, 0, st>>>(a); };
+    constexpr int groups = RowOf<D, 4>::scales;
+    if (bits == 8) run(cache_attn_kernel<T, D, 8, false>);
+    else if (groups > 1 && a.G <= 16 / groups) run(cache_attn_kernel<T, D, 4, (groups > 1)>);
+    else run(cache_attn_kernel<T, D, 4, false>);
     if (a.parts == 1) return;
-    const unsigned units = static_cast<unsigned>(a.batch) * a.Hq * (D / 64);
-    if (a.parts > 8) cache_join_kernel<T, D, 16><<<dim3(units), 256, 0, st>>>(a);
-    else cache_join_kernel<T, D, 4><<<dim3((units + 3) / 4), 256, 0, st>>>(a);
+    const unsigned units = static_cast<unsigned>(a.batch) * a.Hq * (D / 64);     // 16 lanes each
+    if (a.parts > kFewParts) cache_join_kernel<T, D><<<dim3(units), 256, 0, st>>>(a);
+    else cache_join_few_kernel<T, D><<<dim3((units + 15) / 16), 256, 0, st>>>(a);
 }
 
 template <typename T>

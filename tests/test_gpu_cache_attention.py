@@ -81,6 +81,14 @@ def test_heads(D, bits, act):
         Case([70, 1, 33], Hq, Hkv, D, 16, bits, act, seed=Hq).check()
 
 
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("D", [128, 256])
+@pytest.mark.parametrize("G", [2, 4, 5, 8, 9])
+def test_scales_of_more_groups(G, D, act):    # 4 bits: 4 or 8 heads and fewer take the matrix cores' columns twice
+    Case([70, 1, 33, 0], 2 * G, 2, D, 16, 4, act, seed=G).check()
+    Case([1500], G, 1, D, 16, 4, act, seed=G).check()
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("P", [1, 3, 24, 64, 100, 256])
 def test_pages(P, bits):
