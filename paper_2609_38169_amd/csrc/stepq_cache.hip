@@ -136,9 +136,9 @@ __device__ __forceinline__ uint32_t rounded_quotient(float x, float s, float r)
 //   A workgroup takes 32 tokens (D = 128) whose places it looks up once, and a share
 // of their 2 Hkv rows: found again for every row, 50 us where 42 did.  Bound by memory: 25497
 // tokens of 8 heads of 128 bfloat16 out of a projection's output, 8 bits, 104 MB in 256-byte pieces
-// and 53 MB out, in 39 us, 4.0 TB/s, with the vector units busy 40 % of it (41 us with divisions and
-// conversions, 18.8 M vector instructions for 8.0, which filled them).  The next one or three
-// rows' loads ahead gain nothing (70 us with the read for 69, 18 for 16 of fp32).  4 tokens: 3.3 us, a launch.
+// and 53 MB out, in 38 us, 4.1 TB/s, the vector units busy half of it (41 us with divisions and
+// conversions, 18.8 M vector instructions for 9.6, which filled them).  The next one or three
+// rows' loads ahead gain nothing (70 us with the read for 69, 18 for 16 of fp32).  4 tokens: 2.4 us, a launch.
 template <typename T, int D, int BITS>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(RowsArgs a)
 {
