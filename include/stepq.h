@@ -515,16 +515,17 @@ typedef struct {
  * tokens, split over their length and joined:
  *   o = sum_t p_t v_t,  p = softmax over t of scale q.k_t,  lse = log sum_t exp(scale q.k_t)
  * with the values that the cache holds.
- *   q, o [batch][Hq][D] in act_dtype; lse [batch][Hq] fp32 or NULL; lengths [batch]
- *   int32: request b's tokens are the first lengths[b] of its pages (0 .. max_pages
- *   * page_size);
+ *   q (16-byte aligned), o [batch][Hq][D] in act_dtype; lse [batch][Hq] fp32 or NULL;
+ *   lengths [batch] int32: request b's tokens are the first lengths[b] of its pages (0 ..
+ *   max_pages * page_size; less counts as 0, more as all of them);
  *   selected [batch][Hkv][n_select] int32 (n_select > 0): for each key/value head the
  *   positions in page_table of the pages that are read, distinct, in any order; what
  *   lies outside [0, max_pages) is none, tokens past the length are left out.
  * What no request's tokens use may hold anything.  A row without a key, or with all
  * scores -inf, gets o = 0 and lse = -inf.  A key that is not finite makes its heads'
- * o NaN, a value its group of dimensions.  Scores, weights and sums are fp32, weights
- * in 16 bits (bfloat16) or 24 (fp32).  o overlaps no input. */
+ * o NaN, a value its group of dimensions; a query that is not finite may make its
+ * own so.  Scores, weights and sums are fp32, weights in 16 bits (bfloat16) or 24
+ * (fp32).  o overlaps no input. */
 stepq_status stepq_cache_attention_workspace(const stepq_cache_desc *desc, const stepq_cache_attn_desc *attn,
                                              size_t *bytes);
 stepq_status stepq_cache_attention(const stepq_cache_desc *desc, const stepq_cache_attn_desc *attn, const void *cache,
@@ -556,9 +557,9 @@ typedef struct {
  *   score = sum_d hi_d sum_h max(q_hd, 0) + lo_d sum_h min(q_hd, 0)
  * over the query heads h of the key/value head, with the page's bounds: no key of the
  * page has a larger sum of q_h.k.  (For a negative scale of the attention, -q is
- * scored.)  Sums are formed in 64 bits and rounded once, to fp32; a score that is NaN
- * counts as the highest, a page that there is not as the lowest, and of equal scores
- * the lowest position is taken. */
+ * scored.)  q and bounds are 16-byte aligned.  Sums are formed in 64 bits and rounded
+ * once, to fp32; a score that is NaN counts as the highest, a page that there is not
+ * as the lowest, and of equal scores the lowest position is taken. */
 stepq_status stepq_cache_select_workspace(const stepq_cache_desc *desc, const stepq_cache_select_desc *select,
                                           size_t *bytes);
 stepq_status stepq_cache_select(const stepq_cache_desc *desc, const stepq_cache_select_desc *select, const void *bounds,

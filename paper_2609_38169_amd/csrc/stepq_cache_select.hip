@@ -265,8 +265,10 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(SelectArgs a)
         for (int i = 0; i < EACH; ++i) {
             const uint32_t before = more0 + mores[i][wave] + __popcll(bm[i] & below);
             const uint32_t equal = same0 + sames[i][wave] + __popcll(bs[i] & below);
-            if ((bm[i] >> lane & 1) || ((bs[i] >> lane & 1) && equal < want))
-                out[a.n_first + before + min(equal, want)] = p0 + i * THREADS + tid;
+            const uint32_t at = a.n_first + before + min(equal, want);
+            // within the row also where another call has written to the same workspace meanwhile
+            if (((bm[i] >> lane & 1) || ((bs[i] >> lane & 1) && equal < want)) && at < static_cast<uint32_t>(a.n_select - a.n_last))
+                out[at] = p0 + i * THREADS + tid;
         }
         more0 += waves[0], same0 += waves[1];
         __syncthreads();
