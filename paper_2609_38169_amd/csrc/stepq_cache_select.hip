@@ -40,23 +40,22 @@ __device__ __forceinline__ double exchanged(double x)
     return __longlong_as_double(static_cast<long long>(hi << 32 | lo));
 }
 
-// score = sum_d hi_d sum_h max(q_hd, 0) + lo_d sum_h min(q_hd, 0): a lane keeps
-// the sums over the heads for 8 dimensions of one bound and takes page after page,
-// four at a time; D/4 lanes make a page's score.  Summed in 64 bits and rounded once: an error
+// score = sum_d hi_d sum_h max(q_hd, 0) + lo_d sum_h min(q_hd, 0): the workgroup adds
+// up the heads, a lane takes 8 dimensions of one bound of page after page, four at a
+// time; D/4 lanes make a page's score.  Summed in 64 bits and rounded once: an error
 // of 2^-45 of the terms, so that the order of summation hardly ever tells.
-// Bound by vector issue (70 % of the cycles, half of them before the first page: the sums
-// over the heads) and latency: 64 requests x 8 heads x 217 pages of 128 dimensions
-// (57 MB) in 18.9 us, 8192 pages of one request (34 MB) in 11.8; 19.5 and 11.8 with every sum
-// added up by every lane; eight pages at a time, or half as many workgroups, are no faster.
+// Bound by vector issue (58 % of the cycles: conversions, products, the lanes' sums) and
+// latency: 64 requests x 8 heads x 217 pages of 128 dimensions (57 MB) in 16.7 us, 8192
+// pages of one request (34 MB) in 9.1; 18.9 and 11.6 with the heads added up by every lane for itself,
+// 18.5 and 10.7 with the next pages' bounds on their way before that.  Eight pages at a time, or half as many
+// workgroups, are no faster; twice as many 2 us slower where there are many requests.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
 {
     constexpr int lanes = D / 4, at_once = 256 / lanes, U = 4;
+    __shared__ alignas(16) double sums[2 * D];        // over the heads: of the negative parts, then the positive ones
     const int lane = threadIdx.x % lanes, sub = threadIdx.x / lanes;
-    int x = blockIdx.x;
-    const int turn = x % a.turns;
-    x /= a.turns;
-    const int hk = x % a.Hkv, b = x / a.Hkv;
+    const int turn = blockIdx.x % a.turns, pair = blockIdx.x / a.turns, hk = pair % a.Hkv, b = pair / a.Hkv;
     // page ids and queries are asked for before the length is there
     const int32_t *table = a.table + static_cast<size_t>(b) * a.max_pages;
     const auto ids = [&](int p0, int (&id)[U], int end) {
@@ -70,23 +69,30 @@ __global__ __launch_bounds__(256) void cache_score_kernel(SelectArgs a)
     ids(a.n_first + turn * at_once * U, next, a.max_pages);
     const bool high = lane >= lanes / 2;
     const int d0 = lane % (lanes / 2) * 8;
-    double w[8] = {};
-    const T *q = static_cast<const T *>(a.q) + (static_cast<size_t>(b) * a.Hkv + hk) * a.G * D + d0;
-    struct alignas(16) Eight {
-        T x[8];
-    };
-    Eight e = *reinterpret_cast<const Eight *>(q);
+    const T *q = static_cast<const T *>(a.q) + (static_cast<size_t>(b) * a.Hkv + hk) * a.G * D;
+    constexpr int SUMS = 2 * D;
+    T e[(SUMS + 255) / 256];
+#pragma unroll
+    for (int j = 0; j * 256 < SUMS; ++j) e[j] = q[(threadIdx.x + j * 256) % D];
     const int pages = pages_of(a, b), end = pages - a.n_last;
     if (pages <= a.n_select || a.n_first + turn * at_once * U >= end) return;
-    for (int h = 0; h < a.G; ++h) {
-        if (h) e = *reinterpret_cast<const Eight *>(q + static_cast<size_t>(h) * D);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y = widen(e.x[i]);
+    for (int j = 0; j * 256 < SUMS; ++j) {
+        const int x = threadIdx.x + j * 256;
+        if (x >= SUMS) break;
+        double sum = 0.0;
+#pragma unroll 4
+        for (int h = 0; h < a.G; ++h) {
+            const float y = widen(h ? q[static_cast<size_t>(h) * D + x % D] : e[j]);
             // a NaN reaches both sums
-            w[i] += static_cast<double>(high ? (y < 0.0f ? 0.0f : y) : (y > 0.0f ? 0.0f : y));
+            sum += static_cast<double>(x >= D ? (y < 0.0f ? 0.0f : y) : (y > 0.0f ? 0.0f : y));
         }
+        sums[x] = sum;
     }
+    __syncthreads();
+    double w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = sums[high * D + d0 + i];
     uint32_t *keys = a.keys + (static_cast<size_t>(b) * a.Hkv + hk) * a.max_pages;
     for (int p0 = a.n_first + turn * at_once * U; p0 < end; p0 += a.turns * at_once * U) {
         uint4 v[U];
