@@ -508,7 +508,7 @@ typedef struct {
     int32_t max_pages;        /* columns of page_table */
     int32_t act_dtype;        /* stepq_dtype of q and o */
     int32_t n_select;         /* columns of selected; 0: all of each request's tokens */
-    float scale;              /* scores are scale q.k */
+    float scale;              /* scores are scale q.k; at most 2^120 in magnitude */
 } stepq_cache_attn_desc;
 
 /* Softmax attention of one query token of each of `batch` requests over its

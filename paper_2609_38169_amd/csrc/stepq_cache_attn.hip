@@ -602,6 +602,8 @@ stepq_status check(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
     if (!known_dtype(d->act_dtype)) return bad("unknown activation dtype");
     if (d->batch < 0 || d->max_pages < 0 || d->n_select < 0) return bad("negative count");
     if (!std::isfinite(d->scale)) return bad("scale must be finite");
+    if (std::fabs(d->scale) > 0x1p120f)               // times log2 e and a code's unit it has to be finite too
+        return set_error(STEPQ_E_UNSUPPORTED, "a scale past 2^120");
     if (static_cast<int64_t>(std::max(d->max_pages, d->n_select)) * c->page_size >= (int64_t(1) << 30))
         return set_error(STEPQ_E_UNSUPPORTED, "2^30 tokens or more in a request's pages or in its selected ones");
     if (static_cast<int64_t>(d->batch) * d->n_q_heads > (int64_t(1) << 23))      // a launch has less than 2^32 threads
