@@ -18,7 +18,8 @@ struct CacheAttnArgs {
     float *acc;              // [parts][batch * Hq][D]: its unnormalised output
     int32_t batch, Hq, G, max_pages, n_select, parts, chunk;
     FastDiv div_items, div_blocks, div_hkv;      // by the workgroups of one part, by the blocks of 16 heads, by Hkv
-    float scale;             // times log2 e: scores are kept in powers of two
+    float scale;             // times log2 e, scores are kept in powers of two; and 16 of 4 bits, whose codes come as sixteenths
+    float unit;              // of the values' sums: 1, or 16 of 4 bits
 };
 
 constexpr int kMaxChunk = 1024;
@@ -253,7 +254,7 @@ void cache_attn_kernel(CacheAttnArgs a)
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const float y = i % 2 ? upper_bf16(sx[i / 2]) : lower_bf16(sx[i / 2]);
-            sc[wave][lane / KT][i][lane % KT] = mine_there ? (BITS == 4 ? 16.0f * y : y) : 0.0f;
+            sc[wave][lane / KT][i][lane % KT] = mine_there ? y : 0.0f;
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -460,7 +461,7 @@ void cache_attn_kernel(CacheAttnArgs a)
             const float d = sl[0][x];
             T *o = static_cast<T *>(a.o) + (first + x) * D + 4 * c;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = narrow<T>(d == 0.0f ? 0.0f : y[i] / d);
+            for (int i = 0; i < 4; ++i) o[i] = narrow<T>(d == 0.0f ? 0.0f : y[i] / d * a.unit);
         } else {
             reinterpret_cast<f32x4 *>(a.acc + (part * all + first + x) * D)[c] = y;
         }
@@ -510,7 +511,7 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnArgs a)
         }
     T *o = static_cast<T *>(a.o) + row * D + d;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = narrow<T>(z == 0.0f ? 0.0f : sum[i] / z);
+    for (int i = 0; i < 4; ++i) o[i] = narrow<T>(z == 0.0f ? 0.0f : sum[i] / z * a.unit);
     if (d == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
 }
 
@@ -568,7 +569,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a)
     z = zs[0] + zs[1] + zs[2] + zs[3];
     T *o = static_cast<T *>(a.o) + row * D + d;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = narrow<T>(z == 0.0f ? 0.0f : y[i] / z);
+    for (int i = 0; i < 4; ++i) o[i] = narrow<T>(z == 0.0f ? 0.0f : y[i] / z * a.unit);
     if (d == 0 && a.lse) a.lse[row] = z == 0.0f ? -INFINITY : (base + log2f(z)) * kLn2;
 }
 
@@ -685,7 +686,8 @@ extern "C" stepq_status stepq_cache_attention(const stepq_cache_desc *c, const s
     a.div_blocks = fast_div(blocks), a.div_hkv = fast_div(static_cast<uint32_t>(a.c.Hkv));
     a.acc = static_cast<float *>(workspace);
     if (need) a.ml = reinterpret_cast<float2 *>(a.acc + rows * c->head_dim * a.parts);
-    a.scale = d->scale * 1.4426950408889634f;
+    a.unit = c->bits == 4 ? 16.0f : 1.0f;
+    a.scale = d->scale * 1.4426950408889634f * a.unit;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (d->act_dtype == STEPQ_BF16) launch<bf16_t>(a, c->head_dim, c->bits, s);
     else launch<float>(a, c->head_dim, c->bits, s);

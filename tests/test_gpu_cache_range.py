@@ -1,0 +1,80 @@
+"""Attention over quantized caches at the ends of the numbers' range: keys and
+values up to the type's largest.
+
+Tolerances, from the arithmetic.  Products of queries (8 bits, or planes of 24) and
+codes (7 bits) are exact.  A score is a sum of D of them, a product with each
+group's scale and a place in the exponent: D + 8 roundings of at most 2^-23 (the
+matrix cores need not round to the nearest) of sum_d |q_d k_d|, together e; an
+exponential is off by 2^-23 more.  Weights are so off by 2 e + 2^-22, their planes
+by 2^-16 (bfloat16) or 2^-22 (float32), and the two sums of n terms by n 2^-23 each,
+all relative; the output is rounded once, by half a step.  lse is off by e and the
+sum's n 2^-23, and by 2^-22 of itself."""
+import pytest
+import torch
+
+import _cache as C
+from test_gpu_cache_attention import Case
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+LARGEST = 2.0 ** 128 * (1 - 2.0 ** -24)
+
+
+def set_scales(c, which, s):
+    """Scales s [n_pages][Hkv][P] (bfloat16 values) of all groups of the keys (0) or values (1) that are, codes as they are."""
+    part = C.parts(c.mem, c.P, c.D, c.bits)[2 + which].view(torch.bfloat16)
+    held, each = (c.K, c.V)[which], c.D // part.shape[-1]
+    there = torch.isfinite(part)
+    old = torch.where(there, part.double(), 1.0)
+    s = s.to(torch.bfloat16)[..., None].expand(part.shape)
+    held.mul_((s.double() / old).repeat_interleave(each, -1))
+    held.copy_(torch.round(held / s.double().repeat_interleave(each, -1)) * s.double().repeat_interleave(each, -1))
+    part.copy_(torch.where(there, s, part))
+
+
+def check(c, scale):
+    o, lse = c.call(scale)
+    ro, size, rl = C.attention(c.q, c.K, c.V, c.table, c.lengths, None, scale)
+    B, Hq, D = c.q.shape
+    G = Hq // c.Hkv
+    for b in range(B):
+        n = int(c.lengths[b])
+        k = c.K[c.table[b].long()].transpose(1, 2).reshape(-1, c.Hkv, D)[:n]                # [n][Hkv][D]
+        for h in range(Hq):
+            terms = (c.q[b, h].double().abs() * k[:, h // G].abs()).sum(-1).max() * abs(scale)
+            e = (D + 8) * 2.0 ** -23 * float(terms)
+            w = 2 * e + 2.0 ** -22 + (2.0 ** -16 if o.dtype == BF16 else 2.0 ** -22) + 2 * n * 2.0 ** -23
+            off = (o[b, h].double() - ro[b, h]).abs()
+            bound = w * size[b, h] + (2.0 ** -8 if o.dtype == BF16 else 2.0 ** -24) * ro[b, h].abs()
+            assert (off <= bound).all(), (b, h, float((off / size[b, h]).max()), w)
+            gap = abs(float(lse[b, h]) - float(rl[b, h]))
+            assert gap <= e + n * 2.0 ** -23 + 2.0 ** -22 * (1 + abs(float(rl[b, h]))), (b, h, gap, e)
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_keys_up_to_the_largest(D, bits, act):
+    """Rows of up to 2.9e38 (4 bits) and 3.2e38, with queries that bring the scores to a few units."""
+    c = Case([70, 1, 33, 1300], 4, 2, D, 16, bits, act, seed=D)
+    set_scales(c, 0, torch.full(c.K.shape[:3], 1.9375 * 2.0 ** (124 if bits == 4 else 120)))
+    assert 2.8e38 < c.K.abs().max() < 3.3e38
+    c.q = (c.q.float() * 2.0 ** -60).to(act)
+    check(c, 2.0 ** -66 * D ** -0.5)
+
+
+def largest_scale(n, bits):
+    """The largest scale of values of which n stay in the range: n times the largest magnitude (a sixteenth of it of 4
+    bits) below the type's largest, and that itself at most 3.3e38."""
+    top = C.TOP[bits]
+    s = torch.tensor(min(3.3e38 / top, LARGEST / n / top * (16 if bits == 4 else 1)), dtype=torch.float32)
+    return (s.view(torch.int32) & -65536).view(torch.float32)
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("n", [1, 2, 16])
+def test_values_up_to_the_largest(n, bits, act):
+    c = Case([n], 4, 2, 64, 16, bits, act, seed=n)
+    set_scales(c, 1, largest_scale(n, bits).expand(c.V.shape[:3]))
+    check(c, 64 ** -0.5)
