@@ -336,10 +336,11 @@ void cache_attn_kernel(CacheAttnArgs a)
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, s[rt][i]);
-        // what is taken off follows the maximum only when that has passed it by 2^6
+        // What is taken off begins 6 above the maximum and follows only when that has passed it: weights are at most 1, so
+        // that sums over n values of at most a stay within n a
         top = swap_max32(swap_max16(top)) * scale;
-        if (__any(!(top <= low + 6.0f) || m == -INFINITY)) {
-            const float to_m = fmaxf(m, top), nb = to_m == -INFINITY ? 0.0f : to_m;
+        if (__any(!(top <= low) || m == -INFINITY)) {
+            const float to_m = fmaxf(m, top), nb = to_m == -INFINITY ? 0.0f : to_m + 6.0f;
             const float f = __builtin_amdgcn_exp2f(m == -INFINITY ? m : low - nb);
             l *= f;
 #pragma unroll

@@ -1,5 +1,5 @@
 """Attention over quantized caches at the ends of the numbers' range: keys and
-values up to the type's largest.
+values up to the type's largest, sums close to it.
 
 Tolerances, from the arithmetic.  Products of queries (8 bits, or planes of 24) and
 codes (7 bits) are exact.  A score is a sum of D of them, a product with each
@@ -9,6 +9,8 @@ exponential is off by 2^-23 more.  Weights are so off by 2 e + 2^-22, their plan
 by 2^-16 (bfloat16) or 2^-22 (float32), and the two sums of n terms by n 2^-23 each,
 all relative; the output is rounded once, by half a step.  lse is off by e and the
 sum's n 2^-23, and by 2^-22 of itself."""
+import math
+
 import pytest
 import torch
 
@@ -73,8 +75,31 @@ def largest_scale(n, bits):
 
 @pytest.mark.parametrize("act", [F32, BF16])
 @pytest.mark.parametrize("bits", [8, 4])
-@pytest.mark.parametrize("n", [1, 2, 16])
+@pytest.mark.parametrize("n", [1, 2, 16, 100, 700, 5000])
 def test_values_up_to_the_largest(n, bits, act):
     c = Case([n], 4, 2, 64, 16, bits, act, seed=n)
     set_scales(c, 1, largest_scale(n, bits).expand(c.V.shape[:3]))
     check(c, 64 ** -0.5)
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("n", [300, 700, 3000])
+def test_sums_of_scores_that_rise(n, bits, act):
+    """Scores that rise by a factor of 45 (less than 2^6) after the first tiles, values of one sign at the largest: sums of
+    weights above 1 would pass the range."""
+    D = 64
+    c = Case([n], 2, 1, D, 16, bits, act, seed=n)
+    pos = torch.zeros(c.K.shape[:3], dtype=torch.int64)
+    for t in range(n):
+        pos[c.table[0, t // 16], 0, t % 16] = t % 1024 if n > 768 else t
+    for i, x in ((0, c.K), (1, c.V)):                # every key is the same row but for its scale, every value all top codes
+        codes = torch.full((D,), C.TOP[bits], dtype=torch.float64)
+        C.parts(c.mem, 16, D, bits)[i][:] = C.rows_to_bytes(codes, bits)
+        part = C.parts(c.mem, 16, D, bits)[2 + i].view(torch.bfloat16)
+        part.copy_(torch.where(torch.isfinite(part), torch.ones_like(part), part))
+        x.copy_(codes.expand(x.shape))
+    set_scales(c, 0, torch.where(pos < 128, 1.0, 1.5).float())
+    set_scales(c, 1, largest_scale(n, bits).expand(c.V.shape[:3]))
+    c.q = torch.ones_like(c.q)
+    check(c, math.log(45.0) / (0.5 * D * C.TOP[bits]))
