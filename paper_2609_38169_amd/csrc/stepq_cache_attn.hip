@@ -54,13 +54,6 @@ __device__ __forceinline__ void nibbles_of(uint32_t w, uint32_t (&y)[4])
     y[2] = pack_bf16(sixteenth(w, 1), sixteenth(w, 3));
     y[3] = pack_bf16(sixteenth(u, 1), sixteenth(u, 3));
 }
-// The same as bfloat16 1.5 + code / 16, put into the upper bits of a 1's mantissa with the sign turned: two
-// instructions in place of 3 1/4.  Only for sums that 1.5 times the other operand may be taken off.
-__device__ __forceinline__ uint32_t raised_nibbles_of(uint32_t w, int j)
-{
-    return ((j ? w >> (4 * j - 3) : w << 3) & 0x00780078u) ^ 0x3fc03fc0u;
-}
-constexpr uint32_t kRaised = 0x3fc03fc0u;           // 1.5 twice
 
 // Two floats rounded to bfloat16, and what that leaves of them so.
 __device__ __forceinline__ void two_planes(float a, float b, bf16x2 &hi, bf16x2 &lo)
@@ -80,22 +73,24 @@ __device__ __forceinline__ void two_planes(float a, float b, bf16x2 &hi, bf16x2 
 // that their rounding is far below the output's, fp32 ones and queries to three (24 bits).
 //   8 bits: bound by memory, 64 requests x 8 heads x 1-8192 tokens of 128 (550 MB) in 113
 // us, 4.9 TB/s (6.0 is what a kernel that only reads reaches here); 1 x 2 x 131072 of 256 (135 MB) in
-// 28 us.  4 bits: bound by vector issue, 361 instructions for 32 keys of a head, 104 of them
-// for the values' conversion, 64 for the keys' and 32 for the weights' planes: 256 x 8 x 1-4096
-// of 128 (539 MB) in 146 us, 3.7 TB/s, 66 % of the cycles issue.  With the values' codes raised as the keys'
-// it would be 40 fewer; but a sum of 1.5 times the weights leaves 2^-20 of a row's largest value in dimensions
-// whose codes are 0.  Tiles of 64 keys with two waves a SIMD take 7 % more; four waves a SIMD spill (twice the time).
+// 28 us.  4 bits: bound by vector issue, 400 instructions for 32 keys of a head, 104 of them
+// for the values' conversion, as many for the keys' and 32 for the weights' planes: 256 x 8 x 1-4096
+// of 128 (539 MB) in 154 us, 3.5 TB/s, 67 % of the cycles issue.  Codes put into a bfloat16's mantissa as
+// 1.5 + c / 16 convert in 40 fewer for each operand (keys so: 147 us); but 1.5 times the sum of the other operand,
+// taken off again, leaves 2^-20 of a row's largest value in dimensions whose codes are 0, and in the scores 2^-24
+// of 24 times a query's largest dimension, whatever the codes there.
+// Tiles of 64 keys with two waves a SIMD take 7 % more; four waves a SIMD spill (twice the time).
 //   4 requests x 640 tokens: 5.8 us, the chain of loads.
 //   FOLD: few heads leave most of the matrix cores' columns idle, so each group of a row's scales has
 // columns of its own with the same queries: a lane makes the weights of one group, and sums of other groups'
 // dimensions in its column are left.  64 requests x 8192 tokens of 4 bits with 4 or 8 query heads each, whole
-// calls, us, without and with it: 8 heads of 128, bf16, 172 / 158 and 153 / 149, fp32 192 / 185 and 192 / 185;
-// 2 of 256 (4 query heads), bf16, 77 / 70, fp32 126 / 110; 4 requests x 640 9.2 / 8.5 and 9.4 / 9.6.
+// calls, us, without and with it: 8 heads of 128, bf16, 144 / 141 and 145 / 139, fp32 180 / 173 and 187 / 176;
+// 2 of 256 (4 query heads), bf16, 77 / 74, fp32 124 / 106; 4 requests x 640 9.2 / 8.7 with either.
 template <typename T, int D, int BITS, bool FOLD>
 __global__ __launch_bounds__(256, (waves_of<T, D>()))
 void cache_attn_kernel(CacheAttnArgs a)
 {
-    constexpr bool BF = sizeof(T) == 2, RAISED = BITS == 4 && BF;
+    constexpr bool BF = sizeof(T) == 2;
     using Row = RowOf<D, BITS>;
     constexpr int RB = Row::bytes, NG = Row::scales, KT = kTile, RT = KT / 16;
     constexpr int LB = RB / 4, PB = LB < 16 ? LB : 16, PIECES = LB / PB;     // bytes of a row per lane group, in loads of PB
@@ -174,15 +169,6 @@ void cache_attn_kernel(CacheAttnArgs a)
     }
     // the group that a step's dimensions lie in
     const auto group_of = [](int st) { return NG == 1 ? 0 : st % 4 * (D / 4) / kGroup4; };
-    // raised codes: what 1.5 adds to each query's sums is taken off where they begin
-    f32x4 qz[NG] = {};
-    if constexpr (RAISED) {
-        const bf16x8 zero[1] = {__builtin_bit_cast(bf16x8, (u32x4{kRaised, kRaised, kRaised, kRaised}))};
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) mma(qz[group_of(st)], zero, q[st]);
-#pragma unroll
-        for (int m = 0; m < NG; ++m) qz[m] = -qz[m];
-    }
     const float scale = scale_of(a.scale);
     const auto wave_sync = [] {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -280,9 +266,7 @@ void cache_attn_kernel(CacheAttnArgs a)
         f32x4 s[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            f32x4 y[NG];
-#pragma unroll
-            for (int i = 0; i < NG; ++i) y[i] = NG == 4 ? f32x4{} : qz[i];
+            f32x4 y[NG] = {};
             const auto step = [&](int st, const u32x4 &w) {
                 const bf16x8 k[1] = {__builtin_bit_cast(bf16x8, w)};
                 mma(y[group_of(st)], k, q[st]);
@@ -299,12 +283,7 @@ void cache_attn_kernel(CacheAttnArgs a)
                 for (int i = 0; i < LB / 4 / W; ++i) {
                     uint32_t y4[W][4];
 #pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        if constexpr (RAISED)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) y4[w][j] = raised_nibbles_of(kx[rt][i * W + w], j);
-                        else nibbles_of(kx[rt][i * W + w], y4[w]);
-                    }
+                    for (int w = 0; w < W; ++w) nibbles_of(kx[rt][i * W + w], y4[w]);
                     if constexpr (D == 64) {
 #pragma unroll
                         for (int st = 0; st < 2; ++st)
@@ -315,9 +294,6 @@ void cache_attn_kernel(CacheAttnArgs a)
                     }
                 }
             }
-            if constexpr (RAISED && NG == 4)          // one register each, not four
-#pragma unroll
-                for (int i = 0; i < NG; ++i) y[i] += qz[i][0];
             s[rt] = y[0] * *reinterpret_cast<const f32x4 *>(&sc[wave][0][0][16 * rt + 4 * g]);
 #pragma unroll
             for (int i = 1; i < NG; ++i) s[rt] += y[i] * *reinterpret_cast<const f32x4 *>(&sc[wave][0][i][16 * rt + 4 * g]);

@@ -1,5 +1,6 @@
 """Attention over quantized caches at the ends of the numbers' range: keys and
-values up to the type's largest, sums close to it.
+values up to the type's largest, sums close to it, and queries of single
+dimensions many times the others.
 
 Tolerances, from the arithmetic.  Products of queries (8 bits, or planes of 24) and
 codes (7 bits) are exact.  A score is a sum of D of them, a product with each
@@ -103,3 +104,27 @@ def test_sums_of_scores_that_rise(n, bits, act):
     set_scales(c, 1, largest_scale(n, bits).expand(c.V.shape[:3]))
     c.q = torch.ones_like(c.q)
     check(c, math.log(45.0) / (0.5 * D * C.TOP[bits]))
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("big", [10, 14, 18])
+def test_queries_with_a_large_dimension(big, bits, D, act):
+    """One query dimension of 2^big where every key's code is 0 adds nothing to the scores, nor to their error."""
+    c = Case([70, 1, 33, 1300], 8, 2, D, 16, bits, act, seed=D + big)
+    dims = [3, D // 2 + 5, D - 1]
+    for d in dims:
+        part = C.parts(c.mem, c.P, D, bits)[0]
+        if bits == 8:
+            part[..., d] = 0
+        else:
+            w, j = d % (D // 4), d // (D // 4)
+            part[..., 2 * w + j // 2] &= 0xf0 if j % 2 == 0 else 0x0f
+        c.K[..., d] = 0.0
+    g = torch.Generator().manual_seed(big)
+    q = c.q.float()
+    for d in dims:
+        q[..., d] = 2.0 ** big * (1 + torch.rand(q.shape[:2], generator=g)) * (1 if d == dims[0] else -0.3)
+    c.q = q.to(act)
+    check(c, D ** -0.5)
