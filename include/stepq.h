@@ -477,7 +477,7 @@ stepq_status stepq_cache_bytes(const stepq_cache_desc *desc, size_t *cache_bytes
 
 typedef struct {
     int64_t n_tokens;         /* T: tokens of all sequences together, < 2^31 */
-    int32_t n_seq;            /* sequences */
+    int32_t n_seq;            /* sequences, < 2^31 - 64 */
     int32_t max_pages;        /* columns of page_table */
     int32_t act_dtype;        /* stepq_dtype of k and v */
     /* elements from one token to the next (k and v may be slices of one

@@ -46,6 +46,7 @@ struct RowsArgs {
 
 // The sequence that token t belongs to, the last one that begins at or before it (-1: none), and where it begins.
 // A wave's lanes hold 64 of the bounds, spread over all of them; where that does not tell, the rest is looked up.
+// 64 (n_seq / 64 + 1), the largest index and one step, is below 2^31.
 __device__ __forceinline__ int sequence_of(const RowsArgs &a, int t, int *begin)
 {
     *begin = t;
@@ -390,6 +391,7 @@ stepq_status check_tokens(const stepq_cache_desc *d, const stepq_cache_tokens *t
     // a launch has less than 2^32 threads, 8 elements each of keys and values
     if (t->n_tokens >= (int64_t(1) << 31) || static_cast<double>(t->n_tokens) * heads >= 0x1p33)
         return set_error(STEPQ_E_UNSUPPORTED, "2^31 tokens or 2^33 elements or more in one call: split it");
+    if (t->n_seq > INT32_MAX - 64) return set_error(STEPQ_E_UNSUPPORTED, "2^31 - 64 sequences or more");     // see sequence_of
     if (const stepq_status st = check_paged(d, cache, t->n_seq, t->max_pages, table)) return st;
     if (t->n_tokens && t->n_seq && (!starts || !k || !v)) return bad("NULL starts or token rows");
     const int el = t->act_dtype == STEPQ_F32 ? 4 : 2;

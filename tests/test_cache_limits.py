@@ -5,7 +5,7 @@ import ctypes
 import pytest
 
 from paper_2609_38169_amd import stepq
-from test_cache_host import UNSUPPORTED, P, attn, cache, size
+from test_cache_host import UNSUPPORTED, P, attn, cache, size, tokens
 
 
 @pytest.mark.parametrize("bits", [8, 4])
@@ -18,3 +18,12 @@ def test_scales(bits):
         d = attn(scale=scale)
         assert size(L.stepq_cache_attention_workspace, c, d)[0] == UNSUPPORTED and "scale" in stepq.stepq_last_error()
         assert L.stepq_cache_attention(ctypes.byref(c), ctypes.byref(d), P, P, P, P, None, P, P, P, 1 << 40, None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("n_seq", [2 ** 31 - 64, 2 ** 31 - 1])
+def test_sequences(n_seq):
+    """The search for a token's sequence adds a 64th of them, and one, to an index: in 32 bits up to 2^31 - 65."""
+    L, c, t = stepq.lib(), cache(), tokens(n_seq=n_seq)
+    for f in (L.stepq_cache_write, L.stepq_cache_read):
+        assert f(ctypes.byref(c), ctypes.byref(t), P, P, P, P, P, P, None) == UNSUPPORTED
+        assert "sequences" in stepq.stepq_last_error()
