@@ -862,8 +862,8 @@ def _attn_desc(cache, batch, n_q_heads, max_pages, n_select, scale, code):
 def stepq_cache_attention_workspace(cache: Cache, batch, n_q_heads, max_pages, n_select=0,
                                     act_dtype=torch.bfloat16) -> int:
     """Bytes of workspace a stepq_cache_attention call of these sizes takes."""
-    d = _attn_desc(cache, batch, n_q_heads, max_pages, n_select, None,
-                   STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16)
+    d = _attn_desc(cache, *(_whole(x, n, 32) for x, n in zip((batch, n_q_heads, max_pages, n_select), (
+        "batch", "n_q_heads", "max_pages", "n_select"))), None, STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16)
     n = ctypes.c_size_t()
     _check(lib().stepq_cache_attention_workspace(ctypes.byref(cache.desc), ctypes.byref(d), ctypes.byref(n)))
     return n.value
@@ -916,8 +916,9 @@ def stepq_cache_bounds(cache: Cache, page_table, starts, lengths, bounds, stream
 def stepq_cache_select_workspace(cache: Cache, batch, n_q_heads, max_pages, n_select, n_first=1, n_last=1,
                                  act_dtype=torch.bfloat16) -> int:
     """Bytes of workspace a stepq_cache_select call of these sizes takes."""
-    d = stepq_cache_select_desc(batch, n_q_heads, max_pages, STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16,
-                                n_select, n_first, n_last)
+    b, h, m, s, first, last = (_whole(x, n, 32) for x, n in zip((batch, n_q_heads, max_pages, n_select, n_first, n_last), (
+        "batch", "n_q_heads", "max_pages", "n_select", "n_first", "n_last")))
+    d = stepq_cache_select_desc(b, h, m, STEPQ_F32 if act_dtype == torch.float32 else STEPQ_BF16, s, first, last)
     n = ctypes.c_size_t()
     _check(lib().stepq_cache_select_workspace(ctypes.byref(cache.desc), ctypes.byref(d), ctypes.byref(n)))
     return n.value

@@ -3,6 +3,7 @@ that they take: host only, nothing here reaches a launch."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2609_38169_amd import stepq
 from test_cache_host import UNSUPPORTED, P, attn, cache, size, tokens
@@ -27,3 +28,17 @@ def test_sequences(n_seq):
     for f in (L.stepq_cache_write, L.stepq_cache_read):
         assert f(ctypes.byref(c), ctypes.byref(t), P, P, P, P, P, P, None) == UNSUPPORTED
         assert "sequences" in stepq.stepq_last_error()
+
+
+def test_counts_that_no_field_holds():
+    """The workspaces' sizes are of the counts asked for, or of none."""
+    m = torch.zeros(4096, dtype=torch.uint8)
+    m = m[-m.data_ptr() % 128:]
+    c = stepq.Cache(1, 2, 1, 64, 8, memory=m)
+    for f, args in ((stepq.stepq_cache_attention_workspace, (1, 2, 100, 0)),
+                    (stepq.stepq_cache_select_workspace, (1, 2, 100, 5, 1, 1))):
+        f(c, *args)
+        for i in range(len(args)):
+            for bad in (2 ** 32 + args[i], 2 ** 31, 0.5):
+                with pytest.raises(ValueError):
+                    f(c, *args[:i], bad, *args[i + 1:])
