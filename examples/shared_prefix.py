@@ -126,7 +126,7 @@ class Server:
             cache.bounds(table, starts, last, self.bounds[i])
         q, o = q.contiguous(), torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if select:
-            cache.select(q, self.bounds[i], table, last, self.selected)
+            cache.select(q, self.bounds[i], table, last, self.selected, n_first=min(1, self.select - 1))
         cache.attend(q, row_table, row_lengths, o, selected=self.selected if select else None)
         return o
 
