@@ -2,8 +2,9 @@
 // (the layout is defined in include/stepq.h), and the checks of their descriptor.
 #pragma once
 
-#include "stepq_seq.h"
+#include "stepq_div.h"
 #include "stepq_plan.h"
+#include "stepq_seq.h"
 
 namespace stepq {
 
@@ -40,12 +41,6 @@ inline CacheView cache_view(const stepq_cache_desc *d, const void *mem)
 stepq_status check_cache(const stepq_cache_desc *d);
 // A cache's memory and the tables of a call with n requests of max_pages pages each.
 stepq_status check_paged(const stepq_cache_desc *d, const void *cache, int32_t n, int32_t max_pages, const int32_t *page_table);
-
-__device__ __forceinline__ int page_of(int t, FastDiv d)
-{
-    const uint32_t u = static_cast<uint32_t>(t);
-    return static_cast<int>((__umulhi(u, d.mul) + u) >> d.shift);
-}
 
 // The record of head hk of page id; NULL: no such page.
 __device__ __forceinline__ uint8_t *record_of(const CacheView &c, int id, int hk)

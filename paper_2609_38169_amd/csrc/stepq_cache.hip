@@ -81,7 +81,7 @@ __device__ __forceinline__ uint8_t *place_of(const RowsArgs &a, int t, int *row,
     const int start = a.starts[s];
     const int64_t pos = static_cast<int64_t>(start) + (static_cast<int64_t>(t) - begin);
     if (start < 0 || pos >= static_cast<int64_t>(a.max_pages) * a.c.page) return nullptr;
-    const int p = page_of(static_cast<int>(pos), a.c.div_page);
+    const int p = fdiv(static_cast<int>(pos), a.c.div_page);
     *row = static_cast<int>(pos) - p * a.c.page;
     return record_of(a.c, a.table[static_cast<size_t>(s) * a.max_pages + p], 0);
 }
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(RowsArgs a)
     constexpr int rows = kThreads / S::lanes, per = S::runs / Row::scales;    // runs of one group: all (8 bits, D = 64), 2 or 1
     constexpr float q = BITS == 8 ? 127.0f : 7.0f, below = (1.0f - 0x1p-22f) / q;
     const int lane = threadIdx.x % S::lanes;
-    const int block = page_of(blockIdx.x, a.div_slices), slice = blockIdx.x - block * a.slices;
+    const int block = fdiv(blockIdx.x, a.div_slices), slice = blockIdx.x - block * a.slices;
     const int64_t t64 = static_cast<int64_t>(block) * rows + threadIdx.x / S::lanes;
     const int t = static_cast<int>(min(t64, static_cast<int64_t>(a.n_tokens - 1)));
     int row = 0;
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(RowsArgs a)
     using Row = RowOf<D, BITS>;
     constexpr int lanes = D / 8, rows = kThreads / lanes, U = 4;
     const int lane = threadIdx.x % lanes, d0 = lane * 8;
-    const int block = page_of(blockIdx.x, a.div_slices), slice = blockIdx.x - block * a.slices;
+    const int block = fdiv(blockIdx.x, a.div_slices), slice = blockIdx.x - block * a.slices;
     const int64_t t64 = static_cast<int64_t>(block) * rows + threadIdx.x / lanes;
     const int t = static_cast<int>(min(t64, static_cast<int64_t>(a.n_tokens - 1)));
     int row = 0;
@@ -278,7 +278,7 @@ struct BoundsArgs {
     CacheView c;
     const int32_t *table, *starts, *lengths;
     bf16_t *bounds;                      // [n_pages][Hkv][2][D]
-    int32_t batch, max_pages, turns;     // workgroups that take the pages of one (request, head) in turn
+    int32_t max_pages, turns;            // workgroups that take the pages of one (request, head) in turn
 };
 
 // Towards -inf to bfloat16.
@@ -310,8 +310,8 @@ __global__ __launch_bounds__(kThreads) void cache_bounds_kernel(BoundsArgs a)
     const int len = static_cast<int>(min(static_cast<int64_t>(max(a.lengths[b], 0)), static_cast<int64_t>(a.max_pages) * a.c.page));
     const int start = a.starts[b];
     if (start < 0 || start >= len) return;
-    const int last = page_of(len - 1, a.c.div_page);
-    for (int p = page_of(start, a.c.div_page) + turn; p <= last; p += a.turns) {
+    const int last = fdiv(len - 1, a.c.div_page);
+    for (int p = fdiv(start, a.c.div_page) + turn; p <= last; p += a.turns) {
         const int id = a.table[static_cast<size_t>(b) * a.max_pages + p];
         const uint8_t *rec = record_of(a.c, id, hk);
         if (!rec) continue;
@@ -482,7 +482,7 @@ extern "C" stepq_status stepq_cache_bounds(const stepq_cache_desc *d, const void
     if (!aligned(bounds, 16)) return bad("bounds must be 16-byte aligned");
     const int64_t pairs = static_cast<int64_t>(batch) * d->n_kv_heads;
     const int32_t turns = static_cast<int32_t>(std::clamp<int64_t>(1024 / pairs, 1, max_pages));
-    const BoundsArgs a{cache_view(d, cache), page_table, starts, lengths, static_cast<bf16_t *>(bounds), batch, max_pages, turns};
+    const BoundsArgs a{cache_view(d, cache), page_table, starts, lengths, static_cast<bf16_t *>(bounds), max_pages, turns};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_shape(d, [&](auto D, auto B) {
         cache_bounds_kernel<D, B><<<dim3(static_cast<unsigned>(pairs * turns)), kThreads, 0, s>>>(a);

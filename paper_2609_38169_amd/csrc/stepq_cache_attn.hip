@@ -112,8 +112,8 @@ void cache_attn_kernel(CacheAttnArgs a)
     const int32_t *table = a.table + static_cast<size_t>(b) * a.max_pages;
     const int32_t *chosen = a.selected ? a.selected + static_cast<size_t>(bh) * a.n_select : nullptr;
     const int from = part * a.chunk, most = (chosen ? a.n_select : a.max_pages) * page;
-    const int first_page = page_of(from, a.c.div_page);
-    const int end_page = most ? page_of(min(most, from + a.chunk) - 1, a.c.div_page) + 1 : 0;
+    const int first_page = fdiv(from, a.c.div_page);
+    const int end_page = most ? fdiv(min(most, from + a.chunk) - 1, a.c.div_page) + 1 : 0;
     // page p's position and id; both are looked up before the length is there
     const auto look = [&](int p, int &pos, int &id) {
         pos = chosen ? chosen[p] : p;
@@ -189,7 +189,7 @@ void cache_attn_kernel(CacheAttnArgs a)
         at = 0, unit = 0, row = 0;
         bool ok = false;
         if (t < to) {
-            const int p = page_of(t, a.c.div_page), in_page = t - p * page;
+            const int p = fdiv(t, a.c.div_page), in_page = t - p * page;
             const int2 e = pages[p - first_page];
             ok = e.x >= 0 && in_page < e.y;
             if (ok) at = static_cast<int64_t>(e.x) * a.c.record, row = in_page, unit = e.x * record_units + in_page * (RB / 32);

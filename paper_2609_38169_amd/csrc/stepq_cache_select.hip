@@ -21,7 +21,7 @@ struct SelectArgs {
 __device__ __forceinline__ int pages_of(const SelectArgs &a, int b)
 {
     const int len = static_cast<int>(min(static_cast<int64_t>(max(a.lengths[b], 0)), static_cast<int64_t>(a.max_pages) * a.page));
-    return len ? page_of(len - 1, a.div_page) + 1 : 0;
+    return len ? fdiv(len - 1, a.div_page) + 1 : 0;
 }
 
 // Scores as whole numbers that order as they do; NaN above all (and 0, below -inf, for a page that there is not).

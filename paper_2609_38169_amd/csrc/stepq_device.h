@@ -6,6 +6,7 @@
 // everything here is internal to the including translation unit.
 #pragma once
 
+#include "stepq_div.h"
 #include "stepq_internal.h"
 
 namespace stepq {
@@ -137,12 +138,6 @@ __device__ __forceinline__ float sbyte(uint32_t w, int e)
 __device__ __forceinline__ float uniform_f(float x)
 {
     return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x)));
-}
-
-__device__ __forceinline__ int fdiv(int n, FastDiv d)
-{
-    const uint32_t u = static_cast<uint32_t>(n);
-    return static_cast<int>((__umulhi(u, d.mul) + u) >> d.shift);
 }
 
 template <int CTRL, int ROWS>

@@ -1,16 +1,11 @@
 // Shared by the attention kernels: reductions over the lanes that hold a query's scores, and the scale's place.
 #pragma once
 
+#include "stepq_div.h"
 #include "stepq_mma.h"
 #include "stepq_plan.h"
 
 namespace stepq {
-
-__device__ __forceinline__ int fdiv(int n, FastDiv d)
-{
-    const uint32_t u = static_cast<uint32_t>(n);
-    return static_cast<int>((__umulhi(u, d.mul) + u) >> d.shift);
-}
 
 constexpr float kLn2 = 0.6931471805599453f;
 
