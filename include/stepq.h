@@ -525,9 +525,10 @@ typedef struct {
  * scores -inf, gets o = 0 and lse = -inf.  A key that is not finite makes its heads'
  * o NaN, a value its group of dimensions; a query that is not finite may make its
  * own so.  Scores, weights and sums are fp32, weights in 16 bits (bfloat16) or 24
- * (fp32).  Sums are formed before they are divided: of n tokens whose values are at
- * most a, o is finite where n a (n a / 16 of 4 bits) is below 3.4e38, for queries up to
- * 2^112 and scores below 2e38.  o overlaps no input. */
+ * (fp32; fewer beside 8-bit values below 2^-96).  Sums are formed before they are
+ * divided: of n tokens whose values are at most a, o is finite where n a (n a / 16 of
+ * 4 bits) is below 3.4e38, with queries up to 2^112 and sums of |q_d k_d| below 2e38,
+ * times the scale as well.  o overlaps no input. */
 stepq_status stepq_cache_attention_workspace(const stepq_cache_desc *desc, const stepq_cache_attn_desc *attn,
                                              size_t *bytes);
 stepq_status stepq_cache_attention(const stepq_cache_desc *desc, const stepq_cache_attn_desc *attn, const void *cache,

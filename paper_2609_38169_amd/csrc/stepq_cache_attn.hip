@@ -78,7 +78,7 @@ __device__ __forceinline__ void two_planes(float a, float b, bf16x2 &hi, bf16x2 
 // of 128 (539 MB) in 154 us, 3.5 TB/s, 67 % of the cycles issue.  Codes put into a bfloat16's mantissa as
 // 1.5 + c / 16 convert in 40 fewer for each operand (keys so: 147 us); but 1.5 times the sum of the other operand,
 // taken off again, leaves 2^-20 of a row's largest value in dimensions whose codes are 0, and in the scores 2^-24
-// of 24 times a query's largest dimension, whatever the codes there.
+// of 24 times a query's largest dimension and the key's scale, whatever the codes there.
 // Tiles of 64 keys with two waves a SIMD take 7 % more; four waves a SIMD spill (twice the time).
 //   4 requests x 640 tokens: 5.8 us, the chain of loads.
 //   FOLD: few heads leave most of the matrix cores' columns idle, so each group of a row's scales has
@@ -559,12 +559,15 @@ Cut cut_of(const stepq_cache_desc *c, const stepq_cache_attn_desc *d)
 {
     const int64_t tokens = static_cast<int64_t>(d->n_select ? d->n_select : d->max_pages) * c->page_size;
     if (d->batch == 0 || tokens == 0) return {kMaxChunk, 1};
-    // Two workgroups a CU (one of D = 256), of 256 to 1024 tokens; whole calls, us, at 256 / 512 / 768 / 1024:
+    // Ranges of 256 to 1024 tokens, so many that there are two for a CU, or one of D = 256 (registers let three or two run at
+    // once, in fp32 two or one); whole calls, us, at 256 / 512 / 768 / 1024 under tables as wide as the longest request:
     //   8 heads of 128, 8 bits, bf16: 1 request x 32768 tokens 21.0 / 19.1 / 21.4 / 24; 16 x 1024 13.4 / 13.4 / 15.8 / 18;
     //     64 x 4096 122 / 110 / 106 / 105; 64 x 1-8192 138 / 125 / - / 117; 2 heads, 2 x 4096 9.6 / 11.9 / 15.0 / 16
     //   2 heads of 256, 8 bits: 1 x 131072 51 / 39 / - / 33; 64 x 8192 125 / 116 / 113 / 105
     // A join, a second launch, takes 3 us more, which a workgroup spends on 768 tokens (512 in fp32): 4 requests x 640 6.2
     // in one part, 9.3 in three; 23 x 1333 in fp32 14.8 in two, 10.6 in six.
+    // Lengths are on the device: what is cut is the table.  Ranges past a request's length end at once, but are launched;
+    // under a table for 131072 tokens 4 x 1-640 take 7.6 us for 5.9, 64 x 1-8192 145 for 116, 256 x 1-4096 of 4 bits 301 for 156.
     const int64_t G = d->n_q_heads / c->n_kv_heads, blocks = static_cast<int64_t>(d->batch) * c->n_kv_heads * ((G + 15) / 16);
     const int64_t fill = c->head_dim == 256 ? 256 : 512, one = d->act_dtype == STEPQ_BF16 ? 768 : 512;
     const int64_t want = std::clamp<int64_t>((blocks * tokens + fill - 1) / fill, 256, kMaxChunk);
